@@ -1,0 +1,556 @@
+// The matrix product behind the linear layer and its gradients: out[m][n] = sum over k of A(m, k) B(n, k),
+// 16-bit operands, 32-bit sums, on the matrix cores.
+//
+// Operands lie in memory either with k running along a row ("row": x and w of the forward pass, dy of
+// the input's gradient) or with m or n running along it ("col": w of the input's gradient, dy and x of
+// the weight's).  Both go to LDS as they lie, 16 bytes a lane, and come out of it as the matrix cores
+// want them: a lane of v_mfma_f32_32x32x16 holds eight consecutive k of one m or n, which a row operand
+// has next to each other (one 16-byte read) and a col operand below each other (two reads that
+// transpose 4 x 16 values among 16 lanes, ds_read_b64_tr_b16).
+//
+// A workgroup computes BM x BN of the output, 64 of k at a time, in two buffers: while one is
+// multiplied, the loads of the next run straight into the other.
+#pragma once
+
+#include <type_traits>
+
+#include "moc_training.h"
+
+namespace {
+
+constexpr int kStepK = 64;                      // k of a step
+constexpr int kRowBytes = kStepK * 2;           // of a row operand's row in LDS
+constexpr int kWindow = 0x7FFFFFF0;             // bytes a buffer descriptor covers; an offset of this reads as 0
+
+using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
+using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
+using f32x16 = float __attribute__((ext_vector_type(16)));
+using s16x4 = short __attribute__((ext_vector_type(4)));
+using s16x8 = short __attribute__((ext_vector_type(8)));
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
+
+template <int TYPE>
+__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+  if constexpr (TYPE == MOC_BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+enum { kRow = 0, kCol = 1 };                       // how an operand lies
+enum { kDirect = 0, kThroughRegisters = 1 };       // how it gets to LDS
+
+struct Operand {
+  const void* data;
+  const uint8_t* scales;     // a checkpoint's
+  int64_t stride, scale_stride;
+};
+
+struct Epilogue {
+  const void* bias;
+  int bias_type;
+  int act;
+  const void* residual;
+  int residual_type;
+  int64_t residual_stride;
+  const void* pre;            // the activation's argument: times its derivative
+  const uint8_t* pre_scales;
+  int pre_type;
+  int64_t pre_stride, pre_scale_stride;
+  void* out;
+  int out_type;
+  int64_t out_stride;
+  uint8_t *codes, *scales;    // the checkpoint of what the activation is taken of; null: none
+  int kept_type;
+  int64_t code_stride, scale_stride;
+  float most;
+};
+
+struct LinearArgs {
+  Operand a, b;
+  int m, n, k;
+  int tiles_m, tiles_n, splits, split_k;   // split_k: k of a split, a multiple of kStepK
+  float* partial;                          // [splits][m][partial_stride], splits > 1 only
+  int64_t partial_stride;                  // n up to a multiple of MOC_BLOCK
+  Epilogue e;
+};
+
+// ---- epilogue -----------------------------------------------------------------------------------
+
+__device__ __forceinline__ const char* row_at(const void* x, int type, int64_t row, int64_t stride) {
+  return static_cast<const char*>(x) + row * stride * (type == MOC_F32 ? 4 : type == MOC_BF16 || type == MOC_F16 ? 2 : 1);
+}
+
+// What is left of a run after the bias and the checkpoint.
+__device__ __forceinline__ void finish_run(const Epilogue& e, int64_t row, int col, int n, float (&v)[kRun]) {
+  if (e.pre) {
+    float u[kRun];
+    const char* p = row_at(e.pre, e.pre_type, row, e.pre_stride);
+    if (e.pre_type == MOC_E4M3) load_held<MOC_E4M3>(p, e.pre_scales + row * e.pre_scale_stride, col, n, u);
+    else if (e.pre_type == MOC_I8) load_held<MOC_I8>(p, e.pre_scales + row * e.pre_scale_stride, col, n, u);
+    else load_any(e.pre_type, p, col, n, u);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = times_slope(e.act, v[i], u[i]);
+  } else if (e.act != MOC_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = act_of(e.act, v[i]);
+  }
+  if (e.residual) {
+    float r[kRun];
+    load_any(e.residual_type, row_at(e.residual, e.residual_type, row, e.residual_stride), col, n, r);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] += r[i];
+  }
+  store_any(e.out_type, const_cast<char*>(row_at(e.out, e.out_type, row, e.out_stride)), col, n, v);
+}
+
+// A run of finished sums; the four lanes of a quad have a block of a row, n <= 0 beyond the row.
+__device__ __forceinline__ void finish_sum(const Epilogue& e, int64_t row, int col, int n, const float (&bias)[kRun], float (&v)[kRun]) {
+#pragma unroll
+  for (int r = 0; r < kRun; ++r) v[r] = r < n ? v[r] + bias[r] : 0.0f;
+  if (e.codes) keep_any(e.kept_type, v, col, n, e.most, e.codes + row * e.code_stride, e.scales + row * e.scale_stride);
+  if (n > 0) finish_run(e, row, col, n, v);
+}
+
+// ---- operands to LDS ----------------------------------------------------------------------------
+
+using Lds = __attribute__((address_space(3))) uint8_t;
+
+// Which 16 bytes of its row of the tile lie at place `pos` of row `row` in LDS.  Reads of one
+// instruction then meet all banks evenly: 16 rows of a row operand at one k, 4 rows of a col operand.
+template <int LAY, int WIDTH>
+__device__ __forceinline__ int swizzle(int row) {
+  if constexpr (LAY == kRow) return (row >> 1) & 7;
+  else if constexpr (WIDTH >= 128) return (row & 3) << 2;
+  else if constexpr (WIDTH == 64) return ((row >> 1) & 1) << 2;
+  else return 0;
+}
+
+// The part of an operand that a workgroup goes through: WIDTH of m or n from `first`, k from `begin`.
+template <int LAY, int WIDTH, int THREADS>
+struct Tile {
+  static constexpr int kPieces = WIDTH * 8;                    // 16 bytes each
+  static constexpr int kEach = kPieces / THREADS;              // of a thread
+  static constexpr int kPerRow = LAY == kRow ? 8 : WIDTH / 8;  // of a row in LDS
+  static_assert(kPieces % THREADS == 0);
+  // the row in LDS, and the 16 bytes of the tile's row, of piece i of this thread
+  static __device__ __forceinline__ int row(int i) { return (i * THREADS + (int)threadIdx.x) / kPerRow; }
+  static __device__ __forceinline__ int piece(int i) {
+    return ((i * THREADS + (int)threadIdx.x) % kPerRow) ^ swizzle<LAY, WIDTH>(row(i));
+  }
+};
+
+// Straight into LDS by buffer loads, which read 0 beyond their window: offsets are set once, the
+// window's base moves with k.  Rows, and runs of eight along a row, are whole here.
+template <int LAY, int WIDTH, int THREADS>
+struct DirectLoader {
+  using T = Tile<LAY, WIDTH, THREADS>;
+  const char* base;       // of the window: the tile's first row and k
+  int64_t left;           // bytes from there to the operand's end
+  int64_t step;           // bytes the base moves by
+  int offset[T::kEach];
+  int k_left;
+
+  __device__ __forceinline__ DirectLoader(const Operand& x, int first, int extent, int begin, int end) {
+    const int64_t rb = x.stride * 2;
+    const char* const data = static_cast<const char*>(x.data);
+    if constexpr (LAY == kRow) {
+      base = data + first * rb + (int64_t)begin * 2;
+      left = (int64_t)(extent - first - 1) * rb + (int64_t)(end - begin) * 2;
+      step = kRowBytes;
+    } else {
+      base = data + begin * rb + (int64_t)first * 2;
+      left = (int64_t)(end - begin - 1) * rb + (int64_t)(extent - first) * 2;
+      step = kStepK * rb;
+    }
+    k_left = end - begin;
+#pragma unroll
+    for (int i = 0; i < T::kEach; ++i) {
+      const int row = T::row(i), piece = T::piece(i);
+      offset[i] = (int)(row * rb) + piece * 16;
+      if (LAY == kCol && first + piece * 8 >= extent) offset[i] = kWindow;
+    }
+  }
+  __device__ __forceinline__ void load(Lds* to) {
+    const __amdgpu_buffer_rsrc_t window =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (int)(left < kWindow ? (left > 0 ? left : 0) : kWindow), 0x00020000);
+    const bool last = LAY == kRow && k_left < kStepK;
+#pragma unroll
+    for (int i = 0; i < T::kEach; ++i) {
+      int at = offset[i];
+      if (last && T::piece(i) * 8 >= k_left) at = kWindow;
+      const int wave = (i * THREADS + ((int)threadIdx.x & ~(kWave - 1))) * 16;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(window, (__attribute__((address_space(3))) void*)(to + __builtin_amdgcn_readfirstlane(wave)), 16, at, 0, 0, 0);
+    }
+    base += step;
+    left -= step;
+    k_left -= kStepK;
+  }
+  __device__ __forceinline__ void put(Lds*) {}
+};
+
+// Through registers: any alignment and size, and checkpoints, whose codes become values on the way.
+template <int LAY, int WIDTH, int THREADS, int TYPE, int HELD>
+struct RegisterLoader {
+  using T = Tile<LAY, WIDTH, THREADS>;
+  using V = typename Stored<TYPE>::type;
+  static constexpr bool kKept = HELD == MOC_E4M3 || HELD == MOC_I8;
+  Operand x;
+  int first, extent, k, end;
+  uint4 held[T::kEach];        // 16-bit values, or eight codes and their scale
+  uint8_t scale[kKept ? T::kEach : 1];
+
+  __device__ __forceinline__ RegisterLoader(const Operand& x_, int first_, int extent_, int begin, int end_) : x(x_), first(first_), extent(extent_), k(begin), end(end_) {}
+
+  __device__ __forceinline__ void load(Lds*) {
+#pragma unroll
+    for (int i = 0; i < T::kEach; ++i) {
+      const int row = T::row(i), piece = T::piece(i) * 8;
+      // the memory's row and the place in it, and how many of the eight exist
+      const int r = LAY == kRow ? first + row : k + row, c = LAY == kRow ? k + piece : first + piece;
+      const int n = r < (LAY == kRow ? extent : end) ? (LAY == kRow ? end : extent) - c : 0;
+      held[i] = uint4{0, 0, 0, 0};
+      if constexpr (kKept) {
+        scale[i] = 0;
+        if (n > 0) {
+          const uint2 codes = load_codes(static_cast<const uint8_t*>(x.data) + r * x.stride + c, n);
+          held[i].x = codes.x;
+          held[i].y = codes.y;
+          scale[i] = x.scales[r * x.scale_stride + c / MOC_BLOCK];
+        }
+      } else {
+        const uint16_t* p = static_cast<const uint16_t*>(x.data) + r * x.stride + c;
+        if (n >= 8) {
+          __builtin_memcpy(&held[i], p, 16);
+        } else if (n > 0) {
+          uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int j = 0; j < 7; ++j)
+            if (j < n) w[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
+          held[i] = uint4{w[0], w[1], w[2], w[3]};
+        }
+      }
+    }
+    k += kStepK;
+  }
+  __device__ __forceinline__ void put(Lds* to) {
+#pragma unroll
+    for (int i = 0; i < T::kEach; ++i) {
+      u32x4 out = {held[i].x, held[i].y, held[i].z, held[i].w};
+      if constexpr (kKept) {
+        float v[kRun];
+        decode_run<HELD>(uint2{held[i].x, held[i].y}, scale_of(scale[i]), v);
+        V t[kRun];
+#pragma unroll
+        for (int j = 0; j < kRun; ++j) t[j] = (V)v[j];
+        __builtin_memcpy(&out, t, 16);
+      }
+      *(__attribute__((address_space(3))) u32x4*)(to + (i * THREADS + (int)threadIdx.x) * 16) = out;
+    }
+  }
+};
+
+// ---- LDS to the matrix cores --------------------------------------------------------------------
+
+// 32 x 16 pieces of an operand for one wave, whose m or n start at `first` in the tile.
+template <int LAY, int WIDTH, int COUNT>
+struct Reader {
+  int at[COUNT][LAY == kRow ? 4 : 1];
+
+  __device__ __forceinline__ explicit Reader(int first) {
+    const int lane = threadIdx.x & (kWave - 1);
+    if constexpr (LAY == kRow) {
+      const int row = first + (lane & 31);
+#pragma unroll
+      for (int c = 0; c < COUNT; ++c)
+#pragma unroll
+        for (int s = 0; s < 4; ++s) at[c][s] = (row + 32 * c) * kRowBytes + ((2 * s + (lane >> 5)) ^ swizzle<LAY, WIDTH>(row)) * 16;
+    } else {
+      const int in = lane & 15, k = (lane >> 5) * 8 + (in >> 2);   // swizzle() looks at k % 4 only
+#pragma unroll
+      for (int c = 0; c < COUNT; ++c) {
+        const int col = first + 32 * c + ((lane >> 4) & 1) * 16 + (in & 3) * 4;
+        at[c][0] = k * WIDTH * 2 + ((col >> 3) ^ swizzle<LAY, WIDTH>(in >> 2)) * 16 + (col & 7) * 2;
+      }
+    }
+  }
+  // k of 16 * s .. 16 * s + 15
+  __device__ __forceinline__ s16x8 read(const Lds* from, int c, int s) const {
+    if constexpr (LAY == kRow) {
+      return *(const __attribute__((address_space(3))) s16x8*)(from + at[c][s]);
+    } else {
+      using P = __attribute__((address_space(3))) s16x4*;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(from + at[c][0] + 16 * s * WIDTH * 2));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(from + at[c][0] + (16 * s + 4) * WIDTH * 2));
+      return s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    }
+  }
+};
+
+// ---- the kernel ---------------------------------------------------------------------------------
+
+// TYPE of the operands; HELD: of b, TYPE or a checkpoint's.
+template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int LOAD, int HELD>
+__global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) {
+  constexpr int kThreads = WM * WN * kWave;
+  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;   // 32 x 32 outputs of a wave
+  __shared__ __attribute__((aligned(1024))) uint8_t a0[BM * kRowBytes], a1[BM * kRowBytes], b0[BN * kRowBytes], b1[BN * kRowBytes];
+
+  // Workgroups go round the eight XCDs: each XCD takes a stretch of neighbouring tiles, in groups of
+  // eight rows of tiles, so that what its L2 holds is used again.
+  int64_t tile = blockIdx.x;
+  const int tiles = g.tiles_m * g.tiles_n, per = tiles / 8, more = tiles % 8, xcd = (int)(tile % 8);
+  tile = (int64_t)xcd * per + (xcd < more ? xcd : more) + tile / 8;
+  const int band = 8 * g.tiles_n, first_m = (int)(tile / band) * 8, height = min(8, g.tiles_m - first_m), in = (int)(tile % band);
+  const int m0 = (first_m + in % height) * BM, n0 = in / height * BN;
+  const int begin = blockIdx.y * g.split_k, end = min(g.k, begin + g.split_k);
+
+  using LoadA = typename std::conditional<LOAD == kDirect, DirectLoader<ALAY, BM, kThreads>, RegisterLoader<ALAY, BM, kThreads, TYPE, TYPE>>::type;
+  using LoadB = typename std::conditional<LOAD == kDirect && HELD == TYPE, DirectLoader<BLAY, BN, kThreads>, RegisterLoader<BLAY, BN, kThreads, TYPE, HELD>>::type;
+  LoadA la(g.a, m0, g.m, begin, end);
+  LoadB lb(g.b, n0, g.n, begin, end);
+
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  const Reader<ALAY, BM, TM> ra(wm);
+  const Reader<BLAY, BN, TN> rb(wn);
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  // What is read for 16 of k while the 16 before are multiplied; the scheduler stays between the
+  // barriers, or it would read all of a step first and spill.
+  const auto multiply = [&](const Lds* a, const Lds* b) {
+    s16x8 fa[2][TM], fb[2][TN];
+    const auto fetch = [&](int s) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) fb[s & 1][j] = rb.read(b, j, s);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) fa[s & 1][i] = ra.read(a, i, s);
+    };
+    fetch(0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if (s < 3) fetch(s + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mfma<TYPE>(fb[s & 1][j], fa[s & 1][i], acc[i][j]);   // rows of the result: n
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  Lds *const pa0 = (Lds*)a0, *const pa1 = (Lds*)a1, *const pb0 = (Lds*)b0, *const pb1 = (Lds*)b1;
+  const auto load = [&](Lds* a, Lds* b) {
+    la.load(a);
+    lb.load(b);
+  };
+  const auto put = [&](Lds* a, Lds* b) {
+    la.put(a);
+    lb.put(b);
+  };
+  const auto arrived = [] {
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's loads into LDS
+    __syncthreads();
+  };
+  // Steps in pairs, so that each buffer has its own code (and the compiler sees that the loads do not
+  // touch what is read); an odd one comes first.
+  int steps = end > begin ? (end - begin + kStepK - 1) / kStepK : 0;
+  if (steps & 1) {
+    load(pa1, pb1);
+    put(pa1, pb1);
+    arrived();
+    if (steps > 1) load(pa0, pb0);
+    multiply(pa1, pb1);
+    if (steps > 1) put(pa0, pb0);
+  } else if (steps > 0) {
+    load(pa0, pb0);
+    put(pa0, pb0);
+  }
+  for (steps /= 2; steps > 0; --steps) {
+    arrived();
+    load(pa1, pb1);
+    multiply(pa0, pb0);
+    put(pa1, pb1);
+    arrived();
+    if (steps > 1) load(pa0, pb0);
+    multiply(pa1, pb1);
+    if (steps > 1) put(pa0, pb0);
+  }
+
+  // Out by way of LDS, so that lanes next to each other have runs next to each other and a quad has a
+  // block of 32.  A lane has 16 of the 32 n of one m: 8 * (r / 4) + 4 * (lane / 32) + r % 4.  Every
+  // wave stages its own outputs, 64 rows at a time, in memory of its own; 16 bytes of a row are moved
+  // by the row's number, so that writes (32 rows at once) and reads (whole rows) meet all banks.
+  constexpr int TH = TM < 2 ? TM : 2, kCols = TN * 32, kChunks = kCols / 4, kMove = kChunks < 16 ? kChunks - 1 : 15;
+  constexpr int kStage = TH * 32 * kCols * 4, kPer = (int)sizeof b0 / kStage;   // waves that one of the arrays has room for
+  static_assert(sizeof a0 <= sizeof b0 && kPer >= 1 && (kPer >= WM * WN || (sizeof a0 == sizeof b0 && 4 * kPer >= WM * WN)));
+  __syncthreads();   // the last step's reads
+  const int array = wave / kPer;
+  Lds* const stage = (array == 0 ? pb0 : array == 1 ? pb1 : array == 2 ? pa0 : pa1) + wave % kPer * kStage;
+  const int lane = threadIdx.x & (kWave - 1);
+  constexpr int kRuns = kCols / kRun, kRowsAt = kWave / kRuns;   // runs of a row, rows at a time
+  const int col = n0 + wn + lane % kRuns * kRun, n = g.n - col;
+  float bias[kRun];
+#pragma unroll
+  for (int r = 0; r < kRun; ++r) bias[r] = 0.0f;
+  if (g.e.bias && g.splits == 1 && n > 0) load_any(g.e.bias_type, g.e.bias, col, n, bias);
+#pragma unroll
+  for (int half = 0; half < TM / TH; ++half) {
+#pragma unroll
+    for (int i = 0; i < TH; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int m = 32 * i + (lane & 31), chunk = 8 * j + 2 * q + (lane >> 5);
+          const f32x16& c = acc[half * TH + i][j];
+          *(__attribute__((address_space(3))) f32x4*)(stage + m * (kCols * 4) + (chunk ^ (m & kMove)) * 16) = f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+        }
+#pragma unroll 1
+    for (int m = lane / kRuns; m < TH * 32; m += kRowsAt) {
+      const int row = m0 + wm + half * TH * 32 + m;
+      if (row >= g.m) break;   // all lanes of a row, and of a quad
+      float v[kRun];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 c = *(const __attribute__((address_space(3))) f32x4*)(stage + m * (kCols * 4) + ((lane % kRuns * 2 + h) ^ (m & kMove)) * 16);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[4 * h + r] = c[r];
+      }
+      if (g.splits > 1) {
+        if (col < g.partial_stride) store_run<MOC_F32>(g.partial + ((int64_t)blockIdx.y * g.m + row) * g.partial_stride, col, kRun, v);
+      } else {
+        finish_sum(g.e, row, col, n, bias, v);
+      }
+    }
+  }
+}
+
+// The sum of the splits, in their order, and the epilogue; a thread has a run, a quad a block.
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs g) {
+  const Epilogue& e = g.e;
+  const int runs = (int)(g.partial_stride / kRun);
+  const int64_t total = (int64_t)g.m * runs, i = block_of() * 256 + threadIdx.x;
+  if (i >= total) return;   // whole quads
+  const int64_t row = i / runs;
+  const int col = (int)(i - row * runs) * kRun, n = g.n - col;
+  float v[kRun] = {};
+  const float* from = g.partial + row * g.partial_stride + col;
+  for (int s = 0; s < g.splits; ++s, from += g.m * g.partial_stride) {
+    float p[kRun];
+    load_run<MOC_F32>(from, 0, kRun, p);
+#pragma unroll
+    for (int r = 0; r < kRun; ++r) v[r] += p[r];
+  }
+  float bias[kRun] = {};
+  if (e.bias && n > 0) load_any(e.bias_type, e.bias, col, n, bias);
+  finish_sum(e, row, col, n, bias, v);
+}
+
+// ---- dispatch -----------------------------------------------------------------------------------
+
+// How a product is cut up.
+struct LinearPlan {
+  int tile_m, tile_n;
+  int tiles_m, tiles_n, splits, split_k;
+  int64_t partial_stride, work_bytes;
+};
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+inline LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, bool direct, int units) {
+  LinearPlan p = {};
+  if (m <= 32) {
+    p.tile_m = 32;
+    p.tile_n = 128;
+  } else if (direct && ceil_div(m, 256) * ceil_div(n, 256) * 4 >= 3 * (int64_t)units) {
+    p.tile_m = p.tile_n = 256;
+  } else {
+    p.tile_m = p.tile_n = 128;
+  }
+  p.tiles_m = (int)ceil_div(m, p.tile_m);
+  p.tiles_n = (int)ceil_div(n, p.tile_n);
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, steps = ceil_div(k, kStepK);
+  // Few tiles: k is cut too, at least four steps a split, until two workgroups a compute unit have work.
+  int64_t splits = tiles ? 2 * (int64_t)units / tiles : 1;
+  if (splits > steps / 4) splits = steps / 4;
+  if (splits < 1) splits = 1;
+  const int64_t each = ceil_div(steps, splits);
+  p.splits = (int)(steps ? ceil_div(steps, each) : 1);
+  p.split_k = (int)(each * kStepK);
+  p.partial_stride = ceil_div(n, MOC_BLOCK) * MOC_BLOCK;
+  p.work_bytes = p.splits > 1 ? p.splits * m * p.partial_stride * (int64_t)sizeof(float) : 0;
+  return p;
+}
+
+// Whether an operand of 16-bit values can go straight into LDS, `along` values of it in a row.
+inline bool direct_ok(const moc_matrix* x, int64_t along) { return aligned_to(x->data, 16) && x->stride % 8 == 0 && along % 8 == 0; }
+
+inline Operand operand_of(const moc_matrix* x) { return Operand{x->data, x->scales, x->stride, x->scale_stride}; }
+
+inline void set_out(Epilogue& e, const moc_matrix* out) {
+  e.out = out->data;
+  e.out_type = out->type;
+  e.out_stride = out->stride;
+}
+
+using LinearKernel = void (*)(LinearArgs);
+
+template <int TYPE, int ALAY, int BLAY, int HELD>
+LinearKernel pick_linear(int tile_m, bool direct) {
+  if (direct) {
+    if (tile_m == 256) return linear_kernel<TYPE, ALAY, BLAY, 256, 256, 2, 4, kDirect, HELD>;
+    if (tile_m == 128) return linear_kernel<TYPE, ALAY, BLAY, 128, 128, 2, 2, kDirect, HELD>;
+    return linear_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, kDirect, HELD>;
+  }
+  if (tile_m == 128) return linear_kernel<TYPE, ALAY, BLAY, 128, 128, 2, 2, kThroughRegisters, HELD>;
+  return linear_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, kThroughRegisters, HELD>;
+}
+
+// Queues the product: `g` has the operands, sizes and epilogue; held: b's type.
+template <int ALAY, int BLAY, bool KEPT>
+int queue_linear(LinearArgs g, int type, int held, bool direct, void* work, int64_t work_bytes, void* hip_stream) {
+  int units = 0;
+  const int rc = moc_compute_units(&units);
+  if (rc != MOC_OK) return rc;
+  const LinearPlan p = linear_plan(g.m, g.n, g.k, direct, units);
+  if (p.work_bytes > 0 && (!work || !aligned_to(work, 16) || work_bytes < p.work_bytes)) return MOC_EINVAL;
+  if ((int64_t)p.tiles_m * p.tiles_n > (1 << 22)) return MOC_EOVERFLOW;   // a launch's threads
+  g.tiles_m = p.tiles_m;
+  g.tiles_n = p.tiles_n;
+  g.splits = p.splits;
+  g.split_k = p.split_k;
+  g.partial = static_cast<float*>(work);
+  g.partial_stride = p.partial_stride;
+  LinearKernel kern = nullptr;
+  if constexpr (KEPT) {
+    if (type == MOC_BF16) {
+      kern = held == MOC_E4M3 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_E4M3>(p.tile_m, direct)
+             : held == MOC_I8 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_I8>(p.tile_m, direct)
+                              : pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, direct);
+    } else {
+      kern = held == MOC_E4M3 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_E4M3>(p.tile_m, direct)
+             : held == MOC_I8 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_I8>(p.tile_m, direct)
+                              : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, direct);
+    }
+  } else {
+    kern = type == MOC_BF16 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, direct) : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, direct);
+  }
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  const int threads = p.tile_m == 256 ? 512 : 256;
+  hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(threads), 0, stream, g);
+  MOC_HIP(hipGetLastError());
+  if (p.splits > 1) {
+    hipLaunchKernelGGL(linear_join_kernel, grid_of(ceil_div(g.m * (p.partial_stride / kRun), 256)), dim3(256), 0, stream, g);
+    MOC_HIP(hipGetLastError());
+  }
+  return MOC_OK;
+}
+
+}  // namespace

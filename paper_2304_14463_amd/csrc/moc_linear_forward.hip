@@ -1,0 +1,58 @@
+// The linear layer: act(x w^T + bias) + residual, with the checkpoint of the activation's argument.
+#include "moc_linear.h"
+
+extern "C" {
+
+int moc_linear_forward(int64_t rows, int64_t cin, int64_t cout, const moc_matrix* x, const moc_matrix* w, const void* bias, int32_t bias_type,
+                       int32_t act, const moc_matrix* residual, const moc_matrix* y, const moc_matrix* kept, void* work, int64_t work_bytes,
+                       void* hip_stream) {
+  if (!sizes_ok(rows, cin) || !sizes_ok(rows, cout) || act < MOC_ACT_NONE || act > MOC_ACT_SILU) return MOC_EINVAL;
+  if (!matrix_ok(x, rows, cin, true, false) || x->type == MOC_F32 || !matrix_ok(w, cout, cin, true, false) || w->type != x->type) return MOC_EINVAL;
+  if (!matrix_ok(y, rows, cout, true, false) || (y->type != x->type && y->type != MOC_F32) || !params_ok(bias, bias_type)) return MOC_EINVAL;
+  if (residual && (!matrix_ok(residual, rows, cout, true, false) || (residual->type != x->type && residual->type != MOC_F32))) return MOC_EINVAL;
+  if (kept && !matrix_ok(kept, rows, cout, false, true)) return MOC_EINVAL;
+  if (rows == 0 || cout == 0) return MOC_OK;
+  LinearArgs g = {};
+  g.a = operand_of(x);
+  g.b = operand_of(w);
+  g.m = (int)rows;
+  g.n = (int)cout;
+  g.k = (int)cin;
+  Epilogue& e = g.e;
+  e.bias = bias;
+  e.bias_type = bias_type;
+  e.act = act;
+  if (residual) {
+    e.residual = residual->data;
+    e.residual_type = residual->type;
+    e.residual_stride = residual->stride;
+  }
+  set_out(e, y);
+  if (kept) {
+    e.codes = static_cast<uint8_t*>(kept->data);
+    e.scales = kept->scales;
+    e.kept_type = kept->type;
+    e.code_stride = kept->stride;
+    e.scale_stride = kept->scale_stride;
+    e.most = most_kept(kept->type, x->type);
+  }
+  return queue_linear<kRow, kRow, false>(g, x->type, x->type, direct_ok(x, cin) && direct_ok(w, cin), work, work_bytes, hip_stream);
+}
+
+int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout) {
+  if (!sizes_ok(rows, cin) || !sizes_ok(rows, cout)) return MOC_EINVAL;
+  int units = 0;
+  const int rc = moc_compute_units(&units);
+  if (rc != MOC_OK) return rc;
+  int64_t most = 0;
+  for (int direct = 0; direct < 2; ++direct) {
+    const int64_t sizes[3][3] = {{rows, cout, cin}, {rows, cin, cout}, {cout, cin, rows}};
+    for (const auto& s : sizes) {
+      const int64_t bytes = linear_plan(s[0], s[1], s[2], direct != 0, units).work_bytes;
+      most = bytes > most ? bytes : most;
+    }
+  }
+  return most;
+}
+
+}  // extern "C"

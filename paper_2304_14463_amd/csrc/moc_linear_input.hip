@@ -1,0 +1,28 @@
+// The linear layer's gradient with regard to its input, and through the activation before it.
+#include "moc_linear.h"
+
+extern "C" int moc_linear_backward_input(int64_t rows, int64_t cin, int64_t cout, const moc_matrix* dy, const moc_matrix* w, int32_t act,
+                                         const moc_matrix* pre, const moc_matrix* dx, void* work, int64_t work_bytes, void* hip_stream) {
+  if (!sizes_ok(rows, cin) || !sizes_ok(rows, cout) || act < MOC_ACT_NONE || act > MOC_ACT_SILU || (!pre && act != MOC_ACT_NONE)) return MOC_EINVAL;
+  if (!matrix_ok(dy, rows, cout, true, false) || dy->type == MOC_F32 || !matrix_ok(w, cout, cin, true, false) || w->type != dy->type) return MOC_EINVAL;
+  if (!matrix_ok(dx, rows, cin, true, false) || (dx->type != dy->type && dx->type != MOC_F32)) return MOC_EINVAL;
+  if (pre && (!matrix_ok(pre, rows, cin, true, true) || (is_value(pre->type) && pre->type != dy->type && pre->type != MOC_F32))) return MOC_EINVAL;
+  if (rows == 0 || cin == 0) return MOC_OK;
+  LinearArgs g = {};
+  g.a = operand_of(dy);
+  g.b = operand_of(w);
+  g.m = (int)rows;
+  g.n = (int)cin;
+  g.k = (int)cout;
+  Epilogue& e = g.e;
+  e.act = act;
+  if (pre && act != MOC_ACT_NONE) {
+    e.pre = pre->data;
+    e.pre_scales = pre->scales;
+    e.pre_type = pre->type;
+    e.pre_stride = pre->stride;
+    e.pre_scale_stride = pre->scale_stride;
+  }
+  set_out(e, dx);
+  return queue_linear<kRow, kCol, false>(g, dy->type, dy->type, direct_ok(dy, cout) && direct_ok(w, cin), work, work_bytes, hip_stream);
+}

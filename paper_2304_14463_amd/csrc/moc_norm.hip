@@ -1,0 +1,489 @@
+// Layer norm, forward and backward, with the reduction of the parameters' gradients.
+//
+// Bound by memory: every value is read once and written once.  T threads take a row and hold it in
+// registers, CH runs of eight values each, so the variance is that of the differences from the mean
+// and nothing is read again; rows longer than the registers hold are read again from cache.
+// Forward: a wave a row up to 2048 columns (no barrier), then the fewest threads that hold it.
+// Backward: every workgroup goes over many rows and keeps its columns' two sums in registers; they
+// meet in the workspace, one row of sums a workgroup, and a second kernel adds those in their order.
+#include "moc_training.h"
+
+namespace {
+
+constexpr int kMaxThreads = 1024;
+
+struct NormArgs {
+  const void* x;          // tensor or codes
+  const uint8_t* x_scales;
+  int64_t x_stride, x_scale_stride;
+  const void *gamma, *beta;
+  int param_type;
+  float eps;
+  float *mean, *rstd;
+  // forward
+  void* y;
+  int y_type;
+  int64_t y_stride;
+  uint8_t *codes, *scales;
+  int64_t code_stride, scale_stride;
+  int kept_type;          // -1: none
+  float most;
+  // backward
+  const void *dy, *residual;   // residual may be null
+  int dy_type, residual_type;
+  int64_t dy_stride, residual_stride;
+  float* sums;            // [gridDim][2][cols], null: no parameter gradients
+  int64_t rows;
+  int cols;
+};
+
+__device__ __forceinline__ float wave_sum(float a) {
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) a += __shfl_xor(a, s, kWave);
+  return a;
+}
+
+// Sums over the T threads that share a row, in all of them.  `room`: 2 x T / 64 floats of their own.
+// Called by whole workgroups only where T > 64.
+template <int T>
+__device__ __forceinline__ void row_sum2(float& a, float& b, float* room) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  if constexpr (T > kWave) {
+    constexpr int W = T / kWave;
+    const int wave = (threadIdx.x % T) / kWave;
+    __syncthreads();   // the sums before these have been read
+    if (threadIdx.x % kWave == 0) {
+      room[2 * wave] = a;
+      room[2 * wave + 1] = b;
+    }
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      a += room[2 * w];
+      b += room[2 * w + 1];
+    }
+  }
+}
+template <int T>
+__device__ __forceinline__ float row_sum(float a, float* room) {
+  float none = 0.0f;
+  row_sum2<T>(a, none, room);
+  return a;
+}
+
+__device__ __forceinline__ void load_param(const void* p, int type, int col, int n, float other, float (&v)[kRun]) {
+  if (p) {
+    load_any(type, p, col, n, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = other;
+  }
+}
+
+template <int X>
+__device__ __forceinline__ const void* row_of(const void* x, int64_t row, int64_t stride) {
+  return static_cast<const typename Stored<X>::type*>(x) + row * stride;
+}
+__device__ __forceinline__ char* row_any(const void* x, int type, int64_t row, int64_t stride) {
+  return const_cast<char*>(static_cast<const char*>(x)) + row * stride * (type == MOC_F32 ? 4 : 2);
+}
+
+template <int X>
+__device__ __forceinline__ void load_x(const NormArgs& g, int64_t row, int col, int n, float (&v)[kRun]) {
+  load_held<X>(row_of<X>(g.x, row, g.x_stride), g.x_scales + row * g.x_scale_stride, col, n, v);
+}
+
+// ---- forward ------------------------------------------------------------------------------------
+
+// y and its checkpoint of one run.
+__device__ __forceinline__ void finish_run(const NormArgs& g, int64_t row, int col, int n, float mean, float rstd, float (&v)[kRun]) {
+  float ga[kRun], be[kRun];
+  load_param(g.gamma, g.param_type, col, n, 1.0f, ga);
+  load_param(g.beta, g.param_type, col, n, 0.0f, be);
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) v[i] = i < n ? (v[i] - mean) * rstd * ga[i] + be[i] : 0.0f;
+  if (n > 0) store_any(g.y_type, row_any(g.y, g.y_type, row, g.y_stride), col, n, v);
+  if (g.kept_type >= 0) keep_any(g.kept_type, v, col, n, g.most, g.codes + row * g.code_stride, g.scales + row * g.scale_stride);
+}
+
+template <int X, int T, int CH>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormArgs g) {
+  constexpr int kRows = T < 256 ? 256 / T : 1;   // rows of a workgroup
+  static_assert(T <= kWave || kRows == 1);
+  __shared__ float room[2 * T / kWave + 1];
+  const int lane = threadIdx.x % T;
+  const int64_t row = block_of() * kRows + threadIdx.x / T;
+  if (row >= g.rows) return;   // whole waves only, and whole workgroups where they share a row
+  float v[CH][kRun];
+  float s = 0.0f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = (c * T + lane) * kRun;
+    load_x<X>(g, row, min(col, g.cols - 1), g.cols - col, v[c]);
+  }
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) s += v[c][i];
+  const float count = (float)g.cols;
+  const float mean = row_sum<T>(s, room) / count;
+  float q = 0.0f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int n = g.cols - (c * T + lane) * kRun;
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      const float d = v[c][i] - mean;
+      q += i < n ? d * d : 0.0f;
+    }
+  }
+  const float rstd = 1.0f / __builtin_sqrtf(row_sum<T>(q, room) / count + g.eps);
+  if (lane == 0) {
+    g.mean[row] = mean;
+    g.rstd[row] = rstd;
+  }
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = (c * T + lane) * kRun;
+    finish_run(g, row, col, g.cols - col, mean, rstd, v[c]);
+  }
+}
+
+// Rows that do not fit the registers of a workgroup: read three times.
+template <int X>
+__global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormArgs g) {
+  constexpr int T = kMaxThreads;
+  __shared__ float room[2 * T / kWave];
+  const int64_t row = block_of();
+  if (row >= g.rows) return;
+  const int blocks = (g.cols + MOC_BLOCK - 1) / MOC_BLOCK * MOC_BLOCK;   // quads stay together
+  float v[kRun], s = 0.0f;
+  for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
+    load_x<X>(g, row, col, g.cols - col, v);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) s += v[i];
+  }
+  const float count = (float)g.cols;
+  const float mean = row_sum<T>(s, room) / count;
+  float q = 0.0f;
+  for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
+    load_x<X>(g, row, col, g.cols - col, v);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) q += i < g.cols - col ? (v[i] - mean) * (v[i] - mean) : 0.0f;
+  }
+  const float rstd = 1.0f / __builtin_sqrtf(row_sum<T>(q, room) / count + g.eps);
+  if (threadIdx.x == 0) {
+    g.mean[row] = mean;
+    g.rstd[row] = rstd;
+  }
+  for (int col = threadIdx.x * kRun; col < blocks; col += T * kRun) {
+    load_x<X>(g, row, min(col, g.cols - 1), g.cols - col, v);
+    finish_run(g, row, col, g.cols - col, mean, rstd, v);
+  }
+}
+
+// ---- backward -----------------------------------------------------------------------------------
+
+// h and p = dy * gamma of a run, 0 beyond the row; dy stays in d.
+template <int X>
+__device__ __forceinline__ void load_grad(const NormArgs& g, int64_t row, int col, float mean, float rstd, float (&h)[kRun], float (&d)[kRun]) {
+  const int n = g.cols - col;
+  load_any(g.dy_type, row_any(g.dy, g.dy_type, row, g.dy_stride), min(col, g.cols - 1), n, d);
+  load_x<X>(g, row, min(col, g.cols - 1), n, h);
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) h[i] = i < n ? (h[i] - mean) * rstd : 0.0f;
+}
+
+__device__ __forceinline__ void store_dx(const NormArgs& g, int64_t row, int col, float rstd, float a, float b, const float (&h)[kRun], const float (&d)[kRun],
+                                         const float (&ga)[kRun]) {
+  const int n = g.cols - col;
+  if (n <= 0) return;
+  float o[kRun];
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) o[i] = rstd * (d[i] * ga[i] - a - h[i] * b);
+  if (g.residual) {
+    float r[kRun];
+    load_any(g.residual_type, row_any(g.residual, g.residual_type, row, g.residual_stride), col, n, r);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) o[i] += r[i];
+  }
+  store_any(g.y_type, row_any(g.y, g.y_type, row, g.y_stride), col, n, o);
+}
+
+// The sums of a workgroup's rows groups (kRows of T lanes), added in their order, into its row of the
+// workspace.
+template <int T, int kRows, int CH>
+__device__ __forceinline__ void store_sums(const NormArgs& g, const float (&sg)[CH][kRun], const float (&sb)[CH][kRun], float* stage) {
+  const int lane = threadIdx.x % T, mine = threadIdx.x / T;
+  float* const out = g.sums + (int64_t)blockIdx.x * 2 * g.cols;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    float a[kRun], b[kRun];
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      a[i] = sg[c][i];
+      b[i] = sb[c][i];
+    }
+    if constexpr (kRows > 1) {   // stage: [kRows][16][T]
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        stage[(mine * 16 + i) * T + lane] = a[i];
+        stage[(mine * 16 + 8 + i) * T + lane] = b[i];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) a[i] = b[i] = 0.0f;
+      if (mine == 0) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+          for (int i = 0; i < kRun; ++i) {
+            a[i] += stage[(r * 16 + i) * T + lane];
+            b[i] += stage[(r * 16 + 8 + i) * T + lane];
+          }
+      }
+    }
+    const int col = (c * T + lane) * kRun, n = g.cols - col;
+    if (mine == 0 && n > 0) {
+      store_run<MOC_F32>(out, col, n, a);
+      store_run<MOC_F32>(out + g.cols, col, n, b);
+    }
+  }
+}
+
+template <int X, int T, int CH>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_backward_kernel(NormArgs g) {
+  constexpr int kRows = T < 256 ? 256 / T : 1;
+  static_assert(T <= kWave || kRows == 1);
+  __shared__ float room[2 * T / kWave + 1];
+  __shared__ float stage[kRows > 1 ? kRows * 16 * T : 1];
+  const int lane = threadIdx.x % T;
+  float ga[CH][kRun], sg[CH][kRun], sb[CH][kRun];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = (c * T + lane) * kRun;
+    load_param(g.gamma, g.param_type, min(col, g.cols - 1), g.cols - col, 1.0f, ga[c]);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) sg[c][i] = sb[c][i] = 0.0f;
+  }
+  const float count = (float)g.cols;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / T; row < g.rows; row += (int64_t)gridDim.x * kRows) {
+    const float mean = g.mean[row], rstd = g.rstd[row];
+    float h[CH][kRun], d[CH][kRun], a = 0.0f, b = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) load_grad<X>(g, row, (c * T + lane) * kRun, mean, rstd, h[c], d[c]);
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        const float p = d[c][i] * ga[c][i];
+        a += p;
+        b += p * h[c][i];
+        sg[c][i] += d[c][i] * h[c][i];
+        sb[c][i] += d[c][i];
+      }
+    row_sum2<T>(a, b, room);
+    a /= count;
+    b /= count;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) store_dx(g, row, (c * T + lane) * kRun, rstd, a, b, h[c], d[c], ga[c]);
+  }
+  if (g.sums) store_sums<T, kRows, CH>(g, sg, sb, stage);
+}
+
+// Rows that do not fit the registers: two passes a row; the sums go to the workspace as they grow
+// (a workgroup's own row of it, zeroed first).
+template <int X>
+__global__ __launch_bounds__(kMaxThreads) void norm_backward_long_kernel(NormArgs g) {
+  constexpr int T = kMaxThreads;
+  __shared__ float room[2 * T / kWave];
+  float* const sums = g.sums ? g.sums + (int64_t)blockIdx.x * 2 * g.cols : nullptr;
+  const float count = (float)g.cols;
+  if (sums) {
+    const float zero[kRun] = {};
+    for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
+      store_run<MOC_F32>(sums, col, g.cols - col, zero);
+      store_run<MOC_F32>(sums + g.cols, col, g.cols - col, zero);
+    }
+  }
+  for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
+    const float mean = g.mean[row], rstd = g.rstd[row];
+    float h[kRun], d[kRun], ga[kRun], a = 0.0f, b = 0.0f;
+    for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
+      const int n = g.cols - col;
+      load_grad<X>(g, row, col, mean, rstd, h, d);
+      load_param(g.gamma, g.param_type, col, n, 1.0f, ga);
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) {
+        a += d[i] * ga[i];
+        b += d[i] * ga[i] * h[i];
+      }
+      if (sums) {   // the same thread's columns in every row
+        float s[kRun], t[kRun];
+        load_run<MOC_F32>(sums, col, n, s);
+        load_run<MOC_F32>(sums + g.cols, col, n, t);
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+          s[i] += d[i] * h[i];
+          t[i] += d[i];
+        }
+        store_run<MOC_F32>(sums, col, n, s);
+        store_run<MOC_F32>(sums + g.cols, col, n, t);
+      }
+    }
+    row_sum2<T>(a, b, room);
+    a /= count;
+    b /= count;
+    for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
+      load_grad<X>(g, row, col, mean, rstd, h, d);
+      load_param(g.gamma, g.param_type, col, g.cols - col, 1.0f, ga);
+      store_dx(g, row, col, rstd, a, b, h, d, ga);
+    }
+  }
+}
+
+// out[col] = sum over `parts` rows of 2 * cols sums; 64 columns a workgroup, 16 rows at a time.
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float* sums, int parts, int cols, float* dgamma, float* dbeta) {
+  __shared__ float stage[16][64];
+  const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), width = 2 * (int64_t)cols;
+  const int mine = threadIdx.x >> 6;
+  float s = 0.0f;
+  if (col < width)
+    for (int p = mine; p < parts; p += 16) s += sums[p * width + col];
+  stage[mine][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (mine == 0 && col < width) {
+    s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += stage[i][threadIdx.x];
+    (col < cols ? dgamma[col] : dbeta[col - cols]) = s;
+  }
+}
+
+// ---- dispatch -----------------------------------------------------------------------------------
+
+using NormKernel = void (*)(NormArgs);
+struct Shape {
+  NormKernel kern;
+  int threads, rows;   // of a workgroup
+};
+
+template <int X>
+Shape forward_shape(int64_t cols) {
+  if (cols <= 512) return {norm_forward_kernel<X, 64, 1>, 256, 4};
+  if (cols <= 1024) return {norm_forward_kernel<X, 64, 2>, 256, 4};
+  if (cols <= 2048) return {norm_forward_kernel<X, 64, 4>, 256, 4};
+  if (cols <= 4096) return {norm_forward_kernel<X, 256, 2>, 256, 1};
+  if (cols <= 8192) return {norm_forward_kernel<X, 256, 4>, 256, 1};
+  if (cols <= 16384) return {norm_forward_kernel<X, 512, 4>, 512, 1};
+  if (cols <= 32768) return {norm_forward_kernel<X, 1024, 4>, 1024, 1};
+  return {norm_forward_long_kernel<X>, kMaxThreads, 1};
+}
+template <int X>
+Shape backward_shape(int64_t cols) {
+  if (cols <= 512) return {norm_backward_kernel<X, 64, 1>, 256, 4};
+  if (cols <= 1024) return {norm_backward_kernel<X, 64, 2>, 256, 4};
+  if (cols <= 2048) return {norm_backward_kernel<X, 256, 1>, 256, 1};
+  if (cols <= 4096) return {norm_backward_kernel<X, 256, 2>, 256, 1};
+  if (cols <= 8192) return {norm_backward_kernel<X, 512, 2>, 512, 1};
+  if (cols <= 16384) return {norm_backward_kernel<X, 1024, 2>, 1024, 1};
+  return {norm_backward_long_kernel<X>, kMaxThreads, 1};
+}
+Shape shape_of(bool forward, int type, int64_t cols) {
+  switch (type) {
+    case MOC_F32: return forward ? forward_shape<MOC_F32>(cols) : backward_shape<MOC_F32>(cols);
+    case MOC_F16: return forward ? forward_shape<MOC_F16>(cols) : backward_shape<MOC_F16>(cols);
+    case MOC_BF16: return forward ? forward_shape<MOC_BF16>(cols) : backward_shape<MOC_BF16>(cols);
+    case MOC_E4M3: return forward ? forward_shape<MOC_E4M3>(cols) : backward_shape<MOC_E4M3>(cols);
+    default: return forward ? forward_shape<MOC_I8>(cols) : backward_shape<MOC_I8>(cols);
+  }
+}
+
+// Workgroups of the backward pass: as many rows of sums as the card needs to be full of work, no more
+// (each is written and read again).
+int64_t backward_groups(int64_t rows, int64_t cols, int units) {
+  const Shape s = shape_of(false, MOC_BF16, cols);   // rows and threads do not depend on the type
+  const int64_t wanted = (int64_t)units * (2048 / s.threads > 4 ? 4 : 2048 / s.threads), there = (rows + s.rows - 1) / s.rows;
+  return there < wanted ? there : wanted;
+}
+
+}  // namespace
+
+extern "C" {
+
+int moc_norm_forward(int64_t rows, int64_t cols, const moc_matrix* x, const void* gamma, const void* beta, int32_t param_type, float eps,
+                     const moc_matrix* y, const moc_matrix* kept, float* mean, float* rstd, void* hip_stream) {
+  if (!sizes_ok(rows, cols) || cols < 1 || !(eps >= 0.0f)) return MOC_EINVAL;
+  if (!matrix_ok(x, rows, cols, true, true) || !matrix_ok(y, rows, cols, true, false) || (kept && !matrix_ok(kept, rows, cols, false, true))) return MOC_EINVAL;
+  if (!params_ok(gamma, param_type) || !params_ok(beta, param_type)) return MOC_EINVAL;
+  if (rows == 0) return MOC_OK;
+  if (!mean || !rstd || !aligned_to(mean, 4) || !aligned_to(rstd, 4)) return MOC_EINVAL;
+  NormArgs g = {};
+  g.x = x->data; g.x_scales = x->scales; g.x_stride = x->stride; g.x_scale_stride = x->scale_stride;
+  g.gamma = gamma; g.beta = beta; g.param_type = param_type; g.eps = eps;
+  g.mean = mean; g.rstd = rstd;
+  g.y = y->data; g.y_type = y->type; g.y_stride = y->stride;
+  g.kept_type = -1;
+  if (kept) {
+    g.codes = static_cast<uint8_t*>(kept->data); g.scales = kept->scales;
+    g.code_stride = kept->stride; g.scale_stride = kept->scale_stride;
+    g.kept_type = kept->type;
+    g.most = most_kept(kept->type, y->type);
+  }
+  g.rows = rows; g.cols = (int)cols;
+  const Shape s = shape_of(true, x->type, cols);
+  hipLaunchKernelGGL(s.kern, grid_of((rows + s.rows - 1) / s.rows), dim3(s.threads), 0, static_cast<hipStream_t>(hip_stream), g);
+  MOC_HIP(hipGetLastError());
+  return MOC_OK;
+}
+
+int64_t moc_norm_backward_work(int64_t rows, int64_t cols) {
+  if (!sizes_ok(rows, cols) || cols < 1) return MOC_EINVAL;
+  int units = 0;
+  const int rc = moc_compute_units(&units);
+  if (rc != MOC_OK) return rc;
+  return backward_groups(rows, cols, units) * 2 * cols * (int64_t)sizeof(float);
+}
+
+int moc_norm_backward(int64_t rows, int64_t cols, const moc_matrix* dy, const moc_matrix* x, const void* gamma, int32_t param_type,
+                      const float* mean, const float* rstd, const moc_matrix* residual, const moc_matrix* dx, float* dgamma, float* dbeta,
+                      void* work, int64_t work_bytes, void* hip_stream) {
+  if (!sizes_ok(rows, cols) || cols < 1) return MOC_EINVAL;
+  if (!matrix_ok(dy, rows, cols, true, false) || !matrix_ok(x, rows, cols, true, true) || !matrix_ok(dx, rows, cols, true, false)) return MOC_EINVAL;
+  if ((residual && !matrix_ok(residual, rows, cols, true, false)) || !params_ok(gamma, param_type)) return MOC_EINVAL;
+  if ((dgamma == nullptr) != (dbeta == nullptr) || !aligned_to(dgamma, 4) || !aligned_to(dbeta, 4)) return MOC_EINVAL;
+  if (rows > 0 && (!mean || !rstd || !aligned_to(mean, 4) || !aligned_to(rstd, 4))) return MOC_EINVAL;
+  if (rows == 0 && !dgamma) return MOC_OK;
+  int units = 0;
+  const int rc = moc_compute_units(&units);
+  if (rc != MOC_OK) return rc;
+  const int64_t groups = backward_groups(rows, cols, units);
+  if (dgamma && groups > 0 && (!work || !aligned_to(work, 16) || work_bytes < groups * 2 * cols * (int64_t)sizeof(float))) return MOC_EINVAL;
+  const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  if (rows > 0) {
+    NormArgs g = {};
+    g.x = x->data; g.x_scales = x->scales; g.x_stride = x->stride; g.x_scale_stride = x->scale_stride;
+    g.gamma = gamma; g.param_type = param_type;
+    g.mean = const_cast<float*>(mean); g.rstd = const_cast<float*>(rstd);
+    g.y = dx->data; g.y_type = dx->type; g.y_stride = dx->stride;
+    g.dy = dy->data; g.dy_type = dy->type; g.dy_stride = dy->stride;
+    if (residual) {
+      g.residual = residual->data; g.residual_type = residual->type; g.residual_stride = residual->stride;
+    }
+    g.sums = dgamma ? static_cast<float*>(work) : nullptr;
+    g.rows = rows; g.cols = (int)cols;
+    const Shape s = shape_of(false, x->type, cols);
+    hipLaunchKernelGGL(s.kern, dim3((unsigned)groups), dim3(s.threads), 0, stream, g);
+    MOC_HIP(hipGetLastError());
+  }
+  if (dgamma) {
+    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((2 * cols + 63) / 64)), dim3(1024), 0, stream, static_cast<const float*>(work), (int)groups, (int)cols, dgamma, dbeta);
+    MOC_HIP(hipGetLastError());
+  }
+  return MOC_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,282 @@
+// Shared by the kernels of include/moccasin_training.h: runs of eight values loaded, stored and
+// converted, activations, blocks of a checkpoint, and the checks of descriptors.
+#pragma once
+
+#include "moc_internal.h"
+#include "moccasin_training.h"
+
+namespace {
+
+using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
+using f16x2 = _Float16 __attribute__((ext_vector_type(2)));
+using f32x2 = float __attribute__((ext_vector_type(2)));
+
+constexpr float kInf = __builtin_inff();
+constexpr int kMinExp = -111;   // smallest exponent of a scale
+
+// What a thread takes at a time: eight values next to each other in a row, from a column that is a
+// multiple of eight.  16-bit types: 16 bytes, the widest load; four neighbouring lanes hold the 32
+// columns that share a scale.  `n` of them exist (all eight where n >= 8).  Addresses are aligned to
+// the element only: gfx950 takes vector loads at any address, and memcpy says so to the compiler.
+constexpr int kRun = 8;
+
+__device__ __forceinline__ float bits_float(uint32_t b) { return __builtin_bit_cast(float, b); }
+__device__ __forceinline__ uint32_t float_bits(float f) { return __builtin_bit_cast(uint32_t, f); }
+
+template <int TYPE> struct Stored;
+template <> struct Stored<MOC_F32> { using type = float; };
+template <> struct Stored<MOC_F16> { using type = _Float16; };
+template <> struct Stored<MOC_BF16> { using type = __bf16; };
+template <> struct Stored<MOC_E4M3> { using type = uint8_t; };
+template <> struct Stored<MOC_I8> { using type = uint8_t; };
+
+template <int TYPE>
+__device__ __forceinline__ void load_run(const void* row, int64_t col, int n, float (&v)[kRun]) {
+  using T = typename Stored<TYPE>::type;
+  const T* p = static_cast<const T*>(row) + col;
+  T t[kRun];
+  if (n >= kRun) {
+    __builtin_memcpy(t, p, sizeof t);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) t[i] = i < n ? p[i] : T(0.0f);
+  }
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) v[i] = (float)t[i];
+}
+
+template <int TYPE>
+__device__ __forceinline__ void store_run(void* row, int64_t col, int n, const float (&v)[kRun]) {
+  using T = typename Stored<TYPE>::type;
+  T* p = static_cast<T*>(row) + col;
+  T t[kRun];
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) t[i] = (T)v[i];
+  if (n >= kRun) {
+    __builtin_memcpy(p, t, sizeof t);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i)
+      if (i < n) p[i] = t[i];
+  }
+}
+
+// The same with the type known at run time only (uniform over the wave).
+__device__ __forceinline__ void load_any(int type, const void* row, int64_t col, int n, float (&v)[kRun]) {
+  if (type == MOC_BF16) load_run<MOC_BF16>(row, col, n, v);
+  else if (type == MOC_F16) load_run<MOC_F16>(row, col, n, v);
+  else load_run<MOC_F32>(row, col, n, v);
+}
+__device__ __forceinline__ void store_any(int type, void* row, int64_t col, int n, const float (&v)[kRun]) {
+  if (type == MOC_BF16) store_run<MOC_BF16>(row, col, n, v);
+  else if (type == MOC_F16) store_run<MOC_F16>(row, col, n, v);
+  else store_run<MOC_F32>(row, col, n, v);
+}
+
+// ---- checkpoints --------------------------------------------------------------------------------
+
+__device__ __forceinline__ float scale_of(uint8_t byte) { return bits_float((uint32_t)byte << 23); }
+
+// Eight codes, as two words, to the values they stand for.
+template <int FMT>
+__device__ __forceinline__ void decode_run(uint2 c, float scale, float (&v)[kRun]) {
+  const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if constexpr (FMT == MOC_E4M3) {
+      const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], true);
+      v[4 * h] = lo[0] * scale;
+      v[4 * h + 1] = lo[1] * scale;
+      v[4 * h + 2] = hi[0] * scale;
+      v[4 * h + 3] = hi[1] * scale;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int code = (int)(w[h] << (24 - 8 * i)) >> 24;
+        v[4 * h + i] = code == -128 ? bits_float(0x7FC00000u) : (float)code * scale;
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ uint2 load_codes(const uint8_t* p, int n) {
+  uint2 c = {0, 0};
+  if (n >= kRun) {
+    __builtin_memcpy(&c, p, 8);
+  } else {
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kRun - 1; ++i)
+      if (i < n) w[i >> 2] |= (uint32_t)p[i] << (8 * (i & 3));
+    c = {w[0], w[1]};
+  }
+  return c;
+}
+
+__device__ __forceinline__ void store_codes(uint8_t* p, int n, uint2 c) {
+  if (n >= kRun) {
+    __builtin_memcpy(p, &c, 8);
+  } else {
+    const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+    for (int i = 0; i < kRun - 1; ++i)
+      if (i < n) p[i] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+  }
+}
+
+// A row of a matrix that is a tensor or a checkpoint.
+template <int TYPE>
+__device__ __forceinline__ void load_held(const void* row, const uint8_t* scales, int64_t col, int n, float (&v)[kRun]) {
+  if constexpr (TYPE == MOC_E4M3 || TYPE == MOC_I8) {
+    decode_run<TYPE>(load_codes(static_cast<const uint8_t*>(row) + col, n), scale_of(scales[col / MOC_BLOCK]), v);
+  } else {
+    load_run<TYPE>(row, col, n, v);
+  }
+}
+
+// Magnitudes above this are taken for it (what a code stands for stays finite in the values' type).
+inline float most_kept(int fmt, int type) {
+  const float top = type == MOC_F16 ? 32768.0f : 1.7014118346046923e38f;   // 2^15, 2^127
+  return (fmt == MOC_E4M3 ? 1.875f : 1.96875f) * top;
+}
+
+// The largest finite magnitude of a run, `most` at most.
+__device__ __forceinline__ float run_peak(const float (&v)[kRun], float most) {
+  float a = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) {
+    const float m = __builtin_fabsf(v[i]);
+    a = m < kInf && m > a ? m : a;   // a NaN compares false
+  }
+  return fminf(a, most);
+}
+
+// The exponent of a block's scale from its peak: the peak's own exponent less the format's, one more
+// where its fraction is above that of the format's largest value.
+template <int FMT>
+__device__ __forceinline__ int scale_exp(float peak) {
+  const uint32_t b = float_bits(peak);
+  const int k = (int)(b >> 23) - 127 - (FMT == MOC_E4M3 ? 8 : 6) + ((b & 0x7FFFFFu) > (FMT == MOC_E4M3 ? 0x600000u : 0x7E0000u) ? 1 : 0);
+  return max(k, kMinExp);
+}
+
+template <int FMT>
+__device__ __forceinline__ uint2 encode_run(const float (&v)[kRun], int k, float most) {
+  const float inv = bits_float((uint32_t)(127 - k) << 23);
+  uint32_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float q[4];
+    bool good[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = v[4 * h + i];
+      good[i] = __builtin_fabsf(x) < kInf;
+      q[i] = fminf(fmaxf(x, -most), most) * inv;
+    }
+    if constexpr (FMT == MOC_E4M3) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = good[i] ? q[i] : kInf;   // has no code of its own: 0x7F (a NaN would be 0xFF)
+      int r = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+      w[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], r, true);
+    } else {
+      w[h] = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int code = good[i] ? (int)__builtin_rintf(q[i]) : -128;
+        w[h] |= ((uint32_t)code & 0xFFu) << (8 * i);
+      }
+    }
+  }
+  return uint2{w[0], w[1]};
+}
+
+// The maximum over the quad of lanes that holds a block's 32 columns.
+__device__ __forceinline__ float quad_max(float a) {
+  a = fmaxf(a, bits_float((uint32_t)__builtin_amdgcn_mov_dpp((int)float_bits(a), 0xB1, 0xF, 0xF, true)));   // quad_perm 1 0 3 2
+  return fmaxf(a, bits_float((uint32_t)__builtin_amdgcn_mov_dpp((int)float_bits(a), 0x4E, 0xF, 0xF, true)));   // quad_perm 2 3 0 1
+}
+
+// A run of a row into a checkpoint; all four lanes of the quad come here together, those beyond the
+// row with n <= 0 and values of 0.
+template <int FMT>
+__device__ __forceinline__ void keep_run(const float (&v)[kRun], int64_t col, int n, float most, uint8_t* codes, uint8_t* scales) {
+  const int k = scale_exp<FMT>(quad_max(run_peak(v, most)));
+  if (n > 0) {
+    store_codes(codes + col, n, encode_run<FMT>(v, k, most));
+    if ((col & (MOC_BLOCK - 1)) == 0) scales[col / MOC_BLOCK] = (uint8_t)(k + 127);
+  }
+}
+__device__ __forceinline__ void keep_any(int fmt, const float (&v)[kRun], int64_t col, int n, float most, uint8_t* codes, uint8_t* scales) {
+  if (fmt == MOC_E4M3) keep_run<MOC_E4M3>(v, col, n, most, codes, scales);
+  else keep_run<MOC_I8>(v, col, n, most, codes, scales);
+}
+
+// ---- activations --------------------------------------------------------------------------------
+
+// exp2 and the reciprocal are the hardware's (1 ulp each): what is left of that after the rounding to
+// the output's type is below 2^-20 of a value.
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f)); }
+
+constexpr float kGelu1 = 1.5957691216057308f;            // 2 sqrt(2 / pi)
+constexpr float kGelu3 = 1.5957691216057308f * 0.044715f;
+
+__device__ __forceinline__ float act_of(int act, float u) {
+  if (act == MOC_ACT_RELU) return u <= 0.0f ? 0.0f : u;
+  if (act == MOC_ACT_GELU) return u * sigmoid(u * (kGelu1 + kGelu3 * u * u));
+  if (act == MOC_ACT_SILU) return u * sigmoid(u);
+  return u;
+}
+
+// d times the activation's derivative at u.
+__device__ __forceinline__ float times_slope(int act, float d, float u) {
+  if (act == MOC_ACT_RELU) return u <= 0.0f ? 0.0f : u > 0.0f ? d : bits_float(0x7FC00000u);
+  if (act == MOC_ACT_GELU) {
+    // beyond +-16 the derivative is 0 or 1 in 32 bits; the squares of larger arguments would overflow
+    const float c = u < -16.0f ? -16.0f : u > 16.0f ? 16.0f : u;   // keeps a NaN
+    const float s = sigmoid(c * (kGelu1 + kGelu3 * c * c));
+    return d * (s + c * s * (1.0f - s) * (kGelu1 + 3.0f * kGelu3 * c * c));
+  }
+  if (act == MOC_ACT_SILU) {
+    const float s = sigmoid(u);
+    return d * (s * (1.0f + u * (1.0f - s)));
+  }
+  return d;
+}
+
+// ---- grids --------------------------------------------------------------------------------------
+
+// A launch has fewer than 2^32 threads along x: more workgroups than that go on along y.
+inline dim3 grid_of(int64_t blocks) {
+  const int64_t x = blocks < (1 << 21) ? blocks : 1 << 21;
+  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+}
+__device__ __forceinline__ int64_t block_of() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
+// ---- descriptors --------------------------------------------------------------------------------
+
+inline bool is_kept(int type) { return type == MOC_E4M3 || type == MOC_I8; }
+inline bool is_value(int type) { return type == MOC_F32 || type == MOC_F16 || type == MOC_BF16; }
+inline int type_bytes(int type) { return type == MOC_F32 ? 4 : is_kept(type) ? 1 : 2; }
+
+inline bool sizes_ok(int64_t rows, int64_t cols) { return rows >= 0 && rows <= MOC_MAX_ROWS && cols >= 0 && cols <= MOC_MAX_COLS; }
+
+// A tensor (values only) or a checkpoint (kept only) of rows x cols, with memory unless it is empty.
+inline bool matrix_ok(const moc_matrix* x, int64_t rows, int64_t cols, bool values, bool kept) {
+  if (!x || x->reserved != 0) return false;
+  const bool ckpt = is_kept(x->type);
+  if (!(ckpt ? kept : values && is_value(x->type))) return false;
+  if (x->stride < cols || x->stride > MOC_MAX_STRIDE) return false;
+  if (ckpt && (x->scale_stride < (cols + MOC_BLOCK - 1) / MOC_BLOCK || x->scale_stride > MOC_MAX_STRIDE)) return false;
+  if (rows == 0 || cols == 0) return true;
+  if (!x->data || (ckpt && !x->scales)) return false;
+  return reinterpret_cast<uintptr_t>(x->data) % type_bytes(x->type) == 0;
+}
+
+inline bool aligned_to(const void* p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+inline bool params_ok(const void* p, int type) { return !p || (is_value(type) && aligned_to(p, type_bytes(type))); }
+
+}  // namespace
+
+// Compute units of the current device (asked for once each), or an error code.
+int moc_compute_units(int* out);
