@@ -146,6 +146,7 @@ struct Tile {
 template <int LAY, int WIDTH, int THREADS>
 struct DirectLoader {
   using T = Tile<LAY, WIDTH, THREADS>;
+  static constexpr int kLoads = T::kEach;
   const char* base;       // of the window: the tile's first row and k
   int64_t left;           // bytes from there to the operand's end
   int64_t step;           // bytes the base moves by
@@ -195,6 +196,7 @@ template <int LAY, int WIDTH, int THREADS, int TYPE, int HELD>
 struct RegisterLoader {
   using T = Tile<LAY, WIDTH, THREADS>;
   using V = typename Stored<TYPE>::type;
+  static constexpr int kLoads = 0;   // left to the scheduler
   static constexpr bool kKept = HELD == MOC_E4M3 || HELD == MOC_I8;
   Operand x;
   int first, extent, k, end;
@@ -290,9 +292,23 @@ struct Reader {
 
 // ---- the kernel ---------------------------------------------------------------------------------
 
+// Has the scheduler put a read from LDS behind each product, as long as there are any, and then the
+// loads into it, evenly.
+template <int MFMA, int READS, int LOADS, int I = 0>
+__device__ __forceinline__ void interleave() {
+  if constexpr (I < MFMA) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    constexpr int kAt = (READS + MFMA - 1) / MFMA, kReads = READS < kAt ? READS : kAt;
+    constexpr int kLoads = (LOADS + MFMA - I - 1) / (MFMA - I);
+    if constexpr (kReads > 0) __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
+    if constexpr (kLoads > 0) __builtin_amdgcn_sched_group_barrier(0x020, kLoads, 0);
+    interleave<MFMA, READS - kReads, LOADS - kLoads, I + 1>();
+  }
+}
+
 // TYPE of the operands; HELD: of b, TYPE or a checkpoint's.
 template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int LOAD, int HELD>
-__global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) {
+__global__ __launch_bounds__(WM* WN* kWave, BM == 256 ? 1 : 2) void linear_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;   // 32 x 32 outputs of a wave
   __shared__ __attribute__((aligned(1024))) uint8_t a0[BM * kRowBytes], a1[BM * kRowBytes], b0[BN * kRowBytes], b1[BN * kRowBytes];
@@ -323,29 +339,19 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
 
-  // What is read for 16 of k while the 16 before are multiplied; the scheduler stays between the
-  // barriers, or it would read all of a step first and spill.
-  const auto multiply = [&](const Lds* a, const Lds* b) {
-    s16x8 fa[2][TM], fb[2][TN];
-    const auto fetch = [&](int s) {
+  s16x8 fa[2][TM], fb[2][TN];
+  const auto fetch = [&](const Lds* a, const Lds* b, int s) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) fb[s & 1][j] = rb.read(b, j, s);
+    for (int j = 0; j < TN; ++j) fb[s & 1][j] = rb.read(b, j, s);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) fa[s & 1][i] = ra.read(a, i, s);
-    };
-    fetch(0);
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      if (s < 3) fetch(s + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < TM; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mfma<TYPE>(fb[s & 1][j], fa[s & 1][i], acc[i][j]);   // rows of the result: n
-      __builtin_amdgcn_sched_barrier(0);
-    }
+    for (int i = 0; i < TM; ++i) fa[s & 1][i] = ra.read(a, i, s);
   };
-  Lds *const pa0 = (Lds*)a0, *const pa1 = (Lds*)a1, *const pb0 = (Lds*)b0, *const pb1 = (Lds*)b1;
+  const auto multiply = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma<TYPE>(fb[s & 1][j], fa[s & 1][i], acc[i][j]);   // rows of the result: n
+  };
   const auto load = [&](Lds* a, Lds* b) {
     la.load(a);
     lb.load(b);
@@ -355,32 +361,51 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
     lb.put(b);
   };
   const auto arrived = [] {
-    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): this wave's loads into LDS
+    __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0): this wave's loads into LDS, its reads and writes
     __syncthreads();
+  };
+  constexpr int kReads = TM * (ALAY == kRow ? 1 : 2) + TN * (BLAY == kRow ? 1 : 2);
+  // A step on what lies in (a, b), with the next step's operands on their way to (c, d): every 16 of k
+  // are read while the 16 before are multiplied.  The last multiplication comes after the barrier, to
+  // cover the first reads of the next step; (a, b), all read, take the step after that.  What lies
+  // beyond the last step is not read from memory (its window is empty) and not used.
+  const auto step = [&](Lds* a, Lds* b, Lds* c, Lds* d) {
+#pragma unroll
+    for (int s = 0; s < 3; ++s) {
+      fetch(a, b, s + 1);
+      multiply(s);
+      interleave<TM * TN, kReads, 0>();
+      if (s < 2) __builtin_amdgcn_sched_barrier(0);
+    }
+    put(c, d);
+    arrived();
+    fetch(c, d, 0);
+    load(a, b);
+    multiply(3);
+    interleave<TM * TN, kReads, LoadA::kLoads + LoadB::kLoads>();
+    __builtin_amdgcn_sched_barrier(0);
   };
   // Steps in pairs, so that each buffer has its own code (and the compiler sees that the loads do not
   // touch what is read); an odd one comes first.
-  int steps = end > begin ? (end - begin + kStepK - 1) / kStepK : 0;
+  Lds *const pa0 = (Lds*)a0, *const pa1 = (Lds*)a1, *const pb0 = (Lds*)b0, *const pb1 = (Lds*)b1;
+  const int steps = end > begin ? (end - begin + kStepK - 1) / kStepK : 0;
   if (steps & 1) {
     load(pa1, pb1);
     put(pa1, pb1);
     arrived();
-    if (steps > 1) load(pa0, pb0);
-    multiply(pa1, pb1);
-    if (steps > 1) put(pa0, pb0);
+    fetch(pa1, pb1, 0);
+    load(pa0, pb0);
+    step(pa1, pb1, pa0, pb0);
   } else if (steps > 0) {
     load(pa0, pb0);
     put(pa0, pb0);
-  }
-  for (steps /= 2; steps > 0; --steps) {
     arrived();
+    fetch(pa0, pb0, 0);
     load(pa1, pb1);
-    multiply(pa0, pb0);
-    put(pa1, pb1);
-    arrived();
-    if (steps > 1) load(pa0, pb0);
-    multiply(pa1, pb1);
-    if (steps > 1) put(pa0, pb0);
+  }
+  for (int pair = steps / 2; pair > 0; --pair) {
+    step(pa0, pb0, pa1, pb1);
+    step(pa1, pb1, pa0, pb0);
   }
 
   // Out by way of LDS, so that lanes next to each other have runs next to each other and a quad has a
@@ -390,7 +415,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
   constexpr int TH = TM < 2 ? TM : 2, kCols = TN * 32, kChunks = kCols / 4, kMove = kChunks < 16 ? kChunks - 1 : 15;
   constexpr int kStage = TH * 32 * kCols * 4, kPer = (int)sizeof b0 / kStage;   // waves that one of the arrays has room for
   static_assert(sizeof a0 <= sizeof b0 && kPer >= 1 && (kPer >= WM * WN || (sizeof a0 == sizeof b0 && 4 * kPer >= WM * WN)));
-  __syncthreads();   // the last step's reads
+  arrived();   // the last reads; and the loads of nothing that write zeros
   const int array = wave / kPer;
   Lds* const stage = (array == 0 ? pb0 : array == 1 ? pb1 : array == 2 ? pa0 : pa1) + wave % kPer * kStage;
   const int lane = threadIdx.x & (kWave - 1);
@@ -505,7 +530,7 @@ using LinearKernel = void (*)(LinearArgs);
 template <int TYPE, int ALAY, int BLAY, int HELD>
 LinearKernel pick_linear(int tile_m, bool direct) {
   if (direct) {
-    if (tile_m == 256) return linear_kernel<TYPE, ALAY, BLAY, 256, 256, 2, 4, kDirect, HELD>;
+    if (tile_m == 256) return linear_kernel<TYPE, ALAY, BLAY, 256, 256, 2, 2, kDirect, HELD>;
     if (tile_m == 128) return linear_kernel<TYPE, ALAY, BLAY, 128, 128, 2, 2, kDirect, HELD>;
     return linear_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, kDirect, HELD>;
   }
@@ -543,8 +568,7 @@ int queue_linear(LinearArgs g, int type, int held, bool direct, void* work, int6
     kern = type == MOC_BF16 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, direct) : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, direct);
   }
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const int threads = p.tile_m == 256 ? 512 : 256;
-  hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(threads), 0, stream, g);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(256), 0, stream, g);
   MOC_HIP(hipGetLastError());
   if (p.splits > 1) {
     hipLaunchKernelGGL(linear_join_kernel, grid_of(ceil_div(g.m * (p.partial_stride / kRun), 256)), dim3(256), 0, stream, g);
