@@ -308,7 +308,7 @@ __device__ __forceinline__ void interleave() {
 
 // TYPE of the operands; HELD: of b, TYPE or a checkpoint's.
 template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int LOAD, int HELD>
-__global__ __launch_bounds__(WM* WN* kWave, BM == 256 ? 1 : 2) void linear_kernel(LinearArgs g) {
+__global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;   // 32 x 32 outputs of a wave
   __shared__ __attribute__((aligned(1024))) uint8_t a0[BM * kRowBytes], a1[BM * kRowBytes], b0[BN * kRowBytes], b1[BN * kRowBytes];
@@ -530,7 +530,7 @@ using LinearKernel = void (*)(LinearArgs);
 template <int TYPE, int ALAY, int BLAY, int HELD>
 LinearKernel pick_linear(int tile_m, bool direct) {
   if (direct) {
-    if (tile_m == 256) return linear_kernel<TYPE, ALAY, BLAY, 256, 256, 2, 2, kDirect, HELD>;
+    if (tile_m == 256) return linear_kernel<TYPE, ALAY, BLAY, 256, 256, 2, 4, kDirect, HELD>;
     if (tile_m == 128) return linear_kernel<TYPE, ALAY, BLAY, 128, 128, 2, 2, kDirect, HELD>;
     return linear_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, kDirect, HELD>;
   }
@@ -568,7 +568,7 @@ int queue_linear(LinearArgs g, int type, int held, bool direct, void* work, int6
     kern = type == MOC_BF16 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, direct) : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, direct);
   }
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(256), 0, stream, g);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(p.tile_m == 256 ? 512 : 256), 0, stream, g);
   MOC_HIP(hipGetLastError());
   if (p.splits > 1) {
     hipLaunchKernelGGL(linear_join_kernel, grid_of(ceil_div(g.m * (p.partial_stride / kRun), 256)), dim3(256), 0, stream, g);
