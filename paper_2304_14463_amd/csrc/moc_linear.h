@@ -51,13 +51,12 @@ struct Epilogue {
   const void* bias;
   int bias_type;
   int act;
-  const void* residual;
-  int residual_type;
-  int64_t residual_stride;
-  const void* pre;            // the activation's argument: times its derivative
-  const uint8_t* pre_scales;
-  int pre_type;
-  int64_t pre_stride, pre_scale_stride;
+  // A matrix of the output's sizes: the residual, or the activation's argument, through whose
+  // derivative the sum goes then (`slope`).  Null: none.
+  const void* extra;
+  const uint8_t* extra_scales;
+  int extra_type, slope;
+  int64_t extra_stride, extra_scale_stride;
   void* out;
   int out_type;
   int64_t out_stride;
@@ -82,35 +81,82 @@ __device__ __forceinline__ const char* row_at(const void* x, int type, int64_t r
   return static_cast<const char*>(x) + row * stride * (type == MOC_F32 ? 4 : type == MOC_BF16 || type == MOC_F16 ? 2 : 1);
 }
 
-// What is left of a run after the bias and the checkpoint.
-__device__ __forceinline__ void finish_run(const Epilogue& e, int64_t row, int col, int n, float (&v)[kRun]) {
-  if (e.pre) {
-    float u[kRun];
-    const char* p = row_at(e.pre, e.pre_type, row, e.pre_stride);
-    if (e.pre_type == MOC_E4M3) load_held<MOC_E4M3>(p, e.pre_scales + row * e.pre_scale_stride, col, n, u);
-    else if (e.pre_type == MOC_I8) load_held<MOC_I8>(p, e.pre_scales + row * e.pre_scale_stride, col, n, u);
-    else load_any(e.pre_type, p, col, n, u);
+// A run of the extra operand as it lies in memory: loaded early, converted when it is used.
+struct Raw {
+  u32x4 a, b;
+  uint32_t scale;
+};
+
+__device__ __forceinline__ Raw load_extra(const Epilogue& e, int64_t row, int col, int n) {
+  Raw x = {};
+  if (!e.extra || n <= 0) return x;
+  const char* p = row_at(e.extra, e.extra_type, row, e.extra_stride);
+  if (e.extra_type == MOC_E4M3 || e.extra_type == MOC_I8) {
+    const uint2 c = load_codes(reinterpret_cast<const uint8_t*>(p) + col, n);
+    x.a[0] = c.x;
+    x.a[1] = c.y;
+    x.scale = e.extra_scales[row * e.extra_scale_stride + col / MOC_BLOCK];
+  } else if (e.extra_type == MOC_F32) {
+    const float* f = reinterpret_cast<const float*>(p) + col;
+    if (n >= kRun) {
+      __builtin_memcpy(&x.a, f, 16);
+      __builtin_memcpy(&x.b, f + 4, 16);
+    } else {
 #pragma unroll
-    for (int i = 0; i < kRun; ++i) v[i] = times_slope(e.act, v[i], u[i]);
+      for (int i = 0; i < kRun - 1; ++i)
+        if (i < n) (i < 4 ? x.a : x.b)[i & 3] = float_bits(f[i]);
+    }
+  } else {
+    const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + col;
+    if (n >= kRun) {
+      __builtin_memcpy(&x.a, h, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kRun - 1; ++i)
+        if (i < n) x.a[i >> 1] |= (uint32_t)h[i] << (16 * (i & 1));
+    }
+  }
+  return x;
+}
+
+__device__ __forceinline__ void values_of(int type, const Raw& x, float (&v)[kRun]) {
+  if (type == MOC_E4M3) {
+    decode_run<MOC_E4M3>(uint2{x.a[0], x.a[1]}, scale_of((uint8_t)x.scale), v);
+  } else if (type == MOC_I8) {
+    decode_run<MOC_I8>(uint2{x.a[0], x.a[1]}, scale_of((uint8_t)x.scale), v);
+  } else if (type == MOC_F32) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = bits_float(i < 4 ? x.a[i & 3] : x.b[i & 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      const uint16_t h = (uint16_t)(x.a[i >> 1] >> (16 * (i & 1)));
+      v[i] = type == MOC_BF16 ? bits_float((uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+    }
+  }
+}
+
+// A run of finished sums; the four lanes of a quad have a block of a row, n <= 0 beyond the row.
+__device__ __forceinline__ void finish_sum(const Epilogue& e, int64_t row, int col, int n, const float (&bias)[kRun], const Raw& extra, float (&v)[kRun]) {
+#pragma unroll
+  for (int r = 0; r < kRun; ++r) v[r] = r < n ? v[r] + bias[r] : 0.0f;
+  if (e.codes) keep_any(e.kept_type, v, col, n, e.most, e.codes + row * e.code_stride, e.scales + row * e.scale_stride);
+  if (n <= 0) return;
+  if (e.extra) {
+    float x[kRun];
+    values_of(e.extra_type, extra, x);
+    if (e.slope) {
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) v[i] = times_slope(e.act, v[i], x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) v[i] = act_of(e.act, v[i]) + x[i];
+    }
   } else if (e.act != MOC_ACT_NONE) {
 #pragma unroll
     for (int i = 0; i < kRun; ++i) v[i] = act_of(e.act, v[i]);
   }
-  if (e.residual) {
-    float r[kRun];
-    load_any(e.residual_type, row_at(e.residual, e.residual_type, row, e.residual_stride), col, n, r);
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) v[i] += r[i];
-  }
   store_any(e.out_type, const_cast<char*>(row_at(e.out, e.out_type, row, e.out_stride)), col, n, v);
-}
-
-// A run of finished sums; the four lanes of a quad have a block of a row, n <= 0 beyond the row.
-__device__ __forceinline__ void finish_sum(const Epilogue& e, int64_t row, int col, int n, const float (&bias)[kRun], float (&v)[kRun]) {
-#pragma unroll
-  for (int r = 0; r < kRun; ++r) v[r] = r < n ? v[r] + bias[r] : 0.0f;
-  if (e.codes) keep_any(e.kept_type, v, col, n, e.most, e.codes + row * e.code_stride, e.scales + row * e.scale_stride);
-  if (n > 0) finish_run(e, row, col, n, v);
 }
 
 // ---- operands to LDS ----------------------------------------------------------------------------
@@ -188,7 +234,9 @@ struct DirectLoader {
     left -= step;
     k_left -= kStepK;
   }
-  __device__ __forceinline__ void put(Lds*) {}
+  static constexpr int kWork = 0, kWrites = 0;
+  __device__ __forceinline__ void put(Lds*, int) {}
+  __device__ __forceinline__ void mend(Lds*) {}
 };
 
 // Through registers: any alignment and size, and checkpoints, whose codes become values on the way.
@@ -196,7 +244,7 @@ template <int LAY, int WIDTH, int THREADS, int TYPE, int HELD>
 struct RegisterLoader {
   using T = Tile<LAY, WIDTH, THREADS>;
   using V = typename Stored<TYPE>::type;
-  static constexpr int kLoads = 0;   // left to the scheduler
+  static constexpr int kLoads = 0, kWork = 0, kWrites = 0;   // left to the scheduler
   static constexpr bool kKept = HELD == MOC_E4M3 || HELD == MOC_I8;
   Operand x;
   int first, extent, k, end;
@@ -236,9 +284,10 @@ struct RegisterLoader {
     }
     k += kStepK;
   }
-  __device__ __forceinline__ void put(Lds* to) {
+  __device__ __forceinline__ void mend(Lds*) {}
+  __device__ __forceinline__ void put(Lds* to, int h) {
 #pragma unroll
-    for (int i = 0; i < T::kEach; ++i) {
+    for (int i = h * T::kEach / 2; i < (h + 1) * T::kEach / 2; ++i) {
       u32x4 out = {held[i].x, held[i].y, held[i].z, held[i].w};
       if constexpr (kKept) {
         float v[kRun];
@@ -249,6 +298,105 @@ struct RegisterLoader {
         __builtin_memcpy(&out, t, 16);
       }
       *(__attribute__((address_space(3))) u32x4*)(to + (i * THREADS + (int)threadIdx.x) * 16) = out;
+    }
+  }
+};
+
+// A checkpoint whose rows and strides are multiples of 16: a thread has the 32 values of a block in one
+// row, that is two loads and one scale a step, and turns them into 16-bit values between the products.
+template <int WIDTH, int THREADS, int TYPE, int FMT>
+struct KeptLoader {
+  static_assert(WIDTH * kStepK / MOC_BLOCK == THREADS);
+  static constexpr int kPer = WIDTH / MOC_BLOCK;   // blocks of a row of the tile
+  static constexpr int kLoads = 3;
+  static constexpr int kWork = FMT == MOC_E4M3 ? 3 : 8;   // vector instructions for each product
+  static constexpr int kWrites = 4;
+  const uint8_t *base, *scale_base;
+  int64_t left, scale_left, step, scale_step;
+  int offset[2], scale_offset, place;
+  u32x4 codes[2];
+  uint8_t scale;
+  uint32_t rare = 0;
+
+  __device__ __forceinline__ KeptLoader(const Operand& x, int first, int extent, int begin, int end) {
+    const int row = threadIdx.x / kPer, block = threadIdx.x % kPer;
+    base = static_cast<const uint8_t*>(x.data) + begin * x.stride + first;
+    left = (int64_t)(end - begin - 1) * x.stride + (extent - first);
+    step = kStepK * x.stride;
+    scale_base = x.scales + begin * x.scale_stride + first / MOC_BLOCK;
+    scale_left = (int64_t)(end - begin - 1) * x.scale_stride + (extent - first + MOC_BLOCK - 1) / MOC_BLOCK;
+    scale_step = kStepK * x.scale_stride;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) offset[h] = first + block * MOC_BLOCK + 16 * h < extent ? (int)(row * x.stride) + block * MOC_BLOCK + 16 * h : kWindow;
+    scale_offset = first + block * MOC_BLOCK < extent ? (int)(row * x.scale_stride) + block : kWindow;
+    place = (row * (WIDTH / 8) + ((block * 4) ^ swizzle<kCol, WIDTH>(row))) * 16;   // moves whole blocks only
+  }
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t window(const uint8_t* base, int64_t left) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)(left < kWindow ? (left > 0 ? left : 0) : kWindow), 0x00020000);
+  }
+  __device__ __forceinline__ void load(Lds*) {
+    const __amdgpu_buffer_rsrc_t w = window(base, left);
+    scale = __builtin_amdgcn_raw_buffer_load_b8(window(scale_base, scale_left), scale_offset, 0, 0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) codes[h] = __builtin_amdgcn_raw_buffer_load_b128(w, offset[h], 0, 0);
+    base += step;
+    left -= step;
+    scale_base += scale_step;
+    scale_left -= scale_step;
+  }
+  __device__ __forceinline__ void put(Lds* to, int h) {
+    const float s = scale_of(scale);
+    u32x4 out[2];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t w = codes[h][q];
+      if constexpr (FMT == MOC_E4M3) {   // a power of two is exact, as the conversion is
+        if constexpr (TYPE == MOC_BF16) {
+          out[q >> 1][2 * q & 3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, s, false));
+          out[q >> 1][(2 * q & 3) + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, s, true));
+        } else {
+          const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+          out[q >> 1][2 * q & 3] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)(lo[0] * s), (_Float16)(lo[1] * s)});
+          out[q >> 1][(2 * q & 3) + 1] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)(hi[0] * s), (_Float16)(hi[1] * s)});
+        }
+      } else {
+        // code + 128, of which a byte is taken in one instruction; exact unless 128 * s overflows
+        const uint32_t u = w ^ 0x80808080u;
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __builtin_fmaf((float)(u >> (8 * i) & 0xFF), s, s * -128.0f);
+        rare |= (u - 0x01010101u) & ~u & 0x80808080u;   // a byte of it is 0 (and perhaps, for nothing, a 1 above one)
+        if constexpr (TYPE == MOC_BF16) {
+          out[q >> 1][2 * q & 3] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)f[0], (__bf16)f[1]});
+          out[q >> 1][(2 * q & 3) + 1] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)f[2], (__bf16)f[3]});
+        } else {
+          out[q >> 1][2 * q & 3] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)f[0], (_Float16)f[1]});
+          out[q >> 1][(2 * q & 3) + 1] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)f[2], (_Float16)f[3]});
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *(__attribute__((address_space(3))) u32x4*)(to + place + (2 * h + i) * 16) = out[i];
+  }
+  // What put() does not look at, behind it: codes of NaN, and scales of 2^121 and above.
+  __device__ __forceinline__ void mend(Lds* to) {
+    if constexpr (FMT == MOC_I8) {
+      if (rare != 0 || scale >= 127 + 121) {
+        using V = typename Stored<TYPE>::type;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const u32x4 c = codes[i >> 1];
+          float v[kRun];
+          decode_run<FMT>(i & 1 ? uint2{c[2], c[3]} : uint2{c[0], c[1]}, scale_of(scale), v);
+          V t[kRun];
+#pragma unroll
+          for (int j = 0; j < kRun; ++j) t[j] = (V)v[j];
+          u32x4 out;
+          __builtin_memcpy(&out, t, 16);
+          *(__attribute__((address_space(3))) u32x4*)(to + place + i * 16) = out;
+        }
+      }
+      rare = 0;
     }
   }
 };
@@ -292,17 +440,28 @@ struct Reader {
 
 // ---- the kernel ---------------------------------------------------------------------------------
 
-// Has the scheduler put a read from LDS behind each product, as long as there are any, and then the
-// loads into it, evenly.
-template <int MFMA, int READS, int LOADS, int I = 0>
+template <int TYPE, int LAY, int WIDTH, int THREADS, int LOAD, int HELD>
+struct PickB { using type = RegisterLoader<LAY, WIDTH, THREADS, TYPE, HELD>; };
+template <int TYPE, int LAY, int WIDTH, int THREADS>
+struct PickB<TYPE, LAY, WIDTH, THREADS, kDirect, TYPE> { using type = DirectLoader<LAY, WIDTH, THREADS>; };
+template <int TYPE, int WIDTH, int THREADS>
+struct PickB<TYPE, kCol, WIDTH, THREADS, kDirect, MOC_E4M3> { using type = KeptLoader<WIDTH, THREADS, TYPE, MOC_E4M3>; };
+template <int TYPE, int WIDTH, int THREADS>
+struct PickB<TYPE, kCol, WIDTH, THREADS, kDirect, MOC_I8> { using type = KeptLoader<WIDTH, THREADS, TYPE, MOC_I8>; };
+
+// Has the scheduler put a read from LDS behind each product, as long as there are any, then the loads
+// into it, evenly; and `WORK` vector instructions and the writes to LDS that follow from them.
+template <int MFMA, int READS, int LOADS, int WORK, int WRITES, int I = 0>
 __device__ __forceinline__ void interleave() {
   if constexpr (I < MFMA) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     constexpr int kAt = (READS + MFMA - 1) / MFMA, kReads = READS < kAt ? READS : kAt;
-    constexpr int kLoads = (LOADS + MFMA - I - 1) / (MFMA - I);
+    constexpr int kLoads = (LOADS + MFMA - I - 1) / (MFMA - I), kWrites = I * 2 < MFMA ? 0 : (WRITES + MFMA - I - 1) / (MFMA - I);
     if constexpr (kReads > 0) __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
     if constexpr (kLoads > 0) __builtin_amdgcn_sched_group_barrier(0x020, kLoads, 0);
-    interleave<MFMA, READS - kReads, LOADS - kLoads, I + 1>();
+    if constexpr (WORK > 0) __builtin_amdgcn_sched_group_barrier(0x002, WORK, 0);
+    if constexpr (kWrites > 0) __builtin_amdgcn_sched_group_barrier(0x200, kWrites, 0);
+    interleave<MFMA, READS - kReads, LOADS - kLoads, WORK, WRITES - kWrites, I + 1>();
   }
 }
 
@@ -323,7 +482,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
   const int begin = blockIdx.y * g.split_k, end = min(g.k, begin + g.split_k);
 
   using LoadA = typename std::conditional<LOAD == kDirect, DirectLoader<ALAY, BM, kThreads>, RegisterLoader<ALAY, BM, kThreads, TYPE, TYPE>>::type;
-  using LoadB = typename std::conditional<LOAD == kDirect && HELD == TYPE, DirectLoader<BLAY, BN, kThreads>, RegisterLoader<BLAY, BN, kThreads, TYPE, HELD>>::type;
+  using LoadB = typename PickB<TYPE, BLAY, BN, kThreads, LOAD, HELD>::type;
   LoadA la(g.a, m0, g.m, begin, end);
   LoadB lb(g.b, n0, g.n, begin, end);
 
@@ -356,9 +515,9 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
     la.load(a);
     lb.load(b);
   };
-  const auto put = [&](Lds* a, Lds* b) {
-    la.put(a);
-    lb.put(b);
+  const auto put = [&](Lds* a, Lds* b, int h) {
+    la.put(a, h);
+    lb.put(b, h);
   };
   const auto arrived = [] {
     __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0): this wave's loads into LDS, its reads and writes
@@ -374,15 +533,20 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
     for (int s = 0; s < 3; ++s) {
       fetch(a, b, s + 1);
       multiply(s);
-      interleave<TM * TN, kReads, 0>();
-      if (s < 2) __builtin_amdgcn_sched_barrier(0);
+      if (s == 0) {
+        interleave<TM * TN, kReads, 0, 0, 0>();
+      } else {
+        put(c, d, s - 1);
+        interleave<TM * TN, kReads, 0, LoadB::kWork, LoadB::kWrites / 2>();
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    put(c, d);
+    lb.mend(d);
     arrived();
     fetch(c, d, 0);
     load(a, b);
     multiply(3);
-    interleave<TM * TN, kReads, LoadA::kLoads + LoadB::kLoads>();
+    interleave<TM * TN, kReads, LoadA::kLoads + LoadB::kLoads, 0, 0>();
     __builtin_amdgcn_sched_barrier(0);
   };
   // Steps in pairs, so that each buffer has its own code (and the compiler sees that the loads do not
@@ -391,14 +555,18 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
   const int steps = end > begin ? (end - begin + kStepK - 1) / kStepK : 0;
   if (steps & 1) {
     load(pa1, pb1);
-    put(pa1, pb1);
+    put(pa1, pb1, 0);
+    put(pa1, pb1, 1);
+    lb.mend(pb1);
     arrived();
     fetch(pa1, pb1, 0);
     load(pa0, pb0);
     step(pa1, pb1, pa0, pb0);
   } else if (steps > 0) {
     load(pa0, pb0);
-    put(pa0, pb0);
+    put(pa0, pb0, 0);
+    put(pa0, pb0, 1);
+    lb.mend(pb0);
     arrived();
     fetch(pa0, pb0, 0);
     load(pa1, pb1);
@@ -425,8 +593,14 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
 #pragma unroll
   for (int r = 0; r < kRun; ++r) bias[r] = 0.0f;
   if (g.e.bias && g.splits == 1 && n > 0) load_any(g.e.bias_type, g.e.bias, col, n, bias);
+  constexpr int kAhead = 3;   // rows of the extra operand on their way
+  Raw ahead[kAhead];
 #pragma unroll
   for (int half = 0; half < TM / TH; ++half) {
+    const int row0 = m0 + wm + half * TH * 32 + lane / kRuns;
+    const auto extra = [&](int at) { return row0 + at * kRowsAt < g.m && at * kRowsAt < TH * 32 && g.splits == 1 ? load_extra(g.e, row0 + at * kRowsAt, col, n) : Raw{}; };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ahead[i] = extra(i);
 #pragma unroll
     for (int i = 0; i < TH; ++i)
 #pragma unroll
@@ -438,9 +612,13 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
           *(__attribute__((address_space(3))) f32x4*)(stage + m * (kCols * 4) + (chunk ^ (m & kMove)) * 16) = f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
         }
 #pragma unroll 1
-    for (int m = lane / kRuns; m < TH * 32; m += kRowsAt) {
-      const int row = m0 + wm + half * TH * 32 + m;
+    for (int at = 0; at < TH * 32 / kRowsAt; ++at) {
+      const int row = row0 + at * kRowsAt, m = lane / kRuns + at * kRowsAt;
       if (row >= g.m) break;   // all lanes of a row, and of a quad
+      const Raw now = ahead[0];
+#pragma unroll
+      for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
+      ahead[kAhead - 1] = extra(at + kAhead);
       float v[kRun];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -451,7 +629,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
       if (g.splits > 1) {
         if (col < g.partial_stride) store_run<MOC_F32>(g.partial + ((int64_t)blockIdx.y * g.m + row) * g.partial_stride, col, kRun, v);
       } else {
-        finish_sum(g.e, row, col, n, bias, v);
+        finish_sum(g.e, row, col, n, bias, now, v);
       }
     }
   }
@@ -475,7 +653,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs g) {
   }
   float bias[kRun] = {};
   if (e.bias && n > 0) load_any(e.bias_type, e.bias, col, n, bias);
-  finish_sum(e, row, col, n, bias, v);
+  finish_sum(e, row, col, n, bias, load_extra(e, row, col, n), v);
 }
 
 // ---- dispatch -----------------------------------------------------------------------------------
@@ -502,8 +680,8 @@ inline LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, bool direct, int 
   p.tiles_m = (int)ceil_div(m, p.tile_m);
   p.tiles_n = (int)ceil_div(n, p.tile_n);
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, steps = ceil_div(k, kStepK);
-  // Few tiles: k is cut too, at least four steps a split, until two workgroups a compute unit have work.
-  int64_t splits = tiles ? 2 * (int64_t)units / tiles : 1;
+  // Few tiles: k is cut too, at least four steps a split, until every compute unit has the workgroups that it holds.
+  int64_t splits = tiles ? (p.tile_m == 256 ? 1 : 2) * (int64_t)units / tiles : 1;
   if (splits > steps / 4) splits = steps / 4;
   if (splits < 1) splits = 1;
   const int64_t each = ceil_div(steps, splits);
@@ -517,12 +695,23 @@ inline LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, bool direct, int 
 // Whether an operand of 16-bit values can go straight into LDS, `along` values of it in a row.
 inline bool direct_ok(const moc_matrix* x, int64_t along) { return aligned_to(x->data, 16) && x->stride % 8 == 0 && along % 8 == 0; }
 
+// Whether a checkpoint can take KeptLoader.
+inline bool kept_direct_ok(const moc_matrix* x, int64_t along) { return aligned_to(x->data, 16) && x->stride % 16 == 0 && along % 16 == 0; }
+
 inline Operand operand_of(const moc_matrix* x) { return Operand{x->data, x->scales, x->stride, x->scale_stride}; }
 
 inline void set_out(Epilogue& e, const moc_matrix* out) {
   e.out = out->data;
   e.out_type = out->type;
   e.out_stride = out->stride;
+}
+
+// Stretches of rows that the bias's gradient is summed over: two workgroups a compute unit, at least 64
+// rows each (their sums are written and read again).
+inline int64_t moc_bias_stretches(int64_t rows, int64_t cout, int units) {
+  const int64_t across = ceil_div(cout, 512), wanted = 2 * (int64_t)units / across, most = rows / 64;
+  const int64_t n = wanted < most ? wanted : most;
+  return n < 1 ? 1 : n;
 }
 
 using LinearKernel = void (*)(LinearArgs);

@@ -23,9 +23,9 @@ int moc_linear_forward(int64_t rows, int64_t cin, int64_t cout, const moc_matrix
   e.bias_type = bias_type;
   e.act = act;
   if (residual) {
-    e.residual = residual->data;
-    e.residual_type = residual->type;
-    e.residual_stride = residual->stride;
+    e.extra = residual->data;
+    e.extra_type = residual->type;
+    e.extra_stride = residual->stride;
   }
   set_out(e, y);
   if (kept) {
@@ -44,7 +44,7 @@ int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout) {
   int units = 0;
   const int rc = moc_compute_units(&units);
   if (rc != MOC_OK) return rc;
-  int64_t most = 0;
+  int64_t most = cout > 0 ? moc_bias_stretches(rows, cout, units) * cout * (int64_t)sizeof(float) : 0;
   for (int direct = 0; direct < 2; ++direct) {
     const int64_t sizes[3][3] = {{rows, cout, cin}, {rows, cin, cout}, {cout, cin, rows}};
     for (const auto& s : sizes) {

@@ -17,11 +17,12 @@ extern "C" int moc_linear_backward_input(int64_t rows, int64_t cin, int64_t cout
   Epilogue& e = g.e;
   e.act = act;
   if (pre && act != MOC_ACT_NONE) {
-    e.pre = pre->data;
-    e.pre_scales = pre->scales;
-    e.pre_type = pre->type;
-    e.pre_stride = pre->stride;
-    e.pre_scale_stride = pre->scale_stride;
+    e.extra = pre->data;
+    e.extra_scales = pre->scales;
+    e.extra_type = pre->type;
+    e.extra_stride = pre->stride;
+    e.extra_scale_stride = pre->scale_stride;
+    e.slope = 1;
   }
   set_out(e, dx);
   return queue_linear<kRow, kCol, false>(g, dy->type, dy->type, direct_ok(dy, cout) && direct_ok(w, cin), work, work_bytes, hip_stream);

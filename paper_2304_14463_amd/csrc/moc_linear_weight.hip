@@ -3,25 +3,54 @@
 
 namespace {
 
-// db: a column sum of dy.  64 columns a workgroup of 16 x 64 threads, rows in one order.
-__global__ __launch_bounds__(1024) void bias_grad_kernel(const void* dy, int type, int64_t stride, int64_t rows, int cols, float* db) {
-  __shared__ float stage[16][64];
-  const int col = blockIdx.x * 64 + (threadIdx.x & 63), mine = threadIdx.x >> 6;
-  float s = 0.0f;
-  if (col < cols) {
-    for (int64_t row = mine; row < rows; row += 16) {
-      const uint16_t* p = static_cast<const uint16_t*>(dy) + row * stride + col;
-      s += type == MOC_BF16 ? (float)__builtin_bit_cast(__bf16, *p) : (float)__builtin_bit_cast(_Float16, *p);
-    }
-  }
-  stage[mine][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (mine == 0 && col < cols) {
-    s = 0.0f;
+// db: a column sum of dy, bound by memory.  A workgroup has 512 columns, eight a lane, and a stretch of
+// rows, which its four waves take in turn, four at a time; where the rows are cut into several
+// stretches their sums meet in the workspace and are added in order.
+constexpr int kBiasCols = kWave * kRun, kBiasWaves = 4;
+
+struct BiasArgs {
+  const void* dy;
+  int type;
+  int64_t stride, rows, each;   // rows of a stretch
+  int cols;
+  float* out;                   // [stretches][cols]
+};
+
+template <int TYPE>
+__global__ __launch_bounds__(kBiasWaves * kWave) void bias_grad_kernel(BiasArgs g) {
+  __shared__ float stage[kBiasWaves][kRun][kWave];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int col = blockIdx.x * kBiasCols + lane * kRun, n = g.cols - col;
+  const int64_t begin = blockIdx.y * g.each, end = begin + g.each < g.rows ? begin + g.each : g.rows;
+  float s[kRun] = {};
+  constexpr int kAt = 4;
+  for (int64_t row = begin + wave; row < end; row += kAt * kBiasWaves) {
+    float v[kAt][kRun];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s += stage[i][threadIdx.x];
-    db[col] = s;
+    for (int i = 0; i < kAt; ++i) {
+      const int64_t r = row + i * kBiasWaves;
+      load_run<TYPE>(static_cast<const uint16_t*>(g.dy) + (r < end ? r : row) * g.stride, n > 0 ? col : 0, r < end ? n : 0, v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kAt; ++i)
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) s[j] += v[i][j];
   }
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) stage[wave][j][lane] = s[j];
+  __syncthreads();
+  if (wave != 0 || n <= 0) return;
+#pragma unroll
+  for (int j = 0; j < kRun; ++j) s[j] = stage[0][j][lane] + stage[1][j][lane] + stage[2][j][lane] + stage[3][j][lane];
+  store_run<MOC_F32>(g.out + (int64_t)blockIdx.y * g.cols, col, n, s);
+}
+
+__global__ __launch_bounds__(256) void bias_join_kernel(const float* parts, int stretches, int cols, float* db) {
+  const int col = blockIdx.x * 256 + threadIdx.x;
+  if (col >= cols) return;
+  float s = 0.0f;
+  for (int i = 0; i < stretches; ++i) s += parts[(int64_t)i * cols + col];
+  db[col] = s;
 }
 
 }  // namespace
@@ -33,6 +62,9 @@ extern "C" int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cou
   if (!matrix_ok(x, rows, cin, true, true) || (is_value(x->type) && x->type != dy->type)) return MOC_EINVAL;
   if (!matrix_ok(dw, cout, cin, true, false) || (dw->type != dy->type && dw->type != MOC_F32) || !aligned_to(db, 4)) return MOC_EINVAL;
   if (cout == 0) return MOC_OK;
+  int units = 0;
+  const int asked = moc_compute_units(&units);
+  if (asked != MOC_OK) return asked;
   if (cin > 0) {
     LinearArgs g = {};
     g.a = operand_of(dy);
@@ -41,14 +73,29 @@ extern "C" int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cou
     g.n = (int)cin;
     g.k = (int)rows;
     set_out(g.e, dw);
-    const bool direct = direct_ok(dy, cout) && (is_kept(x->type) || direct_ok(x, cin));
+    const bool direct = direct_ok(dy, cout) && (is_kept(x->type) ? kept_direct_ok(x, cin) : direct_ok(x, cin));
     const int rc = queue_linear<kCol, kCol, true>(g, dy->type, x->type, direct, work, work_bytes, hip_stream);
     if (rc != MOC_OK) return rc;
   }
   if (db) {
-    hipLaunchKernelGGL(bias_grad_kernel, dim3((unsigned)((cout + 63) / 64)), dim3(1024), 0, static_cast<hipStream_t>(hip_stream), dy->data, dy->type,
-                       dy->stride, rows, (int)cout, db);
+    const int64_t stretches = moc_bias_stretches(rows, cout, units);
+    if (stretches > 1 && (!work || !aligned_to(work, 16) || work_bytes < stretches * cout * (int64_t)sizeof(float))) return MOC_EINVAL;
+    BiasArgs g = {};
+    g.dy = dy->data;
+    g.type = dy->type;
+    g.stride = dy->stride;
+    g.rows = rows;
+    g.each = (rows + stretches - 1) / stretches;
+    g.cols = (int)cout;
+    g.out = stretches > 1 ? static_cast<float*>(work) : db;   // the product is done with the workspace: one stream
+    const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    const dim3 grid((unsigned)((cout + kBiasCols - 1) / kBiasCols), (unsigned)stretches);
+    hipLaunchKernelGGL(dy->type == MOC_BF16 ? bias_grad_kernel<MOC_BF16> : bias_grad_kernel<MOC_F16>, grid, dim3(kBiasWaves * kWave), 0, stream, g);
     MOC_HIP(hipGetLastError());
+    if (stretches > 1) {
+      hipLaunchKernelGGL(bias_join_kernel, dim3((unsigned)((cout + 255) / 256)), dim3(256), 0, stream, g.out, (int)stretches, (int)cout, db);
+      MOC_HIP(hipGetLastError());
+    }
   }
   return MOC_OK;
 }

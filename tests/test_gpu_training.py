@@ -388,6 +388,44 @@ def test_linear_backward_weight(tr, rows, cin, cout, dtype, held, narrow):
         assert tr.moc_linear_backward_weight(framed(dy, lead, pad), xin, want_bias=False)[1] is None
 
 
+@pytest.mark.parametrize("rows,cin,cout", [(70, 48, 64), (515, 336, 264), (64, 2064, 8), (129, 16, 1032)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_weight_gradient_from_whole_blocks(tr, rows, cin, cout, dtype, fmt):
+    """Sizes whose checkpoints are read 16 codes at a time, half blocks at the rows' ends among them."""
+    dtype = TYPES[dtype]
+    g = gen("blocks", rows, cin, cout, fmt)
+    dy, x = (0.1 * normal(g, rows, cout)).to(dtype), (normal(g, rows, cin) * torch.exp(normal(g, cin))).to(dtype)
+    x[rows // 2, cin // 2] = math.nan
+    codes, scales = ref.keep(x.double(), fmt, dtype)
+    v = ref.values(codes, scales, fmt).to(dtype).double()
+    for pad in (0, 16):
+        kept, _, _ = framed_checkpoint(tr, rows, cin, fmt, 16 - (cin + pad) % 16, pad)
+        kept.codes.copy_(codes), kept.scales.copy_(scales)
+        out = Framed(cout, cin, torch.float32)
+        dw, _ = tr.moc_linear_backward_weight(framed(dy, 0, 0), kept, out=out.inner)
+        near(dw, dy.double().t() @ v, sum_bound(dy.t(), v.nan_to_num(), rows))
+        assert out.intact()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_every_code_in_a_product(tr, fmt, dtype):
+    """one row times 1: the product gives every code's value with every scale that the type can hold"""
+    dtype = TYPES[dtype]
+    bytes_ = torch.arange(16, 250) if dtype == torch.bfloat16 else torch.arange(103, 136)
+    codes = torch.arange(256, dtype=torch.uint8).repeat(len(bytes_))[None]
+    scales = bytes_.to(torch.uint8).repeat_interleave(8)[None]
+    kept = tr.Checkpoint(codes.cuda(), scales.cuda(), fmt)
+    one = torch.zeros(1, 8, dtype=dtype, device="cuda")
+    one[0, 3] = 1
+    want = tr.moc_checkpoint_read(kept, dtype).float()[0]
+    assert torch.equal(want.cpu().nan_to_num(1.5, math.inf, -math.inf), ref.values(codes, scales, fmt)[0].to(dtype).float().nan_to_num(1.5, math.inf, -math.inf))
+    dw, _ = tr.moc_linear_backward_weight(one, kept)
+    assert torch.equal(dw[3].nan_to_num(1.5, math.inf, -math.inf), want.nan_to_num(1.5, math.inf, -math.inf))
+    assert not dw[0].nan_to_num(0, 0, 0).any()
+
+
 @pytest.mark.parametrize("rows,cin,cout", [(4096, 4096, 3840), (3850, 4160, 4104)])
 def test_the_large_tiles(tr, rows, cin, cout):
     """Sizes whose outputs are many tiles of 256 x 256, whole ones and not; sampled rows in 64 bits."""
