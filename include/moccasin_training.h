@@ -123,11 +123,12 @@ int moc_norm_forward(int64_t rows, int64_t cols, const moc_matrix* x, const void
  * Layer norm's gradients, with h = (x - mean) * rstd and p = dy * gamma:
  *   dx = rstd * (p - mean(p) - h * mean(p * h)) + residual
  *   dgamma = sum over rows of dy * h,  dbeta = sum over rows of dy
- *   x         as it was given to moc_norm_forward, or a checkpoint of it
- *   residual  a tensor added to dx (the gradient of a branch around the
+ *   dy        float32, float16 or bfloat16
+ *   x         as it was given to moc_norm_forward, of dy's type, or a
+ *             checkpoint of it
+ *   residual  of dy's type, added to dx (the gradient of a branch around the
  *             norm), or NULL
- *   dx        a tensor; may be dy's or residual's own memory (same type and
- *             stride)
+ *   dx        of dy's type; may be dy's or residual's own memory (same stride)
  *   dgamma, dbeta  device, float [cols]; both or neither (NULL).  With rows ==
  *             0 they are set to zero.
  *   work      moc_norm_backward_work(rows, cols) bytes; NULL without dgamma

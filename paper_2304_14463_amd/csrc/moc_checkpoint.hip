@@ -55,10 +55,7 @@ __global__ __launch_bounds__(kThreads) void checkpoint_read_kernel(CheckpointArg
     if (n <= 0) continue;
     float v[kRun];
     load_held<FMT>(g.codes + at.row * g.code_stride, g.scales + at.row * g.scale_stride, at.col, n, v);
-    if (g.act != MOC_ACT_NONE) {
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) v[j] = act_of(g.act, v[j]);
-    }
+    act_run(g.act, v);
     store_run<TYPE>(static_cast<typename Stored<TYPE>::type*>(g.values) + at.row * g.stride, at.col, n, v);
   }
 }

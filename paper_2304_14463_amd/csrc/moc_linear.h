@@ -27,7 +27,6 @@ using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
 using f32x16 = float __attribute__((ext_vector_type(16)));
 using s16x4 = short __attribute__((ext_vector_type(4)));
 using s16x8 = short __attribute__((ext_vector_type(8)));
-using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
 using f32x4 = float __attribute__((ext_vector_type(4)));
 
 template <int TYPE>
@@ -81,59 +80,9 @@ __device__ __forceinline__ const char* row_at(const void* x, int type, int64_t r
   return static_cast<const char*>(x) + row * stride * (type == MOC_F32 ? 4 : type == MOC_BF16 || type == MOC_F16 ? 2 : 1);
 }
 
-// A run of the extra operand as it lies in memory: loaded early, converted when it is used.
-struct Raw {
-  u32x4 a, b;
-  uint32_t scale;
-};
-
 __device__ __forceinline__ Raw load_extra(const Epilogue& e, int64_t row, int col, int n) {
-  Raw x = {};
-  if (!e.extra || n <= 0) return x;
-  const char* p = row_at(e.extra, e.extra_type, row, e.extra_stride);
-  if (e.extra_type == MOC_E4M3 || e.extra_type == MOC_I8) {
-    const uint2 c = load_codes(reinterpret_cast<const uint8_t*>(p) + col, n);
-    x.a[0] = c.x;
-    x.a[1] = c.y;
-    x.scale = e.extra_scales[row * e.extra_scale_stride + col / MOC_BLOCK];
-  } else if (e.extra_type == MOC_F32) {
-    const float* f = reinterpret_cast<const float*>(p) + col;
-    if (n >= kRun) {
-      __builtin_memcpy(&x.a, f, 16);
-      __builtin_memcpy(&x.b, f + 4, 16);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kRun - 1; ++i)
-        if (i < n) (i < 4 ? x.a : x.b)[i & 3] = float_bits(f[i]);
-    }
-  } else {
-    const uint16_t* h = reinterpret_cast<const uint16_t*>(p) + col;
-    if (n >= kRun) {
-      __builtin_memcpy(&x.a, h, 16);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kRun - 1; ++i)
-        if (i < n) x.a[i >> 1] |= (uint32_t)h[i] << (16 * (i & 1));
-    }
-  }
-  return x;
-}
-
-__device__ __forceinline__ void values_of(int type, const Raw& x, float (&v)[kRun]) {
-  if (type == MOC_E4M3) {
-    decode_run<MOC_E4M3>(uint2{x.a[0], x.a[1]}, scale_of((uint8_t)x.scale), v);
-  } else if (type == MOC_I8) {
-    decode_run<MOC_I8>(uint2{x.a[0], x.a[1]}, scale_of((uint8_t)x.scale), v);
-  } else if (type == MOC_F32) {
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) v[i] = bits_float(i < 4 ? x.a[i & 3] : x.b[i & 3]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) {
-      const uint16_t h = (uint16_t)(x.a[i >> 1] >> (16 * (i & 1)));
-      v[i] = type == MOC_BF16 ? bits_float((uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h);
-    }
-  }
+  if (!e.extra || n <= 0) return Raw{};
+  return load_raw_any(e.extra_type, row_at(e.extra, e.extra_type, row, e.extra_stride), e.extra_scales + row * e.extra_scale_stride, col, n);
 }
 
 // A run of finished sums; the four lanes of a quad have a block of a row, n <= 0 beyond the row.
@@ -142,19 +91,18 @@ __device__ __forceinline__ void finish_sum(const Epilogue& e, int64_t row, int c
   for (int r = 0; r < kRun; ++r) v[r] = r < n ? v[r] + bias[r] : 0.0f;
   if (e.codes) keep_any(e.kept_type, v, col, n, e.most, e.codes + row * e.code_stride, e.scales + row * e.scale_stride);
   if (n <= 0) return;
-  if (e.extra) {
-    float x[kRun];
-    values_of(e.extra_type, extra, x);
-    if (e.slope) {
+  if (e.slope) {
+    float u[kRun];
+    values_of_any(e.extra_type, extra, u);
+    slope_run(e.act, v, u);
+  } else {
+    act_run(e.act, v);
+    if (e.extra) {
+      float r[kRun];
+      values_of_any(e.extra_type, extra, r);
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) v[i] = times_slope(e.act, v[i], x[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) v[i] = act_of(e.act, v[i]) + x[i];
+      for (int i = 0; i < kRun; ++i) v[i] += r[i];
     }
-  } else if (e.act != MOC_ACT_NONE) {
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) v[i] = act_of(e.act, v[i]);
   }
   store_any(e.out_type, const_cast<char*>(row_at(e.out, e.out_type, row, e.out_stride)), col, n, v);
 }

@@ -45,14 +45,6 @@ __global__ __launch_bounds__(kBiasWaves * kWave) void bias_grad_kernel(BiasArgs 
   store_run<MOC_F32>(g.out + (int64_t)blockIdx.y * g.cols, col, n, s);
 }
 
-__global__ __launch_bounds__(256) void bias_join_kernel(const float* parts, int stretches, int cols, float* db) {
-  const int col = blockIdx.x * 256 + threadIdx.x;
-  if (col >= cols) return;
-  float s = 0.0f;
-  for (int i = 0; i < stretches; ++i) s += parts[(int64_t)i * cols + col];
-  db[col] = s;
-}
-
 }  // namespace
 
 extern "C" int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cout, const moc_matrix* dy, const moc_matrix* x, const moc_matrix* dw,
@@ -93,7 +85,7 @@ extern "C" int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cou
     hipLaunchKernelGGL(dy->type == MOC_BF16 ? bias_grad_kernel<MOC_BF16> : bias_grad_kernel<MOC_F16>, grid, dim3(kBiasWaves * kWave), 0, stream, g);
     MOC_HIP(hipGetLastError());
     if (stretches > 1) {
-      hipLaunchKernelGGL(bias_join_kernel, dim3((unsigned)((cout + 255) / 256)), dim3(256), 0, stream, g.out, (int)stretches, (int)cout, db);
+      hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((cout + 63) / 64)), dim3(1024), 0, stream, g.out, (int)stretches, cout, cout, db);
       MOC_HIP(hipGetLastError());
     }
   }

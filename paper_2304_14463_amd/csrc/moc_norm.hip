@@ -3,7 +3,7 @@
 // Bound by memory: every value is read once and written once.  T threads take a row and hold it in
 // registers, CH runs of eight values each, so the variance is that of the differences from the mean
 // and nothing is read again; rows longer than the registers hold are read again from cache.
-// Forward: a wave a row up to 2048 columns (no barrier), then the fewest threads that hold it.
+// Forward: a wave a row up to 4096 columns (no barrier), then the fewest threads that hold it.
 // Backward: every workgroup goes over many rows and keeps its columns' two sums in registers; they
 // meet in the workspace, one row of sums a workgroup, and a second kernel adds those in their order.
 #include "moc_training.h"
@@ -30,17 +30,25 @@ struct NormArgs {
   float most;
   // backward
   const void *dy, *residual;   // residual may be null
-  int dy_type, residual_type;
   int64_t dy_stride, residual_stride;
   float* sums;            // [gridDim][2][cols], null: no parameter gradients
   int64_t rows;
   int cols;
 };
 
+// The sum over the wave, in all lanes: inside rows of 16 by shifts of the vector ALU, then across them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float add_shifted(float a) {
+  return a + bits_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)float_bits(a), CTRL, ROWS, 0xF, true));
+}
 __device__ __forceinline__ float wave_sum(float a) {
-#pragma unroll
-  for (int s = 1; s < kWave; s <<= 1) a += __shfl_xor(a, s, kWave);
-  return a;
+  a = add_shifted<0x111, 0xF>(a);   // row_shr:1, 2, 4, 8
+  a = add_shifted<0x112, 0xF>(a);
+  a = add_shifted<0x114, 0xF>(a);
+  a = add_shifted<0x118, 0xF>(a);
+  a = add_shifted<0x142, 0xA>(a);   // row_bcast:15 into rows 1 and 3, :31 into rows 2 and 3
+  a = add_shifted<0x143, 0xC>(a);
+  return bits_float((uint32_t)__builtin_amdgcn_readlane((int)float_bits(a), kWave - 1));
 }
 
 // Sums over the T threads that share a row, in all of them.  `room`: 2 x T / 64 floats of their own.
@@ -58,12 +66,9 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, float* room) {
       room[2 * wave + 1] = b;
     }
     __syncthreads();
-    a = b = 0.0f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      a += room[2 * w];
-      b += room[2 * w + 1];
-    }
+    const int lane = threadIdx.x % kWave;
+    a = wave_sum(lane < W ? room[2 * lane] : 0.0f);
+    b = wave_sum(lane < W ? room[2 * lane + 1] : 0.0f);
   }
 }
 template <int T>
@@ -94,6 +99,7 @@ template <int X>
 __device__ __forceinline__ void load_x(const NormArgs& g, int64_t row, int col, int n, float (&v)[kRun]) {
   load_held<X>(row_of<X>(g.x, row, g.x_stride), g.x_scales + row * g.x_scale_stride, col, n, v);
 }
+__device__ __forceinline__ bool whole_runs(const NormArgs& g) { return g.cols % kRun == 0; }
 
 // ---- forward ------------------------------------------------------------------------------------
 
@@ -118,15 +124,24 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormArg
   if (row >= g.rows) return;   // whole waves only, and whole workgroups where they share a row
   float v[CH][kRun];
   float s = 0.0f;
+  {
+    Raw w[CH];
+    const void* const x = row_of<X>(g.x, row, g.x_stride);
+    const uint8_t* const scales = g.x_scales + row * g.x_scale_stride;
+    if (whole_runs(g)) {
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int col = (c * T + lane) * kRun;
-    load_x<X>(g, row, min(col, g.cols - 1), g.cols - col, v[c]);
+      for (int c = 0; c < CH; ++c) w[c] = load_raw_whole<X>(x, scales, (c * T + lane) * kRun, g.cols);
+    } else {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) w[c] = load_raw<X>(x, scales, (c * T + lane) * kRun, g.cols - (c * T + lane) * kRun);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      values_of<X>(w[c], v[c]);
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) s += (c * T + lane) * kRun < g.cols ? v[c][i] : 0.0f;
+    }
   }
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) s += v[c][i];
   const float count = (float)g.cols;
   const float mean = row_sum<T>(s, room) / count;
   float q = 0.0f;
@@ -186,18 +201,58 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormArgs
 
 // ---- backward -----------------------------------------------------------------------------------
 
-// h and p = dy * gamma of a run, 0 beyond the row; dy stays in d.
-template <int X>
-__device__ __forceinline__ void load_grad(const NormArgs& g, int64_t row, int col, float mean, float rstd, float (&h)[kRun], float (&d)[kRun]) {
-  const int n = g.cols - col;
-  load_any(g.dy_type, row_any(g.dy, g.dy_type, row, g.dy_stride), min(col, g.cols - 1), n, d);
-  load_x<X>(g, row, min(col, g.cols - 1), n, h);
+// A row's run of x, dy and the residual, on its way or there.
+struct GradRaw {
+  Raw x, d, r;
+};
+template <int X, int D, bool WHOLE>
+__device__ __forceinline__ GradRaw load_grad(const NormArgs& g, int64_t row, int col) {
+  const void *const x = row_of<X>(g.x, row, g.x_stride), *const d = row_of<D>(g.dy, row, g.dy_stride), *const r = row_of<D>(g.residual, row, g.residual_stride);
+  const uint8_t* const scales = g.x_scales + row * g.x_scale_stride;
+  GradRaw w = {};
+  if constexpr (WHOLE) {
+    w.x = load_raw_whole<X>(x, scales, col, g.cols);
+    w.d = load_raw_whole<D>(d, nullptr, col, g.cols);
+    if (g.residual) w.r = load_raw_whole<D>(r, nullptr, col, g.cols);
+  } else {
+    w.x = load_raw<X>(x, scales, col, g.cols - col);
+    w.d = load_raw<D>(d, nullptr, col, g.cols - col);
+    if (g.residual) w.r = load_raw<D>(r, nullptr, col, g.cols - col);
+  }
+  return w;
+}
+template <int X, int D, int T, int CH>
+__device__ __forceinline__ void load_grads(const NormArgs& g, int64_t row, int lane, GradRaw (&w)[CH]) {
+  if (whole_runs(g)) {
 #pragma unroll
-  for (int i = 0; i < kRun; ++i) h[i] = i < n ? (h[i] - mean) * rstd : 0.0f;
+    for (int c = 0; c < CH; ++c) w[c] = load_grad<X, D, true>(g, row, (c * T + lane) * kRun);
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) w[c] = load_grad<X, D, false>(g, row, (c * T + lane) * kRun);
+  }
 }
 
+// To the compiler, another value from here on.
+__device__ __forceinline__ void opaque(Raw& w) {
+  asm("" : "+v"(w.a));
+  asm("" : "+v"(w.b));
+}
+
+// h and dy of a run, 0 beyond the row.
+template <int X, int D>
+__device__ __forceinline__ void values_of_grad(const NormArgs& g, const GradRaw& w, int col, float mean, float rstd, float (&h)[kRun], float (&d)[kRun]) {
+  values_of<X>(w.x, h);
+  values_of<D>(w.d, d);
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) {
+    h[i] = i < g.cols - col ? (h[i] - mean) * rstd : 0.0f;
+    d[i] = i < g.cols - col ? d[i] : 0.0f;
+  }
+}
+
+template <int D>
 __device__ __forceinline__ void store_dx(const NormArgs& g, int64_t row, int col, float rstd, float a, float b, const float (&h)[kRun], const float (&d)[kRun],
-                                         const float (&ga)[kRun]) {
+                                         const float (&ga)[kRun], const Raw& residual) {
   const int n = g.cols - col;
   if (n <= 0) return;
   float o[kRun];
@@ -205,11 +260,11 @@ __device__ __forceinline__ void store_dx(const NormArgs& g, int64_t row, int col
   for (int i = 0; i < kRun; ++i) o[i] = rstd * (d[i] * ga[i] - a - h[i] * b);
   if (g.residual) {
     float r[kRun];
-    load_any(g.residual_type, row_any(g.residual, g.residual_type, row, g.residual_stride), col, n, r);
+    values_of<D>(residual, r);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) o[i] += r[i];
   }
-  store_any(g.y_type, row_any(g.y, g.y_type, row, g.y_stride), col, n, o);
+  store_run<D>(const_cast<void*>(row_of<D>(g.y, row, g.y_stride)), col, n, o);
 }
 
 // The sums of a workgroup's rows groups (kRows of T lanes), added in their order, into its row of the
@@ -254,49 +309,96 @@ __device__ __forceinline__ void store_sums(const NormArgs& g, const float (&sg)[
   }
 }
 
-template <int X, int T, int CH>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_backward_kernel(NormArgs g) {
+// 16 waves a compute unit, 128 registers a thread.  The next row is on its way while the sums over this
+// one are taken.
+template <int X, int D, int T, int CH>
+__global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(NormArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
   static_assert(T <= kWave || kRows == 1);
   __shared__ float room[2 * T / kWave + 1];
   __shared__ float stage[kRows > 1 ? kRows * 16 * T : 1];
   const int lane = threadIdx.x % T;
-  float ga[CH][kRun], sg[CH][kRun], sb[CH][kRun];
+  constexpr bool kHold = CH == 1;   // gamma, in registers; from cache where two runs leave none
+  float held[kRun], sg[CH][kRun], sb[CH][kRun];
+  const auto gamma_of = [&](int c, float(&ga)[kRun]) {
+    const int col = (c * T + lane) * kRun;
+    load_param(g.gamma, g.param_type, min(col, g.cols - 1), g.cols - col, 1.0f, ga);
+  };
+  if constexpr (kHold) gamma_of(0, held);
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    const int col = (c * T + lane) * kRun;
-    load_param(g.gamma, g.param_type, min(col, g.cols - 1), g.cols - col, 1.0f, ga[c]);
 #pragma unroll
     for (int i = 0; i < kRun; ++i) sg[c][i] = sb[c][i] = 0.0f;
   }
   const float count = (float)g.cols;
-  for (int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / T; row < g.rows; row += (int64_t)gridDim.x * kRows) {
-    const float mean = g.mean[row], rstd = g.rstd[row];
-    float h[CH][kRun], d[CH][kRun], a = 0.0f, b = 0.0f;
+  const int64_t step = (int64_t)gridDim.x * kRows;
+  int64_t row = (int64_t)blockIdx.x * kRows + (kRows > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / T) : 0);
+  constexpr bool kAhead = CH == 1;   // two runs a thread: no registers for it
+  GradRaw w[CH];
+  float mean = 0.0f, rstd = 0.0f;
+  if (kAhead && row < g.rows) {
+    load_grads<X, D, T, CH>(g, row, lane, w);
+    mean = g.mean[row];
+    rstd = g.rstd[row];
+  }
+  while (row < g.rows) {
+    if constexpr (!kAhead) {
+      load_grads<X, D, T, CH>(g, row, lane, w);
+      mean = g.mean[row];
+      rstd = g.rstd[row];
+    }
+    // the row stays as it was loaded, and is converted once more after the sums: fewer registers
+    GradRaw now[CH];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) load_grad<X>(g, row, (c * T + lane) * kRun, mean, rstd, h[c], d[c]);
+    for (int c = 0; c < CH; ++c) now[c] = w[c];
+    const float mu = mean, scale = rstd;
+    const int64_t next = row + step;
+    if (kAhead && next < g.rows) {
+      load_grads<X, D, T, CH>(g, next, lane, w);
+      mean = g.mean[next];
+      rstd = g.rstd[next];
+    }
+    float a = 0.0f, b = 0.0f;
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c) {
+      float h[kRun], d[kRun], ga[kRun];
+      values_of_grad<X, D>(g, now[c], (c * T + lane) * kRun, mu, scale, h, d);
+      if constexpr (!kHold) gamma_of(c, ga);
 #pragma unroll
       for (int i = 0; i < kRun; ++i) {
-        const float p = d[c][i] * ga[c][i];
+        if constexpr (kHold) ga[i] = held[i];
+        const float p = d[i] * ga[i];
         a += p;
-        b += p * h[c][i];
-        sg[c][i] += d[c][i] * h[c][i];
-        sb[c][i] += d[c][i];
+        b += p * h[i];
+        sg[c][i] += d[i] * h[i];
+        sb[c][i] += d[i];
       }
+    }
     row_sum2<T>(a, b, room);
     a /= count;
     b /= count;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) store_dx(g, row, (c * T + lane) * kRun, rstd, a, b, h[c], d[c], ga[c]);
+    for (int c = 0; c < CH; ++c) {
+      float h[kRun], d[kRun], ga[kRun];
+      if constexpr (CH > 1) {   // or both conversions become one, and kept
+        opaque(now[c].x);
+        opaque(now[c].d);
+      }
+      values_of_grad<X, D>(g, now[c], (c * T + lane) * kRun, mu, scale, h, d);
+      if constexpr (!kHold) gamma_of(c, ga);
+#pragma unroll
+      for (int i = 0; i < kRun; ++i)
+        if constexpr (kHold) ga[i] = held[i];
+      store_dx<D>(g, row, (c * T + lane) * kRun, scale, a, b, h, d, ga, now[c].r);
+    }
+    row = next;
   }
   if (g.sums) store_sums<T, kRows, CH>(g, sg, sb, stage);
 }
 
 // Rows that do not fit the registers: two passes a row; the sums go to the workspace as they grow
 // (a workgroup's own row of it, zeroed first).
-template <int X>
+template <int X, int D>
 __global__ __launch_bounds__(kMaxThreads) void norm_backward_long_kernel(NormArgs g) {
   constexpr int T = kMaxThreads;
   __shared__ float room[2 * T / kWave];
@@ -314,7 +416,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_long_kernel(NormArg
     float h[kRun], d[kRun], ga[kRun], a = 0.0f, b = 0.0f;
     for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
       const int n = g.cols - col;
-      load_grad<X>(g, row, col, mean, rstd, h, d);
+      values_of_grad<X, D>(g, load_grad<X, D, false>(g, row, col), col, mean, rstd, h, d);
       load_param(g.gamma, g.param_type, col, n, 1.0f, ga);
 #pragma unroll
       for (int i = 0; i < kRun; ++i) {
@@ -338,28 +440,11 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_long_kernel(NormArg
     a /= count;
     b /= count;
     for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
-      load_grad<X>(g, row, col, mean, rstd, h, d);
+      const GradRaw w = load_grad<X, D, false>(g, row, col);
+      values_of_grad<X, D>(g, w, col, mean, rstd, h, d);
       load_param(g.gamma, g.param_type, col, g.cols - col, 1.0f, ga);
-      store_dx(g, row, col, rstd, a, b, h, d, ga);
+      store_dx<D>(g, row, col, rstd, a, b, h, d, ga, w.r);
     }
-  }
-}
-
-// out[col] = sum over `parts` rows of 2 * cols sums; 64 columns a workgroup, 16 rows at a time.
-__global__ __launch_bounds__(1024) void norm_join_kernel(const float* sums, int parts, int cols, float* dgamma, float* dbeta) {
-  __shared__ float stage[16][64];
-  const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63), width = 2 * (int64_t)cols;
-  const int mine = threadIdx.x >> 6;
-  float s = 0.0f;
-  if (col < width)
-    for (int p = mine; p < parts; p += 16) s += sums[p * width + col];
-  stage[mine][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (mine == 0 && col < width) {
-    s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s += stage[i][threadIdx.x];
-    (col < cols ? dgamma[col] : dbeta[col - cols]) = s;
   }
 }
 
@@ -376,37 +461,44 @@ Shape forward_shape(int64_t cols) {
   if (cols <= 512) return {norm_forward_kernel<X, 64, 1>, 256, 4};
   if (cols <= 1024) return {norm_forward_kernel<X, 64, 2>, 256, 4};
   if (cols <= 2048) return {norm_forward_kernel<X, 64, 4>, 256, 4};
-  if (cols <= 4096) return {norm_forward_kernel<X, 256, 2>, 256, 1};
+  if (cols <= 4096) return {norm_forward_kernel<X, 64, 8>, 256, 4};
   if (cols <= 8192) return {norm_forward_kernel<X, 256, 4>, 256, 1};
   if (cols <= 16384) return {norm_forward_kernel<X, 512, 4>, 512, 1};
   if (cols <= 32768) return {norm_forward_kernel<X, 1024, 4>, 1024, 1};
   return {norm_forward_long_kernel<X>, kMaxThreads, 1};
 }
-template <int X>
-Shape backward_shape(int64_t cols) {
-  if (cols <= 512) return {norm_backward_kernel<X, 64, 1>, 256, 4};
-  if (cols <= 1024) return {norm_backward_kernel<X, 64, 2>, 256, 4};
-  if (cols <= 2048) return {norm_backward_kernel<X, 256, 1>, 256, 1};
-  if (cols <= 4096) return {norm_backward_kernel<X, 256, 2>, 256, 1};
-  if (cols <= 8192) return {norm_backward_kernel<X, 512, 2>, 512, 1};
-  if (cols <= 16384) return {norm_backward_kernel<X, 1024, 2>, 1024, 1};
-  return {norm_backward_long_kernel<X>, kMaxThreads, 1};
-}
-Shape shape_of(bool forward, int type, int64_t cols) {
+Shape forward_shape_of(int type, int64_t cols) {
   switch (type) {
-    case MOC_F32: return forward ? forward_shape<MOC_F32>(cols) : backward_shape<MOC_F32>(cols);
-    case MOC_F16: return forward ? forward_shape<MOC_F16>(cols) : backward_shape<MOC_F16>(cols);
-    case MOC_BF16: return forward ? forward_shape<MOC_BF16>(cols) : backward_shape<MOC_BF16>(cols);
-    case MOC_E4M3: return forward ? forward_shape<MOC_E4M3>(cols) : backward_shape<MOC_E4M3>(cols);
-    default: return forward ? forward_shape<MOC_I8>(cols) : backward_shape<MOC_I8>(cols);
+    case MOC_F32: return forward_shape<MOC_F32>(cols);
+    case MOC_F16: return forward_shape<MOC_F16>(cols);
+    case MOC_BF16: return forward_shape<MOC_BF16>(cols);
+    case MOC_E4M3: return forward_shape<MOC_E4M3>(cols);
+    default: return forward_shape<MOC_I8>(cols);
   }
 }
+template <int X, int D>
+Shape backward_shape(int64_t cols) {
+  if (cols <= 512) return {norm_backward_kernel<X, D, 64, 1>, 256, 4};
+  if (cols <= 2048) return {norm_backward_kernel<X, D, 256, 1>, 256, 1};
+  if (cols <= 4096) return {norm_backward_kernel<X, D, 512, 1>, 512, 1};
+  if (cols <= 8192) return {norm_backward_kernel<X, D, 1024, 1>, 1024, 1};
+  if (cols <= 16384) return {norm_backward_kernel<X, D, 1024, 2>, 1024, 1};
+  return {norm_backward_long_kernel<X, D>, kMaxThreads, 1};
+}
+// x of dy's type, or a checkpoint
+template <int D>
+Shape backward_shape_of(int type, int64_t cols) {
+  return type == MOC_E4M3 ? backward_shape<MOC_E4M3, D>(cols) : type == MOC_I8 ? backward_shape<MOC_I8, D>(cols) : backward_shape<D, D>(cols);
+}
+Shape backward_shape_of(int type, int dy_type, int64_t cols) {
+  return dy_type == MOC_BF16 ? backward_shape_of<MOC_BF16>(type, cols) : dy_type == MOC_F16 ? backward_shape_of<MOC_F16>(type, cols) : backward_shape_of<MOC_F32>(type, cols);
+}
 
-// Workgroups of the backward pass: as many rows of sums as the card needs to be full of work, no more
-// (each is written and read again).
+// Workgroups of the backward pass: what the compute units hold at a time, no more (the sums of each are
+// written and read again).
 int64_t backward_groups(int64_t rows, int64_t cols, int units) {
-  const Shape s = shape_of(false, MOC_BF16, cols);   // rows and threads do not depend on the type
-  const int64_t wanted = (int64_t)units * (2048 / s.threads > 4 ? 4 : 2048 / s.threads), there = (rows + s.rows - 1) / s.rows;
+  const Shape s = backward_shape<MOC_BF16, MOC_BF16>(cols);   // rows and threads do not depend on the types
+  const int64_t wanted = (int64_t)units * (kMaxThreads / s.threads), there = (rows + s.rows - 1) / s.rows;
   return there < wanted ? there : wanted;
 }
 
@@ -434,7 +526,7 @@ int moc_norm_forward(int64_t rows, int64_t cols, const moc_matrix* x, const void
     g.most = most_kept(kept->type, y->type);
   }
   g.rows = rows; g.cols = (int)cols;
-  const Shape s = shape_of(true, x->type, cols);
+  const Shape s = forward_shape_of(x->type, cols);
   hipLaunchKernelGGL(s.kern, grid_of((rows + s.rows - 1) / s.rows), dim3(s.threads), 0, static_cast<hipStream_t>(hip_stream), g);
   MOC_HIP(hipGetLastError());
   return MOC_OK;
@@ -454,6 +546,7 @@ int moc_norm_backward(int64_t rows, int64_t cols, const moc_matrix* dy, const mo
   if (!sizes_ok(rows, cols) || cols < 1) return MOC_EINVAL;
   if (!matrix_ok(dy, rows, cols, true, false) || !matrix_ok(x, rows, cols, true, true) || !matrix_ok(dx, rows, cols, true, false)) return MOC_EINVAL;
   if ((residual && !matrix_ok(residual, rows, cols, true, false)) || !params_ok(gamma, param_type)) return MOC_EINVAL;
+  if (dx->type != dy->type || (residual && residual->type != dy->type) || (is_value(x->type) && x->type != dy->type)) return MOC_EINVAL;
   if ((dgamma == nullptr) != (dbeta == nullptr) || !aligned_to(dgamma, 4) || !aligned_to(dbeta, 4)) return MOC_EINVAL;
   if (rows > 0 && (!mean || !rstd || !aligned_to(mean, 4) || !aligned_to(rstd, 4))) return MOC_EINVAL;
   if (rows == 0 && !dgamma) return MOC_OK;
@@ -468,20 +561,26 @@ int moc_norm_backward(int64_t rows, int64_t cols, const moc_matrix* dy, const mo
     g.x = x->data; g.x_scales = x->scales; g.x_stride = x->stride; g.x_scale_stride = x->scale_stride;
     g.gamma = gamma; g.param_type = param_type;
     g.mean = const_cast<float*>(mean); g.rstd = const_cast<float*>(rstd);
-    g.y = dx->data; g.y_type = dx->type; g.y_stride = dx->stride;
-    g.dy = dy->data; g.dy_type = dy->type; g.dy_stride = dy->stride;
+    g.y = dx->data; g.y_stride = dx->stride;
+    g.dy = dy->data; g.dy_stride = dy->stride;
     if (residual) {
-      g.residual = residual->data; g.residual_type = residual->type; g.residual_stride = residual->stride;
+      g.residual = residual->data; g.residual_stride = residual->stride;
     }
     g.sums = dgamma ? static_cast<float*>(work) : nullptr;
     g.rows = rows; g.cols = (int)cols;
-    const Shape s = shape_of(false, x->type, cols);
+    const Shape s = backward_shape_of(x->type, dy->type, cols);
     hipLaunchKernelGGL(s.kern, dim3((unsigned)groups), dim3(s.threads), 0, stream, g);
     MOC_HIP(hipGetLastError());
   }
   if (dgamma) {
-    hipLaunchKernelGGL(norm_join_kernel, dim3((unsigned)((2 * cols + 63) / 64)), dim3(1024), 0, stream, static_cast<const float*>(work), (int)groups, (int)cols, dgamma, dbeta);
-    MOC_HIP(hipGetLastError());
+    // the sums of a workgroup are dgamma's and dbeta's one after the other, and so they may be wanted
+    const float* const sums = static_cast<const float*>(work);
+    const bool together = dbeta == dgamma + cols;
+    for (int i = 0; i < (together ? 1 : 2); ++i) {
+      const int64_t wide = together ? 2 * cols : cols;
+      hipLaunchKernelGGL(join_sums_kernel, dim3((unsigned)((wide + 63) / 64)), dim3(1024), 0, stream, sums + i * cols, (int)groups, wide, 2 * cols, i ? dbeta : dgamma);
+      MOC_HIP(hipGetLastError());
+    }
   }
   return MOC_OK;
 }

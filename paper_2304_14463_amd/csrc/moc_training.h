@@ -90,10 +90,13 @@ __device__ __forceinline__ void decode_run(uint2 c, float scale, float (&v)[kRun
       v[4 * h + 2] = hi[0] * scale;
       v[4 * h + 3] = hi[1] * scale;
     } else {
+      const uint32_t u = w[h] ^ 0x80808080u;   // code + 128: a byte of it is converted in one instruction
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int code = (int)(w[h] << (24 - 8 * i)) >> 24;
-        v[4 * h + i] = code == -128 ? bits_float(0x7FC00000u) : (float)code * scale;
+      for (int i = 0; i < 4; ++i) v[4 * h + i] = ((float)(u >> (8 * i) & 0xFF) - 128.0f) * scale;
+      if (((u - 0x01010101u) & ~u & 0x80808080u) != 0) {   // a byte is 0: a code is NaN's
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if ((u >> (8 * i) & 0xFF) == 0) v[4 * h + i] = bits_float(0x7FC00000u);
       }
     }
   }
@@ -216,32 +219,153 @@ __device__ __forceinline__ void keep_any(int fmt, const float (&v)[kRun], int64_
 
 // exp2 and the reciprocal are the hardware's (1 ulp each): what is left of that after the rounding to
 // the output's type is below 2^-20 of a value.
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f)); }
+__device__ __forceinline__ float over_one_plus(float u, float e) { return u * __builtin_amdgcn_rcpf(1.0f + e); }
+__device__ __forceinline__ float exp_minus(float z) { return __builtin_amdgcn_exp2f(z * -1.4426950408889634f); }
 
 constexpr float kGelu1 = 1.5957691216057308f;            // 2 sqrt(2 / pi)
 constexpr float kGelu3 = 1.5957691216057308f * 0.044715f;
+constexpr float kLog2e = 1.4426950408889634f;
 
-__device__ __forceinline__ float act_of(int act, float u) {
-  if (act == MOC_ACT_RELU) return u <= 0.0f ? 0.0f : u;
-  if (act == MOC_ACT_GELU) return u * sigmoid(u * (kGelu1 + kGelu3 * u * u));
-  if (act == MOC_ACT_SILU) return u * sigmoid(u);
-  return u;
+__device__ __forceinline__ void act_run(int act, float (&v)[kRun]) {
+  if (act == MOC_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = v[i] <= 0.0f ? 0.0f : v[i];
+  } else if (act == MOC_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = over_one_plus(v[i], __builtin_amdgcn_exp2f(v[i] * __builtin_fmaf(v[i] * v[i], -kLog2e * kGelu3, -kLog2e * kGelu1)));
+  } else if (act == MOC_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = over_one_plus(v[i], exp_minus(v[i]));
+  }
 }
 
 // d times the activation's derivative at u.
-__device__ __forceinline__ float times_slope(int act, float d, float u) {
-  if (act == MOC_ACT_RELU) return u <= 0.0f ? 0.0f : u > 0.0f ? d : bits_float(0x7FC00000u);
-  if (act == MOC_ACT_GELU) {
-    // beyond +-16 the derivative is 0 or 1 in 32 bits; the squares of larger arguments would overflow
-    const float c = u < -16.0f ? -16.0f : u > 16.0f ? 16.0f : u;   // keeps a NaN
-    const float s = sigmoid(c * (kGelu1 + kGelu3 * c * c));
-    return d * (s + c * s * (1.0f - s) * (kGelu1 + 3.0f * kGelu3 * c * c));
+__device__ __forceinline__ void slope_run(int act, float (&d)[kRun], const float (&u)[kRun]) {
+  if (act == MOC_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) d[i] = u[i] <= 0.0f ? 0.0f : u[i] > 0.0f ? d[i] : bits_float(0x7FC00000u);
+  } else if (act == MOC_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      // beyond +-16 the derivative is 0 or 1 in 32 bits; the squares of larger arguments would overflow
+      const float c = u[i] < -16.0f ? -16.0f : u[i] > 16.0f ? 16.0f : u[i];   // keeps a NaN
+      const float q = c * c, s = over_one_plus(1.0f, __builtin_amdgcn_exp2f(c * __builtin_fmaf(q, -kLog2e * kGelu3, -kLog2e * kGelu1)));
+      d[i] *= __builtin_fmaf(c * s * (1.0f - s), __builtin_fmaf(q, 3.0f * kGelu3, kGelu1), s);
+    }
+  } else if (act == MOC_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      const float s = over_one_plus(1.0f, exp_minus(u[i]));
+      d[i] *= s * __builtin_fmaf(u[i], 1.0f - s, 1.0f);
+    }
   }
-  if (act == MOC_ACT_SILU) {
-    const float s = sigmoid(u);
-    return d * (s * (1.0f + u * (1.0f - s)));
+}
+
+// ---- a run as it lies in memory -----------------------------------------------------------------
+
+// Loaded early, converted when it is used: codes and their scale, 16-bit values, or floats.
+using u32x4 = uint32_t __attribute__((ext_vector_type(4)));
+struct Raw {
+  u32x4 a, b;
+  uint32_t scale;
+};
+
+template <int TYPE>
+__device__ __forceinline__ Raw load_raw(const void* row, const uint8_t* scales, int col, int n) {
+  Raw x = {};
+  if constexpr (TYPE == MOC_E4M3 || TYPE == MOC_I8) {
+    if (n <= 0) return x;
+    const uint2 c = load_codes(static_cast<const uint8_t*>(row) + col, n);
+    x.a[0] = c.x;
+    x.a[1] = c.y;
+    x.scale = scales[col / MOC_BLOCK];
+  } else if constexpr (TYPE == MOC_F32) {
+    const float* f = static_cast<const float*>(row) + col;
+    if (n >= kRun) {
+      __builtin_memcpy(&x.a, f, 16);
+      __builtin_memcpy(&x.b, f + 4, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kRun - 1; ++i)
+        if (i < n) (i < 4 ? x.a : x.b)[i & 3] = float_bits(f[i]);
+    }
+  } else {
+    const uint16_t* h = static_cast<const uint16_t*>(row) + col;
+    if (n >= kRun) {
+      __builtin_memcpy(&x.a, h, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kRun - 1; ++i)
+        if (i < n) x.a[i >> 1] |= (uint32_t)h[i] << (16 * (i & 1));
+    }
   }
-  return d;
+  return x;
+}
+
+// Where every run is whole (a multiple of eight columns): no branch, so that many are under way at once.
+// Beyond the row the last run is read, and not used.
+template <int TYPE>
+__device__ __forceinline__ Raw load_raw_whole(const void* row, const uint8_t* scales, int col, int cols) {
+  return load_raw<TYPE>(row, scales, min(col, cols - kRun), kRun);
+}
+
+template <int TYPE>
+__device__ __forceinline__ void values_of(const Raw& x, float (&v)[kRun]) {
+  if constexpr (TYPE == MOC_E4M3 || TYPE == MOC_I8) {
+    decode_run<TYPE>(uint2{x.a[0], x.a[1]}, scale_of((uint8_t)x.scale), v);
+  } else if constexpr (TYPE == MOC_F32) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = bits_float(i < 4 ? x.a[i & 3] : x.b[i & 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      const uint16_t h = (uint16_t)(x.a[i >> 1] >> (16 * (i & 1)));
+      v[i] = TYPE == MOC_BF16 ? bits_float((uint32_t)h << 16) : (float)__builtin_bit_cast(_Float16, h);
+    }
+  }
+}
+
+// The same with the type known at run time only (uniform over the wave).
+__device__ __forceinline__ Raw load_raw_any(int type, const void* row, const uint8_t* scales, int col, int n) {
+  if (type == MOC_BF16 || type == MOC_F16) return load_raw<MOC_BF16>(row, scales, col, n);
+  if (type == MOC_F32) return load_raw<MOC_F32>(row, scales, col, n);
+  return load_raw<MOC_E4M3>(row, scales, col, n);
+}
+__device__ __forceinline__ void values_of_any(int type, const Raw& x, float (&v)[kRun]) {
+  if (type == MOC_BF16) values_of<MOC_BF16>(x, v);
+  else if (type == MOC_F16) values_of<MOC_F16>(x, v);
+  else if (type == MOC_F32) values_of<MOC_F32>(x, v);
+  else if (type == MOC_E4M3) values_of<MOC_E4M3>(x, v);
+  else values_of<MOC_I8>(x, v);
+}
+
+// ---- sums over parts ----------------------------------------------------------------------------
+
+// out[col] = sum over `parts` rows of `width` floats, `stride` apart, in one order: 64 columns a workgroup, a wave every
+// sixteenth row, four of them under way.
+__global__ __launch_bounds__(1024) void join_sums_kernel(const float* sums, int parts, int64_t width, int64_t stride, float* out) {
+  __shared__ float stage[16][64];
+  const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  const int mine = threadIdx.x >> 6;
+  float s = 0.0f;
+  if (col < width) {
+    int p = mine;
+    for (; p + 48 < parts; p += 64) {
+      float v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = sums[(p + 16 * i) * stride + col];
+      s += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    for (; p < parts; p += 16) s += sums[p * stride + col];
+  }
+  stage[mine][threadIdx.x & 63] = s;
+  __syncthreads();
+  if (mine == 0 && col < width) {
+    s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += stage[i][threadIdx.x];
+    out[col] = s;
+  }
 }
 
 // ---- grids --------------------------------------------------------------------------------------
