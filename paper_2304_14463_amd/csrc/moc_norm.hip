@@ -2,10 +2,10 @@
 //
 // Bound by memory: every value is read once and written once.  T threads take a row and hold it in
 // registers, CH runs of eight values each, so the variance is that of the differences from the mean
-// and nothing is read again; rows longer than the registers hold are read again from cache.
-// Forward: a wave a row up to 4096 columns (no barrier), then the fewest threads that hold it.
-// Backward: every workgroup goes over many rows and keeps its columns' two sums in registers; they
-// meet in the workspace, one row of sums a workgroup, and a second kernel adds those in their order.
+// and nothing is read again; rows longer than 16384 columns are read again from cache.  A wave a row
+// up to 512 columns (no barrier), then the fewest threads that hold it.  Workgroups go over many rows:
+// gamma and beta stay in registers, and in the backward pass so do a column's two sums; they meet in
+// the workspace, one row of sums a workgroup, and a second kernel adds those in their order.
 #include "moc_training.h"
 
 namespace {
@@ -51,32 +51,41 @@ __device__ __forceinline__ float wave_sum(float a) {
   return bits_float((uint32_t)__builtin_amdgcn_readlane((int)float_bits(a), kWave - 1));
 }
 
-// Sums over the T threads that share a row, in all of them.  `room`: 2 x T / 64 floats of their own.
-// Called by whole workgroups only where T > 64.
-template <int T>
-__device__ __forceinline__ void row_sum2(float& a, float& b, float* room) {
-  a = wave_sum(a);
-  b = wave_sum(b);
-  if constexpr (T > kWave) {
-    constexpr int W = T / kWave;
-    const int wave = (threadIdx.x % T) / kWave;
-    __syncthreads();   // the sums before these have been read
-    if (threadIdx.x % kWave == 0) {
-      room[2 * wave] = a;
-      room[2 * wave + 1] = b;
+// The sum over the first W lanes, a power of two up to 16, in all lanes.
+template <int W>
+__device__ __forceinline__ float first_sum(float a) {
+  if constexpr (W > 1) a = add_shifted<0x111, 0xF>(a);
+  if constexpr (W > 2) a = add_shifted<0x112, 0xF>(a);
+  if constexpr (W > 4) a = add_shifted<0x114, 0xF>(a);
+  if constexpr (W > 8) a = add_shifted<0x118, 0xF>(a);
+  return bits_float((uint32_t)__builtin_amdgcn_readlane((int)float_bits(a), W - 1));
+}
+
+// Sums over the T threads that share a row, N of them at a time, in all of the threads.  `room`: two
+// halves of N x T / 64 floats, used in turn, so that one barrier does: what was written two sums ago
+// has been read when all waves have come to the sums in between.  Called by whole workgroups where T > 64.
+template <int T, int N>
+struct RowSums {
+  static constexpr int kWaves = T / kWave, kRoom = 2 * N * kWaves;
+  float* room;
+  int half = 0;
+  __device__ __forceinline__ void operator()(float (&a)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) a[i] = wave_sum(a[i]);
+    if constexpr (T > kWave) {
+      float* const mine = room + half * N * kWaves;
+      const int lane = threadIdx.x % kWave;
+      if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) mine[i * kWaves + (threadIdx.x % T) / kWave] = a[i];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < N; ++i) a[i] = first_sum<kWaves>(mine[i * kWaves + lane % kWaves]);
+      half ^= 1;
     }
-    __syncthreads();
-    const int lane = threadIdx.x % kWave;
-    a = wave_sum(lane < W ? room[2 * lane] : 0.0f);
-    b = wave_sum(lane < W ? room[2 * lane + 1] : 0.0f);
   }
-}
-template <int T>
-__device__ __forceinline__ float row_sum(float a, float* room) {
-  float none = 0.0f;
-  row_sum2<T>(a, none, room);
-  return a;
-}
+};
 
 __device__ __forceinline__ void load_param(const void* p, int type, int col, int n, float other, float (&v)[kRun]) {
   if (p) {
@@ -101,68 +110,119 @@ __device__ __forceinline__ void load_x(const NormArgs& g, int64_t row, int col, 
 }
 __device__ __forceinline__ bool whole_runs(const NormArgs& g) { return g.cols % kRun == 0; }
 
+// 1 / sqrt(x), 1 ulp, subnormal arguments too.
+__device__ __forceinline__ float inverse_root(float x) {
+  const bool small = x < 0x1p-100f;
+  const float r = __builtin_amdgcn_rsqf(small ? x * 0x1p64f : x);
+  return small ? r * 0x1p32f : r;
+}
+
 // ---- forward ------------------------------------------------------------------------------------
 
 // y and its checkpoint of one run.
-__device__ __forceinline__ void finish_run(const NormArgs& g, int64_t row, int col, int n, float mean, float rstd, float (&v)[kRun]) {
-  float ga[kRun], be[kRun];
-  load_param(g.gamma, g.param_type, col, n, 1.0f, ga);
-  load_param(g.beta, g.param_type, col, n, 0.0f, be);
+__device__ __forceinline__ void finish_run(const NormArgs& g, int64_t row, int col, int n, float mean, float rstd, const float (&ga)[kRun], const float (&be)[kRun],
+                                           float (&v)[kRun]) {
 #pragma unroll
-  for (int i = 0; i < kRun; ++i) v[i] = i < n ? (v[i] - mean) * rstd * ga[i] + be[i] : 0.0f;
+  for (int i = 0; i < kRun; ++i) v[i] = (v[i] - mean) * rstd * ga[i] + be[i];
   if (n > 0) store_any(g.y_type, row_any(g.y, g.y_type, row, g.y_stride), col, n, v);
-  if (g.kept_type >= 0) keep_any(g.kept_type, v, col, n, g.most, g.codes + row * g.code_stride, g.scales + row * g.scale_stride);
+  if (g.kept_type < 0) return;
+  if (n < kRun) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) v[i] = i < n ? v[i] : 0.0f;
+  }
+  keep_any(g.kept_type, v, col, n, g.most, g.codes + row * g.code_stride, g.scales + row * g.scale_stride);
 }
 
 template <int X, int T, int CH>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormArgs g) {
-  constexpr int kRows = T < 256 ? 256 / T : 1;   // rows of a workgroup
+__device__ __forceinline__ void load_row(const NormArgs& g, int64_t row, int lane, Raw (&w)[CH]) {
+  const void* const x = row_of<X>(g.x, row, g.x_stride);
+  const uint8_t* const scales = g.x_scales + row * g.x_scale_stride;
+  if (whole_runs(g)) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) w[c] = load_raw_whole<X>(x, scales, (c * T + lane) * kRun, g.cols);
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) w[c] = load_raw<X>(x, scales, (c * T + lane) * kRun, g.cols - (c * T + lane) * kRun);
+  }
+}
+
+// Workgroups go over rows with gamma and beta in registers (from cache they would be four times the
+// bytes of a row), R rows at a time, whose sums are taken together, and the next R on their way.  16
+// waves a compute unit at least.
+template <int X, int T, int CH, int R>
+__global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_forward_kernel(NormArgs g) {
+  constexpr int kRows = T < 256 ? 256 / T : 1;   // groups of R rows of a workgroup at a time
   static_assert(T <= kWave || kRows == 1);
-  __shared__ float room[2 * T / kWave + 1];
+  using Sums = RowSums<T, R>;
+  __shared__ float room[Sums::kRoom];
+  Sums sums{room};
   const int lane = threadIdx.x % T;
-  const int64_t row = block_of() * kRows + threadIdx.x / T;
-  if (row >= g.rows) return;   // whole waves only, and whole workgroups where they share a row
-  float v[CH][kRun];
-  float s = 0.0f;
-  {
-    Raw w[CH];
-    const void* const x = row_of<X>(g.x, row, g.x_stride);
-    const uint8_t* const scales = g.x_scales + row * g.x_scale_stride;
-    if (whole_runs(g)) {
-#pragma unroll
-      for (int c = 0; c < CH; ++c) w[c] = load_raw_whole<X>(x, scales, (c * T + lane) * kRun, g.cols);
-    } else {
-#pragma unroll
-      for (int c = 0; c < CH; ++c) w[c] = load_raw<X>(x, scales, (c * T + lane) * kRun, g.cols - (c * T + lane) * kRun);
-    }
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      values_of<X>(w[c], v[c]);
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) s += (c * T + lane) * kRun < g.cols ? v[c][i] : 0.0f;
-    }
-  }
-  const float count = (float)g.cols;
-  const float mean = row_sum<T>(s, room) / count;
-  float q = 0.0f;
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int n = g.cols - (c * T + lane) * kRun;
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) {
-      const float d = v[c][i] - mean;
-      q += i < n ? d * d : 0.0f;
-    }
-  }
-  const float rstd = 1.0f / __builtin_sqrtf(row_sum<T>(q, room) / count + g.eps);
-  if (lane == 0) {
-    g.mean[row] = mean;
-    g.rstd[row] = rstd;
-  }
+  float ga[CH][kRun], be[CH][kRun];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int col = (c * T + lane) * kRun;
-    finish_run(g, row, col, g.cols - col, mean, rstd, v[c]);
+    load_param(g.gamma, g.param_type, min(col, g.cols - 1), g.cols - col, 1.0f, ga[c]);
+    load_param(g.beta, g.param_type, min(col, g.cols - 1), g.cols - col, 0.0f, be[c]);
+  }
+  const float part = 1.0f / (float)g.cols;
+  const bool whole = whole_runs(g);
+  const int64_t step = (int64_t)gridDim.x * kRows * R;
+  int64_t row = ((int64_t)blockIdx.x * kRows + (kRows > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / T) : 0)) * R;
+  Raw w[R][CH];
+  const auto load = [&](int64_t from) {   // beyond the last row it is read again
+#pragma unroll
+    for (int r = 0; r < R; ++r) load_row<X, T, CH>(g, min(from + r, g.rows - 1), lane, w[r]);
+  };
+  if (row < g.rows) load(row);
+  for (; row < g.rows; row += step) {
+    float v[R][CH][kRun], mean[R], rstd[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mean[r] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        values_of<X>(w[r][c], v[r][c]);
+        float s = 0.0f;   // 0 where a row ends inside a run
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) s += v[r][c][i];
+        mean[r] += (c * T + lane) * kRun < g.cols ? s : 0.0f;
+      }
+    }
+    load(row + step);
+    sums(mean);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      mean[r] /= (float)g.cols;   // a division, so that equal values leave no difference
+      rstd[r] = 0.0f;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int n = g.cols - (c * T + lane) * kRun;
+        float q = 0.0f;
+        if (whole) {
+#pragma unroll
+          for (int i = 0; i < kRun; ++i) q += (v[r][c][i] - mean[r]) * (v[r][c][i] - mean[r]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < kRun; ++i) q += i < n ? (v[r][c][i] - mean[r]) * (v[r][c][i] - mean[r]) : 0.0f;
+        }
+        rstd[r] += n > 0 ? q : 0.0f;
+      }
+    }
+    sums(rstd);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + r >= g.rows) break;
+      rstd[r] = inverse_root(rstd[r] * part + g.eps);
+      if (lane == 0) {
+        g.mean[row + r] = mean[r];
+        g.rstd[row + r] = rstd[r];
+      }
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int col = (c * T + lane) * kRun;
+        finish_run(g, row + r, col, g.cols - col, mean[r], rstd[r], ga[c], be[c], v[r][c]);
+      }
+    }
   }
 }
 
@@ -170,32 +230,39 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void norm_forward_kernel(NormArg
 template <int X>
 __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormArgs g) {
   constexpr int T = kMaxThreads;
-  __shared__ float room[2 * T / kWave];
-  const int64_t row = block_of();
-  if (row >= g.rows) return;
+  using Sums = RowSums<T, 1>;
+  __shared__ float room[Sums::kRoom];
+  Sums sums{room};
   const int blocks = (g.cols + MOC_BLOCK - 1) / MOC_BLOCK * MOC_BLOCK;   // quads stay together
-  float v[kRun], s = 0.0f;
-  for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
-    load_x<X>(g, row, col, g.cols - col, v);
+  for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
+    float v[kRun], s[1] = {0.0f};
+    for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
+      load_x<X>(g, row, col, g.cols - col, v);
 #pragma unroll
-    for (int i = 0; i < kRun; ++i) s += v[i];
-  }
-  const float count = (float)g.cols;
-  const float mean = row_sum<T>(s, room) / count;
-  float q = 0.0f;
-  for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
-    load_x<X>(g, row, col, g.cols - col, v);
+      for (int i = 0; i < kRun; ++i) s[0] += v[i];
+    }
+    const float count = (float)g.cols;
+    sums(s);
+    const float mean = s[0] / count;
+    float q[1] = {0.0f};
+    for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
+      load_x<X>(g, row, col, g.cols - col, v);
 #pragma unroll
-    for (int i = 0; i < kRun; ++i) q += i < g.cols - col ? (v[i] - mean) * (v[i] - mean) : 0.0f;
-  }
-  const float rstd = 1.0f / __builtin_sqrtf(row_sum<T>(q, room) / count + g.eps);
-  if (threadIdx.x == 0) {
-    g.mean[row] = mean;
-    g.rstd[row] = rstd;
-  }
-  for (int col = threadIdx.x * kRun; col < blocks; col += T * kRun) {
-    load_x<X>(g, row, min(col, g.cols - 1), g.cols - col, v);
-    finish_run(g, row, col, g.cols - col, mean, rstd, v);
+      for (int i = 0; i < kRun; ++i) q[0] += i < g.cols - col ? (v[i] - mean) * (v[i] - mean) : 0.0f;
+    }
+    sums(q);
+    const float rstd = 1.0f / __builtin_sqrtf(q[0] / count + g.eps);
+    if (threadIdx.x == 0) {
+      g.mean[row] = mean;
+      g.rstd[row] = rstd;
+    }
+    for (int col = threadIdx.x * kRun; col < blocks; col += T * kRun) {
+      float ga[kRun], be[kRun];
+      load_x<X>(g, row, min(col, g.cols - 1), g.cols - col, v);
+      load_param(g.gamma, g.param_type, min(col, g.cols - 1), g.cols - col, 1.0f, ga);
+      load_param(g.beta, g.param_type, min(col, g.cols - 1), g.cols - col, 0.0f, be);
+      finish_run(g, row, col, g.cols - col, mean, rstd, ga, be, v);
+    }
   }
 }
 
@@ -315,7 +382,9 @@ template <int X, int D, int T, int CH>
 __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(NormArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
   static_assert(T <= kWave || kRows == 1);
-  __shared__ float room[2 * T / kWave + 1];
+  using Sums = RowSums<T, 2>;
+  __shared__ float room[Sums::kRoom];
+  Sums sums{room};
   __shared__ float stage[kRows > 1 ? kRows * 16 * T : 1];
   const int lane = threadIdx.x % T;
   constexpr bool kHold = CH == 1;   // gamma, in registers; from cache where two runs leave none
@@ -330,7 +399,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(Nor
 #pragma unroll
     for (int i = 0; i < kRun; ++i) sg[c][i] = sb[c][i] = 0.0f;
   }
-  const float count = (float)g.cols;
+  const float part = 1.0f / (float)g.cols;
   const int64_t step = (int64_t)gridDim.x * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + (kRows > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / T) : 0);
   constexpr bool kAhead = CH == 1;   // two runs a thread: no registers for it
@@ -358,7 +427,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(Nor
       mean = g.mean[next];
       rstd = g.rstd[next];
     }
-    float a = 0.0f, b = 0.0f;
+    float m[2] = {0.0f, 0.0f};   // of p, of p * h
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float h[kRun], d[kRun], ga[kRun];
@@ -368,15 +437,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(Nor
       for (int i = 0; i < kRun; ++i) {
         if constexpr (kHold) ga[i] = held[i];
         const float p = d[i] * ga[i];
-        a += p;
-        b += p * h[i];
+        m[0] += p;
+        m[1] += p * h[i];
         sg[c][i] += d[i] * h[i];
         sb[c][i] += d[i];
       }
     }
-    row_sum2<T>(a, b, room);
-    a /= count;
-    b /= count;
+    sums(m);
+    const float a = m[0] * part, b = m[1] * part;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float h[kRun], d[kRun], ga[kRun];
@@ -401,7 +469,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(Nor
 template <int X, int D>
 __global__ __launch_bounds__(kMaxThreads) void norm_backward_long_kernel(NormArgs g) {
   constexpr int T = kMaxThreads;
-  __shared__ float room[2 * T / kWave];
+  using Sums = RowSums<T, 2>;
+  __shared__ float room[Sums::kRoom];
+  Sums over_row{room};
   float* const sums = g.sums ? g.sums + (int64_t)blockIdx.x * 2 * g.cols : nullptr;
   const float count = (float)g.cols;
   if (sums) {
@@ -413,15 +483,15 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_long_kernel(NormArg
   }
   for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
     const float mean = g.mean[row], rstd = g.rstd[row];
-    float h[kRun], d[kRun], ga[kRun], a = 0.0f, b = 0.0f;
+    float h[kRun], d[kRun], ga[kRun], m[2] = {0.0f, 0.0f};
     for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
       const int n = g.cols - col;
       values_of_grad<X, D>(g, load_grad<X, D, false>(g, row, col), col, mean, rstd, h, d);
       load_param(g.gamma, g.param_type, col, n, 1.0f, ga);
 #pragma unroll
       for (int i = 0; i < kRun; ++i) {
-        a += d[i] * ga[i];
-        b += d[i] * ga[i] * h[i];
+        m[0] += d[i] * ga[i];
+        m[1] += d[i] * ga[i] * h[i];
       }
       if (sums) {   // the same thread's columns in every row
         float s[kRun], t[kRun];
@@ -436,9 +506,8 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward_long_kernel(NormArg
         store_run<MOC_F32>(sums + g.cols, col, n, t);
       }
     }
-    row_sum2<T>(a, b, room);
-    a /= count;
-    b /= count;
+    over_row(m);
+    const float a = m[0] / count, b = m[1] / count;
     for (int col = threadIdx.x * kRun; col < g.cols; col += T * kRun) {
       const GradRaw w = load_grad<X, D, false>(g, row, col);
       values_of_grad<X, D>(g, w, col, mean, rstd, h, d);
@@ -458,13 +527,11 @@ struct Shape {
 
 template <int X>
 Shape forward_shape(int64_t cols) {
-  if (cols <= 512) return {norm_forward_kernel<X, 64, 1>, 256, 4};
-  if (cols <= 1024) return {norm_forward_kernel<X, 64, 2>, 256, 4};
-  if (cols <= 2048) return {norm_forward_kernel<X, 64, 4>, 256, 4};
-  if (cols <= 4096) return {norm_forward_kernel<X, 64, 8>, 256, 4};
-  if (cols <= 8192) return {norm_forward_kernel<X, 256, 4>, 256, 1};
-  if (cols <= 16384) return {norm_forward_kernel<X, 512, 4>, 512, 1};
-  if (cols <= 32768) return {norm_forward_kernel<X, 1024, 4>, 1024, 1};
+  if (cols <= 512) return {norm_forward_kernel<X, 64, 1, 2>, 256, 8};
+  if (cols <= 2048) return {norm_forward_kernel<X, 256, 1, 2>, 256, 2};
+  if (cols <= 4096) return {norm_forward_kernel<X, 512, 1, 2>, 512, 2};
+  if (cols <= 8192) return {norm_forward_kernel<X, 1024, 1, 2>, 1024, 2};
+  if (cols <= 16384) return {norm_forward_kernel<X, 1024, 2, 1>, 1024, 1};
   return {norm_forward_long_kernel<X>, kMaxThreads, 1};
 }
 Shape forward_shape_of(int type, int64_t cols) {
@@ -494,12 +561,14 @@ Shape backward_shape_of(int type, int dy_type, int64_t cols) {
   return dy_type == MOC_BF16 ? backward_shape_of<MOC_BF16>(type, cols) : dy_type == MOC_F16 ? backward_shape_of<MOC_F16>(type, cols) : backward_shape_of<MOC_F32>(type, cols);
 }
 
-// Workgroups of the backward pass: what the compute units hold at a time, no more (the sums of each are
-// written and read again).
-int64_t backward_groups(int64_t rows, int64_t cols, int units) {
-  const Shape s = backward_shape<MOC_BF16, MOC_BF16>(cols);   // rows and threads do not depend on the types
+// Workgroups: what the compute units hold at a time, no more (the backward pass writes the sums of each
+// and reads them again).
+int64_t groups_of(const Shape& s, int64_t rows, int units) {
   const int64_t wanted = (int64_t)units * (kMaxThreads / s.threads), there = (rows + s.rows - 1) / s.rows;
   return there < wanted ? there : wanted;
+}
+int64_t backward_groups(int64_t rows, int64_t cols, int units) {
+  return groups_of(backward_shape<MOC_BF16, MOC_BF16>(cols), rows, units);   // does not depend on the types
 }
 
 }  // namespace
@@ -513,6 +582,9 @@ int moc_norm_forward(int64_t rows, int64_t cols, const moc_matrix* x, const void
   if (!params_ok(gamma, param_type) || !params_ok(beta, param_type)) return MOC_EINVAL;
   if (rows == 0) return MOC_OK;
   if (!mean || !rstd || !aligned_to(mean, 4) || !aligned_to(rstd, 4)) return MOC_EINVAL;
+  int units = 0;
+  const int rc = moc_compute_units(&units);
+  if (rc != MOC_OK) return rc;
   NormArgs g = {};
   g.x = x->data; g.x_scales = x->scales; g.x_stride = x->stride; g.x_scale_stride = x->scale_stride;
   g.gamma = gamma; g.beta = beta; g.param_type = param_type; g.eps = eps;
@@ -527,7 +599,7 @@ int moc_norm_forward(int64_t rows, int64_t cols, const moc_matrix* x, const void
   }
   g.rows = rows; g.cols = (int)cols;
   const Shape s = forward_shape_of(x->type, cols);
-  hipLaunchKernelGGL(s.kern, grid_of((rows + s.rows - 1) / s.rows), dim3(s.threads), 0, static_cast<hipStream_t>(hip_stream), g);
+  hipLaunchKernelGGL(s.kern, dim3((unsigned)groups_of(s, rows, units)), dim3(s.threads), 0, static_cast<hipStream_t>(hip_stream), g);
   MOC_HIP(hipGetLastError());
   return MOC_OK;
 }

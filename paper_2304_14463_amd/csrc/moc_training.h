@@ -143,15 +143,27 @@ inline float most_kept(int fmt, int type) {
   return (fmt == MOC_E4M3 ? 1.875f : 1.96875f) * top;
 }
 
-// The largest finite magnitude of a run, `most` at most.
-__device__ __forceinline__ float run_peak(const float (&v)[kRun], float most) {
-  float a = 0.0f;
+// Whether a run has values that are not finite or above `most`; its largest finite magnitude, `most` at
+// most.  Both are rare: the maximum takes no notice of NaN, and what is not finite times 0 is NaN.
+__device__ __forceinline__ bool run_peak(const float (&v)[kRun], float most, float& peak) {
+  float a = 0.0f, odd = 0.0f;
 #pragma unroll
   for (int i = 0; i < kRun; ++i) {
-    const float m = __builtin_fabsf(v[i]);
-    a = m < kInf && m > a ? m : a;   // a NaN compares false
+    a = fmaxf(a, __builtin_fabsf(v[i]));
+    odd = __builtin_fmaf(v[i], 0.0f, odd);
   }
-  return fminf(a, most);
+  const bool special = odd != odd || a > most;
+  if (special) {
+    a = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+      const float m = __builtin_fabsf(v[i]);
+      a = m < kInf && m > a ? m : a;
+    }
+    a = fminf(a, most);
+  }
+  peak = a;
+  return special;
 }
 
 // The exponent of a block's scale from its peak: the peak's own exponent less the format's, one more
@@ -163,35 +175,33 @@ __device__ __forceinline__ int scale_exp(float peak) {
   return max(k, kMinExp);
 }
 
+// Four finite values within the format's range, scaled, to four codes.
 template <int FMT>
-__device__ __forceinline__ uint2 encode_run(const float (&v)[kRun], int k, float most) {
-  const float inv = bits_float((uint32_t)(127 - k) << 23);
-  uint32_t w[2];
+__device__ __forceinline__ uint32_t encode_four(const float* q) {
+  if constexpr (FMT == MOC_E4M3) {
+    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], r, true);
+  } else {
+    // 1.5 * 2^23 rounds to whole numbers, ties to even, and leaves them in the lowest byte
+    uint32_t b[4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float q[4];
-    bool good[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = v[4 * h + i];
-      good[i] = __builtin_fabsf(x) < kInf;
-      q[i] = fminf(fmaxf(x, -most), most) * inv;
-    }
-    if constexpr (FMT == MOC_E4M3) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) q[i] = good[i] ? q[i] : kInf;   // has no code of its own: 0x7F (a NaN would be 0xFF)
-      int r = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
-      w[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], r, true);
-    } else {
-      w[h] = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int code = good[i] ? (int)__builtin_rintf(q[i]) : -128;
-        w[h] |= ((uint32_t)code & 0xFFu) << (8 * i);
-      }
-    }
+    for (int i = 0; i < 4; ++i) b[i] = float_bits(q[i] + 12582912.0f);
+    const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000C0Cu);
+    return lo | hi;
   }
-  return uint2{w[0], w[1]};
+}
+
+template <int FMT>
+__device__ __forceinline__ uint2 encode_run(const float (&v)[kRun], int k, float most, bool special) {
+  const float inv = bits_float((uint32_t)(127 - k) << 23);
+  float q[kRun];
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) q[i] = v[i] * inv;
+  if (special) {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) q[i] = __builtin_fabsf(v[i]) < kInf ? fminf(fmaxf(v[i], -most), most) * inv : FMT == MOC_E4M3 ? kInf : -128.0f;   // infinity has no code of its own: 0x7F
+  }
+  return uint2{encode_four<FMT>(q), encode_four<FMT>(q + 4)};
 }
 
 // The maximum over the quad of lanes that holds a block's 32 columns.
@@ -204,9 +214,11 @@ __device__ __forceinline__ float quad_max(float a) {
 // row with n <= 0 and values of 0.
 template <int FMT>
 __device__ __forceinline__ void keep_run(const float (&v)[kRun], int64_t col, int n, float most, uint8_t* codes, uint8_t* scales) {
-  const int k = scale_exp<FMT>(quad_max(run_peak(v, most)));
+  float peak;
+  const bool special = run_peak(v, most, peak);
+  const int k = scale_exp<FMT>(quad_max(peak));
   if (n > 0) {
-    store_codes(codes + col, n, encode_run<FMT>(v, k, most));
+    store_codes(codes + col, n, encode_run<FMT>(v, k, most, special));
     if ((col & (MOC_BLOCK - 1)) == 0) scales[col / MOC_BLOCK] = (uint8_t)(k + 127);
   }
 }
@@ -343,7 +355,7 @@ __device__ __forceinline__ void values_of_any(int type, const Raw& x, float (&v)
 
 // out[col] = sum over `parts` rows of `width` floats, `stride` apart, in one order: 64 columns a workgroup, a wave every
 // sixteenth row, four of them under way.
-__global__ __launch_bounds__(1024) void join_sums_kernel(const float* sums, int parts, int64_t width, int64_t stride, float* out) {
+[[maybe_unused]] __global__ __launch_bounds__(1024) void join_sums_kernel(const float* sums, int parts, int64_t width, int64_t stride, float* out) {
   __shared__ float stage[16][64];
   const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
   const int mine = threadIdx.x >> 6;
