@@ -2,7 +2,7 @@
 
   paper_2304_14463_amd/libmoccasin_hip.so          the C-ABI evaluator (include/moccasin.h)
   paper_2304_14463_amd/inputs/libmoc_inputs_hip.so device twin of the candidate generator
-  paper_2304_14463_amd/_candidates.so              the native part of the Python binding (host code)
+  paper_2304_14463_amd/_candidates.so, _training.so the native parts of the Python bindings (host code)
 
 hipcc cross-compiles without a GPU.  Run as `python -m paper_2304_14463_amd.build`.
 """
@@ -18,6 +18,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libmoccasin_hip.so")
 BINDING = os.path.join(PKG, "_candidates.so")
+TRAINING = os.path.join(PKG, "_training.so")
 INPUTS_LIB = os.path.join(PKG, "inputs", "libmoc_inputs_hip.so")
 
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-shared", "-fPIC",
@@ -70,7 +71,7 @@ def build_inputs():
     return _hipcc(INPUTS_LIB, srcs)
 
 
-def build_binding():
+def build_binding(out=BINDING, source="candidates.cpp"):
     """Host code against torch's headers: g++, no HIP."""
     import sysconfig
 
@@ -78,13 +79,13 @@ def build_binding():
     from torch.utils.cpp_extension import include_paths
     lib_dir = os.path.join(os.path.dirname(torch.__file__), "lib")
     _run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
-          "-I", os.path.join(ROOT, "include"), *[f"-I{p}" for p in include_paths()], f"-I{sysconfig.get_paths()['include']}", "-o", BINDING,
-          os.path.join(PKG, "binding", "candidates.cpp"), f"-L{lib_dir}", f"-Wl,-rpath,{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-lc10"])
-    return BINDING
+          "-I", os.path.join(ROOT, "include"), *[f"-I{p}" for p in include_paths()], f"-I{sysconfig.get_paths()['include']}", "-o", out,
+          os.path.join(PKG, "binding", source), f"-L{lib_dir}", f"-Wl,-rpath,{lib_dir}", "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    return out
 
 
 def build_all():
-    return [build_binding(), build_library(), build_inputs()]
+    return [build_binding(), build_binding(TRAINING, "training.cpp"), build_library(), build_inputs()]
 
 
 if __name__ == "__main__":

@@ -1,9 +1,9 @@
 """Python binding of the operators that a rematerialisation plan is run with (C ABI in
 include/moccasin_training.h, in the same library as the evaluator).
 
-Argument marshalling only, as in `moccasin`: tensors are checked and turned into descriptors, results
-and workspaces are torch tensors, everything is asynchronous on `stream` (default: torch's current
-stream).  Matrices are two-dimensional CUDA tensors whose values of a row lie next to each other; rows
+Argument marshalling only, as in `moccasin`: tensors are checked and turned into descriptors (natively,
+binding/training.cpp), results and workspaces are torch tensors, everything is asynchronous on `stream`
+(default: torch's current stream).  Matrices are two-dimensional CUDA tensors whose values of a row lie next to each other; rows
 may be any distance apart.  There is no CPU fallback: a missing library or GPU raises.
 
 A `Checkpoint` is an activation kept in 8 bits: a byte a value and a scale for 32 columns of a row.
@@ -51,13 +51,12 @@ class Checkpoint:
 
 
 _lib = None
-_types = None
-_work_bytes = {}
+_native = None
 
 
 def lib():
     """The evaluator's library, with these operators in it."""
-    global _lib, _types
+    global _lib
     if _lib is None:
         L = moc.lib()
         version = L.moc_training_version() if hasattr(L, "moc_training_version") else 0
@@ -75,65 +74,26 @@ def lib():
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
         for name, args in (("moc_norm_backward_work", [I64, I64]), ("moc_linear_work", [I64, I64, I64])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, I64
-        torch = moc._tc()
-        _types = {torch.float32: MOC_F32, torch.float16: MOC_F16, torch.bfloat16: MOC_BF16}
         _lib = L
     return _lib
 
 
-def _type(dtype, what):
-    t = _types.get(dtype)
-    if t is None:
-        raise ValueError(f"{what}: float32, float16 or bfloat16 expected, got {dtype}")
-    return t
-
-
-def _matrix(x, what, rows=None, cols=None):
-    """moc_matrix of a tensor or a checkpoint, its sizes checked against those given"""
-    if type(x) is Checkpoint:
-        codes, scales = x.codes, x.scales
-        if not (codes.is_cuda and scales.is_cuda and codes.device == scales.device and codes.dim() == scales.dim() == 2):
-            raise ValueError(f"{what}: a checkpoint's codes and scales must be two-dimensional CUDA tensors on one device")
-        n, c = codes.shape
-        blocks = -(-c // BLOCK)
-        if codes.element_size() != 1 or scales.element_size() != 1 or scales.shape != (n, blocks):
-            raise ValueError(f"{what}: a checkpoint of {n} x {c} has bytes as codes and {n} x {blocks} bytes as scales")
-        stride, scale_stride = _stride(codes, n, c, what), _stride(scales, n, blocks, what)
-        m = Matrix(codes.data_ptr(), scales.data_ptr(), stride, scale_stride, FORMATS[x.fmt], 0)
-    else:
-        if not (x.is_cuda and x.dim() == 2):
-            raise ValueError(f"{what}: a two-dimensional CUDA tensor or a Checkpoint expected")
-        n, c = x.shape
-        m = Matrix(x.data_ptr(), None, _stride(x, n, c, what), 0, _type(x.dtype, what), 0)
-    if (rows is not None and n != rows) or (cols is not None and c != cols):
-        raise ValueError(f"{what}: {rows} x {cols} expected, got {n} x {c}")
-    return m
-
-
-def _stride(x, rows, cols, what):
-    row, col = x.stride()
-    if cols > 1 and col != 1:
-        raise ValueError(f"{what}: the values of a row must lie next to each other")
-    if rows <= 1:
-        return max(cols, 1)
-    if row < cols:
-        raise ValueError(f"{what}: rows must not overlap")
-    return max(row, 1)
-
-
-def _param(p, n, what):
-    """(address, type) of a vector of parameters, (None, 0) for none"""
-    if p is None:
-        return None, 0
-    if not (p.is_cuda and p.is_contiguous() and p.numel() == n):
-        raise ValueError(f"{what}: a contiguous CUDA tensor of {n} values expected")
-    return p.data_ptr(), _type(p.dtype, what)
-
-
-def _floats(p, n, what):
-    if not (p.is_cuda and p.is_contiguous() and p.numel() == n and p.dtype == moc._tc().float32):
-        raise ValueError(f"{what}: a contiguous float32 CUDA tensor of {n} values expected")
-    return p.data_ptr()
+def _bound():
+    """The native part of the binding (binding/training.cpp), loaded on first use: it needs torch."""
+    global _native
+    if _native is None:
+        L = lib()
+        moc._tc()
+        try:
+            from . import _training as native   # built with the library
+        except ImportError as err:
+            raise RuntimeError(f"{moc.LIB_PATH}: the binding's native part does not load ({err}); run python -m paper_2304_14463_amd.build") from err
+        if getattr(native, "training_version", None) != MOC_TRAINING_VERSION:
+            raise RuntimeError(f"{native.__file__}: version {getattr(native, 'training_version', None)} of the training operators, expected "
+                               f"{MOC_TRAINING_VERSION}; run python -m paper_2304_14463_amd.build")
+        native.bind(Checkpoint, moc._stream_handle, {name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in EXPORTS})
+        _native = native
+    return _native
 
 
 def _act(act):
@@ -142,14 +102,13 @@ def _act(act):
     return ACTS[act]
 
 
-def _same_device(first, *others):
-    for x in others:
-        if x is not None and (x.codes if type(x) is Checkpoint else x).device != first.device:
-            raise ValueError("all arguments must be on one device")
-
-
-def _device_of(x):
-    return (x.codes if type(x) is Checkpoint else x).device
+def _call(name, stream, *args):
+    """(code, results..) of a native call; what it allocates belongs to `stream`."""
+    call = getattr(_native or _bound(), name)
+    if stream is None:
+        return call(*args, None)
+    with moc._on(stream):
+        return call(*args, stream.cuda_stream)
 
 
 def empty_checkpoint(rows, cols, fmt, device):
@@ -158,55 +117,17 @@ def empty_checkpoint(rows, cols, fmt, device):
     return Checkpoint(torch.empty((rows, cols), dtype=torch.uint8, device=device), torch.empty((rows, -(-cols // BLOCK)), dtype=torch.uint8, device=device), fmt)
 
 
-def _room_kept(keep, rows, cols, device):
-    """None, the caller's Checkpoint, or a new one of the format"""
-    return keep if keep is None or type(keep) is Checkpoint else empty_checkpoint(rows, cols, keep, device)
-
-
-def _linear_work(L, rows, cin, cout, device, work):
-    """(workspace or None, its bytes)"""
-    key = (rows, cin, cout, device.index)
-    need = _work_bytes.get(key)
-    if need is None:
-        need = L.moc_linear_work(rows, cin, cout)
-        if need < 0:
-            raise moc.MoccasinError(need, "moc_linear_work")
-        if len(_work_bytes) > 4096:
-            _work_bytes.clear()
-        _work_bytes[key] = need
-    if work is None and need:
-        torch = moc._tc()
-        work = torch.empty(need, dtype=torch.uint8, device=device)
-    return work, 0 if work is None else work.numel() * work.element_size()
-
-
-def _ptr(x):
-    return None if x is None else x.data_ptr()
-
-
 def moc_checkpoint_write(x, fmt="e4m3", out=None, stream=None):
     """Keep x [rows, cols] in 8 bits ("e4m3" or "int8").  Returns the Checkpoint (`out`, if given)."""
-    L = lib()
-    mx = _matrix(x, "x")
-    rows, cols = x.shape
-    with moc._on(stream):
-        out = out if out is not None else empty_checkpoint(rows, cols, fmt, x.device)
-    _same_device(x, out)
-    moc._check(L.moc_checkpoint_write(rows, cols, mx, _matrix(out, "out", rows, cols), moc._stream_handle(stream)), "moc_checkpoint_write")
+    code, out = _call("checkpoint_write", stream, x, fmt, out)
+    moc._check(code, "moc_checkpoint_write")
     return out
 
 
 def moc_checkpoint_read(kept, dtype, act="none", out=None, stream=None):
     """act(the values of a checkpoint), as a tensor of `dtype`."""
-    L = lib()
-    mk = _matrix(kept, "kept")
-    if mk.type not in (MOC_E4M3, MOC_I8):
-        raise ValueError("kept: a Checkpoint expected")
-    rows, cols = kept.shape
-    with moc._on(stream):
-        out = out if out is not None else moc._tc().empty((rows, cols), dtype=dtype, device=kept.codes.device)
-    _same_device(kept.codes, out)
-    moc._check(L.moc_checkpoint_read(rows, cols, mk, _act(act), _matrix(out, "out", rows, cols), moc._stream_handle(stream)), "moc_checkpoint_read")
+    code, out = _call("checkpoint_read", stream, kept, dtype, _act(act), out)
+    moc._check(code, "moc_checkpoint_read")
     return out
 
 
@@ -214,22 +135,7 @@ def moc_norm_forward(x, gamma=None, beta=None, eps=1e-5, keep=None, dtype=None, 
     """Layer norm of the rows of x (a tensor or a Checkpoint).  Returns (y, mean, rstd, kept): y of
     `dtype` (default x's, float32 for a checkpoint), mean and rstd float32 [rows], and y in 8 bits if
     `keep` names a format or is a Checkpoint to write to, else None."""
-    L, torch = lib(), moc._tc()
-    mx = _matrix(x, "x")
-    rows, cols = x.shape
-    device = _device_of(x)
-    with moc._on(stream):
-        if out is None:
-            out = torch.empty((rows, cols), dtype=dtype or (torch.float32 if type(x) is Checkpoint else x.dtype), device=device)
-        kept = _room_kept(keep, rows, cols, device)
-        stats = torch.empty((2, rows), dtype=torch.float32, device=device)
-    _same_device(out, x, gamma, beta, kept)
-    (pg, tg), (pb, tb) = _param(gamma, cols, "gamma"), _param(beta, cols, "beta")
-    if pg is not None and pb is not None and tg != tb:
-        raise ValueError("gamma and beta must have one type")
-    mean, rstd = stats[0], stats[1]
-    code = L.moc_norm_forward(rows, cols, mx, pg, pb, tg if pg is not None else tb, eps, _matrix(out, "out", rows, cols),
-                              None if kept is None else _matrix(kept, "keep", rows, cols), mean.data_ptr(), rstd.data_ptr(), moc._stream_handle(stream))
+    code, out, mean, rstd, kept = _call("norm_forward", stream, x, gamma, beta, eps, keep, dtype, out)
     moc._check(code, "moc_norm_forward")
     return out, mean, rstd, kept
 
@@ -237,26 +143,7 @@ def moc_norm_forward(x, gamma=None, beta=None, eps=1e-5, keep=None, dtype=None, 
 def moc_norm_backward(dy, x, gamma, mean, rstd, residual=None, want_params=True, out=None, work=None, stream=None):
     """Layer norm's gradients from dy, x (a tensor or a Checkpoint) and the statistics of the forward
     pass.  Returns (dx of dy's type, dgamma, dbeta float32 or None); `residual` is added to dx."""
-    L, torch = lib(), moc._tc()
-    md = _matrix(dy, "dy")
-    rows, cols = dy.shape
-    mx = _matrix(x, "x", rows, cols)
-    pg, tg = _param(gamma, cols, "gamma")
-    dgamma = dbeta = None
-    with moc._on(stream):
-        out = out if out is not None else torch.empty((rows, cols), dtype=dy.dtype, device=dy.device)
-        if want_params:
-            grads = torch.empty((2, cols), dtype=torch.float32, device=dy.device)
-            dgamma, dbeta = grads[0], grads[1]
-            if work is None:
-                need = L.moc_norm_backward_work(rows, cols)
-                if need < 0:
-                    raise moc.MoccasinError(need, "moc_norm_backward_work")
-                work = torch.empty(need, dtype=torch.uint8, device=dy.device)
-    _same_device(dy, x, gamma, mean, rstd, residual, out, work)
-    code = L.moc_norm_backward(rows, cols, md, mx, pg, tg, _floats(mean, rows, "mean"), _floats(rstd, rows, "rstd"),
-                               None if residual is None else _matrix(residual, "residual", rows, cols), _matrix(out, "out", rows, cols),
-                               _ptr(dgamma), _ptr(dbeta), _ptr(work), 0 if work is None else work.numel() * work.element_size(), moc._stream_handle(stream))
+    code, out, dgamma, dbeta = _call("norm_backward", stream, dy, x, gamma, mean, rstd, residual, want_params, out, work)
     moc._check(code, "moc_norm_backward")
     return out, dgamma, dbeta
 
@@ -264,22 +151,7 @@ def moc_norm_backward(dy, x, gamma, mean, rstd, residual=None, want_params=True,
 def moc_linear_forward(x, w, bias=None, act="none", residual=None, keep=None, dtype=None, out=None, work=None, stream=None):
     """act(x w^T + bias) + residual for x [rows, cin], w [cout, cin].  Returns (y of `dtype`, default
     x's; x w^T + bias in 8 bits if `keep` names a format or is a Checkpoint to write to, else None)."""
-    L, torch = lib(), moc._tc()
-    mx, mw = _matrix(x, "x"), _matrix(w, "w")
-    rows, cin = x.shape
-    cout = w.shape[0]
-    if w.shape[1] != cin:
-        raise ValueError(f"w: {cout} x {cin} expected, got {cout} x {w.shape[1]}")
-    pb, tb = _param(bias, cout, "bias")
-    device = x.device
-    with moc._on(stream):
-        out = out if out is not None else torch.empty((rows, cout), dtype=dtype or x.dtype, device=device)
-        kept = _room_kept(keep, rows, cout, device)
-        work, bytes_ = _linear_work(L, rows, cin, cout, device, work)
-    _same_device(x, w, bias, residual, out, kept, work)
-    code = L.moc_linear_forward(rows, cin, cout, mx, mw, pb, tb, _act(act), None if residual is None else _matrix(residual, "residual", rows, cout),
-                                _matrix(out, "out", rows, cout), None if kept is None else _matrix(kept, "keep", rows, cout), _ptr(work), bytes_,
-                                moc._stream_handle(stream))
+    code, out, kept = _call("linear_forward", stream, x, w, bias, _act(act), residual, keep, dtype, out, work)
     moc._check(code, "moc_linear_forward")
     return out, kept
 
@@ -287,18 +159,7 @@ def moc_linear_forward(x, w, bias=None, act="none", residual=None, keep=None, dt
 def moc_linear_backward_input(dy, w, act="none", pre=None, dtype=None, out=None, work=None, stream=None):
     """(dy w) * act'(pre) for dy [rows, cout], w [cout, cin] and pre [rows, cin], a tensor or a
     Checkpoint of the activation's argument (act "none": no factor)."""
-    L, torch = lib(), moc._tc()
-    md, mw = _matrix(dy, "dy"), _matrix(w, "w")
-    rows, cout = dy.shape
-    cin = w.shape[1]
-    if w.shape[0] != cout:
-        raise ValueError(f"w: {cout} x {cin} expected, got {w.shape[0]} x {cin}")
-    with moc._on(stream):
-        out = out if out is not None else torch.empty((rows, cin), dtype=dtype or dy.dtype, device=dy.device)
-        work, bytes_ = _linear_work(L, rows, cin, cout, dy.device, work)
-    _same_device(dy, w, pre, out, work)
-    code = L.moc_linear_backward_input(rows, cin, cout, md, mw, _act(act), None if pre is None else _matrix(pre, "pre", rows, cin),
-                                       _matrix(out, "out", rows, cin), _ptr(work), bytes_, moc._stream_handle(stream))
+    code, out = _call("linear_backward_input", stream, dy, w, _act(act), pre, dtype, out, work)
     moc._check(code, "moc_linear_backward_input")
     return out
 
@@ -306,16 +167,6 @@ def moc_linear_backward_input(dy, w, act="none", pre=None, dtype=None, out=None,
 def moc_linear_backward_weight(dy, x, dtype=None, want_bias=True, out=None, work=None, stream=None):
     """(dw = dy^T x, db = the column sums of dy, float32 or None) for dy [rows, cout] and x [rows, cin],
     a tensor or a Checkpoint; dw [cout, cin] of `dtype`, default float32."""
-    L, torch = lib(), moc._tc()
-    md = _matrix(dy, "dy")
-    rows, cout = dy.shape
-    mx = _matrix(x, "x", rows)
-    cin = x.shape[1]
-    with moc._on(stream):
-        out = out if out is not None else torch.empty((cout, cin), dtype=dtype or torch.float32, device=dy.device)
-        db = torch.empty(cout, dtype=torch.float32, device=dy.device) if want_bias else None
-        work, bytes_ = _linear_work(L, rows, cin, cout, dy.device, work)
-    _same_device(dy, x, out, work)
-    code = L.moc_linear_backward_weight(rows, cin, cout, md, mx, _matrix(out, "out", cout, cin), _ptr(db), _ptr(work), bytes_, moc._stream_handle(stream))
+    code, out, db = _call("linear_backward_weight", stream, dy, x, dtype, want_bias, out, work)
     moc._check(code, "moc_linear_backward_weight")
     return out, db
