@@ -38,7 +38,7 @@ __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
 }
 
 enum { kRow = 0, kCol = 1 };                       // how an operand lies
-enum { kDirect = 0, kThroughRegisters = 1 };       // how it gets to LDS
+enum Loading { kDirect, kThroughRegisters, kNarrow };   // how operands get to LDS; kNarrow: some have rows of fewer than eight
 
 struct Operand {
   const void* data;
@@ -188,66 +188,99 @@ struct DirectLoader {
 };
 
 // Through registers: any alignment and size, and checkpoints, whose codes become values on the way.
-template <int LAY, int WIDTH, int THREADS, int TYPE, int HELD>
+// Loads have no branch: of a run that the row ends in, the row's last eight are loaded and moved down
+// when they are put; rows beyond the last are the last one, put as zeros where they are k.  NARROW: rows
+// of fewer than eight.
+template <int LAY, int WIDTH, int THREADS, int TYPE, int HELD, bool NARROW = false>
 struct RegisterLoader {
   using T = Tile<LAY, WIDTH, THREADS>;
   using V = typename Stored<TYPE>::type;
   static constexpr int kLoads = 0, kWork = 0, kWrites = 0;   // left to the scheduler
   static constexpr bool kKept = HELD == MOC_E4M3 || HELD == MOC_I8;
+  // A step's part of this thread: 16-bit values, or eight codes and their scale.
+  struct Set {
+    uint32_t w[T::kEach][kKept ? 2 : 4];
+    uint8_t scale[kKept ? T::kEach : 1];
+  };
   Operand x;
-  int first, extent, k, end;
-  uint4 held[T::kEach];        // 16-bit values, or eight codes and their scale
-  uint8_t scale[kKept ? T::kEach : 1];
+  int first, extent, end, next;
+  Set own;
 
-  __device__ __forceinline__ RegisterLoader(const Operand& x_, int first_, int extent_, int begin, int end_) : x(x_), first(first_), extent(extent_), k(begin), end(end_) {}
+  __device__ __forceinline__ RegisterLoader(const Operand& x_, int first_, int extent_, int begin, int end_) : x(x_), first(first_), extent(extent_), end(end_), next(begin) {}
 
-  __device__ __forceinline__ void load(Lds*) {
+  // values of the memory's rows
+  __device__ __forceinline__ int length() const { return LAY == kRow ? end : extent; }
+
+  __device__ __forceinline__ void load(Set& s, int k) const {
+    const int last = (LAY == kRow ? extent : end) - 1, length = this->length();
 #pragma unroll
     for (int i = 0; i < T::kEach; ++i) {
-      const int row = T::row(i), piece = T::piece(i) * 8;
-      // the memory's row and the place in it, and how many of the eight exist
-      const int r = LAY == kRow ? first + row : k + row, c = LAY == kRow ? k + piece : first + piece;
-      const int n = r < (LAY == kRow ? extent : end) ? (LAY == kRow ? end : extent) - c : 0;
-      held[i] = uint4{0, 0, 0, 0};
-      if constexpr (kKept) {
-        scale[i] = 0;
-        if (n > 0) {
-          const uint2 codes = load_codes(static_cast<const uint8_t*>(x.data) + r * x.stride + c, n);
-          held[i].x = codes.x;
-          held[i].y = codes.y;
-          scale[i] = x.scales[r * x.scale_stride + c / MOC_BLOCK];
+      const int row = min((LAY == kRow ? first : k) + T::row(i), last), c = (LAY == kRow ? k : first) + T::piece(i) * kRun;
+      if constexpr (kKept) s.scale[i] = x.scales[row * x.scale_stride + min(c, length - 1) / MOC_BLOCK];
+      if constexpr (NARROW) {
+        const int n = length - c;
+        if constexpr (kKept) {
+          const uint2 codes = load_codes(static_cast<const uint8_t*>(x.data) + row * x.stride + c, n);
+          s.w[i][0] = codes.x;
+          s.w[i][1] = codes.y;
+        } else {
+          const Raw r = load_raw<TYPE>(static_cast<const uint16_t*>(x.data) + row * x.stride, nullptr, c, n);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s.w[i][j] = r.a[j];
         }
       } else {
-        const uint16_t* p = static_cast<const uint16_t*>(x.data) + r * x.stride + c;
-        if (n >= 8) {
-          __builtin_memcpy(&held[i], p, 16);
-        } else if (n > 0) {
-          uint32_t w[4] = {0, 0, 0, 0};
+        const int at = min(c, length - kRun);
+        if constexpr (kKept) __builtin_memcpy(s.w[i], static_cast<const uint8_t*>(x.data) + row * x.stride + at, 8);
+        else __builtin_memcpy(s.w[i], static_cast<const uint16_t*>(x.data) + row * x.stride + at, 16);
+      }
+    }
+  }
+  // Pieces from `from` on, below `to`, of what was loaded for k.
+  __device__ __forceinline__ void put(const Set& s, int k, Lds* lds, int from, int to) const {
+    const int length = this->length();
+    const bool edge = k + kStepK > end || (LAY == kCol && first + WIDTH > extent);   // the same for all
 #pragma unroll
-          for (int j = 0; j < 7; ++j)
-            if (j < n) w[j >> 1] |= (uint32_t)p[j] << (16 * (j & 1));
-          held[i] = uint4{w[0], w[1], w[2], w[3]};
+    for (int i = from; i < to; ++i) {
+      uint64_t v[kKept ? 1 : 2];
+      __builtin_memcpy(v, s.w[i], sizeof v);
+      if (edge) {
+        const int c = (LAY == kRow ? k : first) + T::piece(i) * kRun;
+        const int n = LAY == kCol && k + T::row(i) >= end ? 0 : length - c;
+        const int down = NARROW ? 0 : kRun - n;   // values
+        if (n <= 0) {
+#pragma unroll
+          for (uint64_t& p : v) p = 0;
+        } else if (down > 0) {
+          if constexpr (kKept) {
+            v[0] >>= 8 * down;
+          } else {
+            const int bits = 16 * down;
+            v[0] = bits >= 64 ? v[1] >> (bits - 64) : v[0] >> bits | v[1] << (64 - bits);
+            v[1] = bits >= 64 ? 0 : v[1] >> bits;
+          }
         }
       }
-    }
-    k += kStepK;
-  }
-  __device__ __forceinline__ void mend(Lds*) {}
-  __device__ __forceinline__ void put(Lds* to, int h) {
-#pragma unroll
-    for (int i = h * T::kEach / 2; i < (h + 1) * T::kEach / 2; ++i) {
-      u32x4 out = {held[i].x, held[i].y, held[i].z, held[i].w};
+      u32x4 out;
       if constexpr (kKept) {
-        float v[kRun];
-        decode_run<HELD>(uint2{held[i].x, held[i].y}, scale_of(scale[i]), v);
+        float f[kRun];
+        decode_run<HELD>(uint2{(uint32_t)v[0], (uint32_t)(v[0] >> 32)}, scale_of(s.scale[i]), f);
         V t[kRun];
 #pragma unroll
-        for (int j = 0; j < kRun; ++j) t[j] = (V)v[j];
+        for (int j = 0; j < kRun; ++j) t[j] = (V)f[j];
         __builtin_memcpy(&out, t, 16);
+      } else {
+        __builtin_memcpy(&out, v, 16);
       }
-      *(__attribute__((address_space(3))) u32x4*)(to + (i * THREADS + (int)threadIdx.x) * 16) = out;
+      *(__attribute__((address_space(3))) u32x4*)(lds + (i * THREADS + (int)threadIdx.x) * 16) = out;
     }
   }
+  // One step after the other.
+  __device__ __forceinline__ void load(Lds*) {
+    if (next < end) load(own, next);
+    next += kStepK;
+  }
+  __device__ __forceinline__ void put(Lds* to, int h) const { put(own, next - kStepK, to, h * T::kEach / 2, (h + 1) * T::kEach / 2); }
+  __device__ __forceinline__ void mend(Lds*) {}
 };
 
 // A checkpoint whose rows and strides are multiples of 16: a thread has the 32 values of a block in one
@@ -386,9 +419,88 @@ struct Reader {
   }
 };
 
+// ---- tiles --------------------------------------------------------------------------------------
+
+struct TileAt {
+  int m0, n0;
+};
+// Workgroups go round the eight XCDs: each XCD takes a stretch of neighbouring tiles, in groups of
+// eight rows of tiles, so that what its L2 holds is used again.
+template <int BM, int BN>
+__device__ __forceinline__ TileAt tile_of(const LinearArgs& g) {
+  int64_t tile = blockIdx.x;
+  const int tiles = g.tiles_m * g.tiles_n, per = tiles / 8, more = tiles % 8, xcd = (int)(tile % 8);
+  tile = (int64_t)xcd * per + (xcd < more ? xcd : more) + tile / 8;
+  const int band = 8 * g.tiles_n, first_m = (int)(tile / band) * 8, height = min(8, g.tiles_m - first_m), in = (int)(tile % band);
+  return TileAt{(first_m + in % height) * BM, in / height * BN};
+}
+
+// Out by way of LDS, so that lanes next to each other have runs next to each other and a quad has a
+// block of 32.  A lane has 16 of the 32 n of one m: 8 * (r / 4) + 4 * (lane / 32) + r % 4.  Every
+// wave stages its own outputs, 64 rows at a time, in memory of its own; 16 bytes of a row are moved
+// by the row's number, so that writes (32 rows at once) and reads (whole rows) meet all banks.
+// s0 .. s3: BN, BN, BM and BM rows of an operand's tile, nothing in them still wanted.
+template <int BM, int BN, int WM, int WN>
+__device__ __forceinline__ void write_out(const LinearArgs& g, const f32x16 (&acc)[BM / WM / 32][BN / WN / 32], int m0, int n0, Lds* s0, Lds* s1, Lds* s2, Lds* s3) {
+  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  constexpr int TH = TM < 2 ? TM : 2, kCols = TN * 32, kChunks = kCols / 4, kMove = kChunks < 16 ? kChunks - 1 : 15;
+  constexpr int kStage = TH * 32 * kCols * 4, kPer = BN * kRowBytes / kStage;   // waves that one of the arrays has room for
+  static_assert(BM <= BN && kPer >= 1 && (kPer >= WM * WN || (BM == BN && 4 * kPer >= WM * WN)));
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  const int array = wave / kPer;
+  Lds* const stage = (array == 0 ? s0 : array == 1 ? s1 : array == 2 ? s2 : s3) + wave % kPer * kStage;
+  const int lane = threadIdx.x & (kWave - 1);
+  constexpr int kRuns = kCols / kRun, kRowsAt = kWave / kRuns;   // runs of a row, rows at a time
+  const int col = n0 + wn + lane % kRuns * kRun, n = g.n - col;
+  float bias[kRun];
+#pragma unroll
+  for (int r = 0; r < kRun; ++r) bias[r] = 0.0f;
+  if (g.e.bias && g.splits == 1 && n > 0) load_any(g.e.bias_type, g.e.bias, col, n, bias);
+  constexpr int kAhead = 3;   // rows of the extra operand on their way
+  Raw ahead[kAhead];
+#pragma unroll
+  for (int half = 0; half < TM / TH; ++half) {
+    const int row0 = m0 + wm + half * TH * 32 + lane / kRuns;
+    const auto extra = [&](int at) { return row0 + at * kRowsAt < g.m && at * kRowsAt < TH * 32 && g.splits == 1 ? load_extra(g.e, row0 + at * kRowsAt, col, n) : Raw{}; };
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ahead[i] = extra(i);
+#pragma unroll
+    for (int i = 0; i < TH; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int m = 32 * i + (lane & 31), chunk = 8 * j + 2 * q + (lane >> 5);
+          const f32x16& c = acc[half * TH + i][j];
+          *(__attribute__((address_space(3))) f32x4*)(stage + m * (kCols * 4) + (chunk ^ (m & kMove)) * 16) = f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+        }
+#pragma unroll 1
+    for (int at = 0; at < TH * 32 / kRowsAt; ++at) {
+      const int row = row0 + at * kRowsAt, m = lane / kRuns + at * kRowsAt;
+      if (row >= g.m) break;   // all lanes of a row, and of a quad
+      const Raw now = ahead[0];
+#pragma unroll
+      for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
+      ahead[kAhead - 1] = extra(at + kAhead);
+      float v[kRun];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 c = *(const __attribute__((address_space(3))) f32x4*)(stage + m * (kCols * 4) + ((lane % kRuns * 2 + h) ^ (m & kMove)) * 16);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[4 * h + r] = c[r];
+      }
+      if (g.splits > 1) {
+        if (col < g.partial_stride) store_run<MOC_F32>(g.partial + ((int64_t)blockIdx.y * g.m + row) * g.partial_stride, col, kRun, v);
+      } else {
+        finish_sum(g.e, row, col, n, bias, now, v);
+      }
+    }
+  }
+}
+
 // ---- the kernel ---------------------------------------------------------------------------------
 
-template <int TYPE, int LAY, int WIDTH, int THREADS, int LOAD, int HELD>
+template <int TYPE, int LAY, int WIDTH, int THREADS, Loading LOAD, int HELD>
 struct PickB { using type = RegisterLoader<LAY, WIDTH, THREADS, TYPE, HELD>; };
 template <int TYPE, int LAY, int WIDTH, int THREADS>
 struct PickB<TYPE, LAY, WIDTH, THREADS, kDirect, TYPE> { using type = DirectLoader<LAY, WIDTH, THREADS>; };
@@ -414,19 +526,14 @@ __device__ __forceinline__ void interleave() {
 }
 
 // TYPE of the operands; HELD: of b, TYPE or a checkpoint's.
-template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int LOAD, int HELD>
+template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, Loading LOAD, int HELD>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;   // 32 x 32 outputs of a wave
   __shared__ __attribute__((aligned(1024))) uint8_t a0[BM * kRowBytes], a1[BM * kRowBytes], b0[BN * kRowBytes], b1[BN * kRowBytes];
 
-  // Workgroups go round the eight XCDs: each XCD takes a stretch of neighbouring tiles, in groups of
-  // eight rows of tiles, so that what its L2 holds is used again.
-  int64_t tile = blockIdx.x;
-  const int tiles = g.tiles_m * g.tiles_n, per = tiles / 8, more = tiles % 8, xcd = (int)(tile % 8);
-  tile = (int64_t)xcd * per + (xcd < more ? xcd : more) + tile / 8;
-  const int band = 8 * g.tiles_n, first_m = (int)(tile / band) * 8, height = min(8, g.tiles_m - first_m), in = (int)(tile % band);
-  const int m0 = (first_m + in % height) * BM, n0 = in / height * BN;
+  const TileAt at = tile_of<BM, BN>(g);
+  const int m0 = at.m0, n0 = at.n0;
   const int begin = blockIdx.y * g.split_k, end = min(g.k, begin + g.split_k);
 
   using LoadA = typename std::conditional<LOAD == kDirect, DirectLoader<ALAY, BM, kThreads>, RegisterLoader<ALAY, BM, kThreads, TYPE, TYPE>>::type;
@@ -524,63 +631,87 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
     step(pa1, pb1, pa0, pb0);
   }
 
-  // Out by way of LDS, so that lanes next to each other have runs next to each other and a quad has a
-  // block of 32.  A lane has 16 of the 32 n of one m: 8 * (r / 4) + 4 * (lane / 32) + r % 4.  Every
-  // wave stages its own outputs, 64 rows at a time, in memory of its own; 16 bytes of a row are moved
-  // by the row's number, so that writes (32 rows at once) and reads (whole rows) meet all banks.
-  constexpr int TH = TM < 2 ? TM : 2, kCols = TN * 32, kChunks = kCols / 4, kMove = kChunks < 16 ? kChunks - 1 : 15;
-  constexpr int kStage = TH * 32 * kCols * 4, kPer = (int)sizeof b0 / kStage;   // waves that one of the arrays has room for
-  static_assert(sizeof a0 <= sizeof b0 && kPer >= 1 && (kPer >= WM * WN || (sizeof a0 == sizeof b0 && 4 * kPer >= WM * WN)));
   arrived();   // the last reads; and the loads of nothing that write zeros
-  const int array = wave / kPer;
-  Lds* const stage = (array == 0 ? pb0 : array == 1 ? pb1 : array == 2 ? pa0 : pa1) + wave % kPer * kStage;
-  const int lane = threadIdx.x & (kWave - 1);
-  constexpr int kRuns = kCols / kRun, kRowsAt = kWave / kRuns;   // runs of a row, rows at a time
-  const int col = n0 + wn + lane % kRuns * kRun, n = g.n - col;
-  float bias[kRun];
+  write_out<BM, BN, WM, WN>(g, acc, m0, n0, pb0, pb1, pa0, pa1);
+}
+
+// For products of few or ragged tiles, which wait for memory: every operand goes through registers, four
+// steps of it on their way, so that any alignment does and a short sum is all loaded at once.
+constexpr int kRing = 4;
+template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int HELD, bool NARROW>
+__global__ __launch_bounds__(WM* WN* kWave) void linear_ring_kernel(LinearArgs g) {
+  constexpr int kThreads = WM * WN * kWave;
+  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  __shared__ __attribute__((aligned(1024))) uint8_t a0[BM * kRowBytes], a1[BM * kRowBytes], b0[BN * kRowBytes], b1[BN * kRowBytes];
+  const TileAt at = tile_of<BM, BN>(g);
+  const int begin = blockIdx.y * g.split_k, end = min(g.k, begin + g.split_k);
+  using LoadA = RegisterLoader<ALAY, BM, kThreads, TYPE, TYPE, NARROW>;
+  using LoadB = RegisterLoader<BLAY, BN, kThreads, TYPE, HELD, NARROW>;
+  const LoadA la(g.a, at.m0, g.m, begin, end);
+  const LoadB lb(g.b, at.n0, g.n, begin, end);
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
+  const Reader<ALAY, BM, TM> ra(wm);
+  const Reader<BLAY, BN, TN> rb(wn);
+
+  f32x16 acc[TM][TN];
 #pragma unroll
-  for (int r = 0; r < kRun; ++r) bias[r] = 0.0f;
-  if (g.e.bias && g.splits == 1 && n > 0) load_any(g.e.bias_type, g.e.bias, col, n, bias);
-  constexpr int kAhead = 3;   // rows of the extra operand on their way
-  Raw ahead[kAhead];
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-  for (int half = 0; half < TM / TH; ++half) {
-    const int row0 = m0 + wm + half * TH * 32 + lane / kRuns;
-    const auto extra = [&](int at) { return row0 + at * kRowsAt < g.m && at * kRowsAt < TH * 32 && g.splits == 1 ? load_extra(g.e, row0 + at * kRowsAt, col, n) : Raw{}; };
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) ahead[i] = extra(i);
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  typename LoadA::Set sa[kRing];
+  typename LoadB::Set sb[kRing];
+  Lds *const pa[2] = {(Lds*)a0, (Lds*)a1}, *const pb[2] = {(Lds*)b0, (Lds*)b1};
+  // Beyond the last step it is loaded again: without a branch the compiler knows how many loads are under
+  // way, and waits for one step's only.
+  const int last = begin + (end - begin - 1) / kStepK * kStepK;
+  const auto load = [&](int i, int k) {
+    la.load(sa[i], min(k, last));
+    lb.load(sb[i], min(k, last));
+  };
+  if (begin < end) {
 #pragma unroll
-    for (int i = 0; i < TH; ++i)
+    for (int i = 0; i < kRing; ++i) load(i, begin + i * kStepK);
+  }
+  // Two buffers and a barrier a step: what is put into one was last read before the barrier in between.
+  const auto put = [&](int i, int k) {
+    la.put(sa[i], k, pa[i & 1], 0, LoadA::T::kEach);
+    lb.put(sb[i], k, pb[i & 1], 0, LoadB::T::kEach);
+  };
+  const auto multiply = [&](int i) {
+    __syncthreads();   // waits for what was put, not for loads
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
+    for (int s = 0; s < kStepK / 16; ++s) {
+      s16x8 fa[TM], fb[TN];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int m = 32 * i + (lane & 31), chunk = 8 * j + 2 * q + (lane >> 5);
-          const f32x16& c = acc[half * TH + i][j];
-          *(__attribute__((address_space(3))) f32x4*)(stage + m * (kCols * 4) + (chunk ^ (m & kMove)) * 16) = f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
-        }
-#pragma unroll 1
-    for (int at = 0; at < TH * 32 / kRowsAt; ++at) {
-      const int row = row0 + at * kRowsAt, m = lane / kRuns + at * kRowsAt;
-      if (row >= g.m) break;   // all lanes of a row, and of a quad
-      const Raw now = ahead[0];
+      for (int j = 0; j < TN; ++j) fb[j] = rb.read(pb[i & 1], j, s);
 #pragma unroll
-      for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
-      ahead[kAhead - 1] = extra(at + kAhead);
-      float v[kRun];
+      for (int c = 0; c < TM; ++c) fa[c] = ra.read(pa[i & 1], c, s);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 c = *(const __attribute__((address_space(3))) f32x4*)(stage + m * (kCols * 4) + ((lane % kRuns * 2 + h) ^ (m & kMove)) * 16);
+      for (int c = 0; c < TM; ++c)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[4 * h + r] = c[r];
-      }
-      if (g.splits > 1) {
-        if (col < g.partial_stride) store_run<MOC_F32>(g.partial + ((int64_t)blockIdx.y * g.m + row) * g.partial_stride, col, kRun, v);
-      } else {
-        finish_sum(g.e, row, col, n, bias, now, v);
-      }
+        for (int j = 0; j < TN; ++j) acc[c][j] = mfma<TYPE>(fb[j], fa[c], acc[c][j]);
+    }
+  };
+  int k = begin;
+  for (; k + (kRing - 1) * kStepK < end; k += kRing * kStepK) {
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) {
+      put(i, k + i * kStepK);
+      load(i, k + (i + kRing) * kStepK);
+      multiply(i);
     }
   }
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i) {
+    if (k + i * kStepK >= end) break;
+    put(i, k + i * kStepK);
+    multiply(i);
+  }
+  __syncthreads();
+  write_out<BM, BN, WM, WN>(g, acc, at.m0, at.n0, pb[0], pb[1], pa[0], pa[1]);
 }
 
 // The sum of the splits, in their order, and the epilogue; a thread has a run, a quad a block.
@@ -615,21 +746,25 @@ struct LinearPlan {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-inline LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, bool direct, int units) {
+inline LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, Loading how, int units) {
   LinearPlan p = {};
-  if (m <= 32) {
+  if (how == kNarrow) {
+    p.tile_m = p.tile_n = 64;
+  } else if (m <= 32) {
     p.tile_m = 32;
     p.tile_n = 128;
-  } else if (direct && ceil_div(m, 256) * ceil_div(n, 256) * 4 >= 3 * (int64_t)units) {
+  } else if (how == kDirect && ceil_div(m, 256) * ceil_div(n, 256) * 4 >= 3 * (int64_t)units) {
     p.tile_m = p.tile_n = 256;
-  } else {
+  } else if (ceil_div(m, 128) * ceil_div(n, 128) >= 2 * (int64_t)units) {
     p.tile_m = p.tile_n = 128;
+  } else {
+    p.tile_m = p.tile_n = 64;
   }
   p.tiles_m = (int)ceil_div(m, p.tile_m);
   p.tiles_n = (int)ceil_div(n, p.tile_n);
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, steps = ceil_div(k, kStepK);
   // Few tiles: k is cut too, at least four steps a split, until every compute unit has the workgroups that it holds.
-  int64_t splits = tiles ? (p.tile_m == 256 ? 1 : 2) * (int64_t)units / tiles : 1;
+  int64_t splits = tiles ? (p.tile_m == 256 ? 1 : p.tile_m == 64 ? 4 : 2) * (int64_t)units / tiles : 1;
   if (splits > steps / 4) splits = steps / 4;
   if (splits < 1) splits = 1;
   const int64_t each = ceil_div(steps, splits);
@@ -645,6 +780,9 @@ inline bool direct_ok(const moc_matrix* x, int64_t along) { return aligned_to(x-
 
 // Whether a checkpoint can take KeptLoader.
 inline bool kept_direct_ok(const moc_matrix* x, int64_t along) { return aligned_to(x->data, 16) && x->stride % 16 == 0 && along % 16 == 0; }
+
+// How operands go to LDS, whose rows have `along_a` and `along_b` values.
+inline Loading loading_of(bool direct, int64_t along_a, int64_t along_b) { return along_a < kRun || along_b < kRun ? kNarrow : direct ? kDirect : kThroughRegisters; }
 
 inline Operand operand_of(const moc_matrix* x) { return Operand{x->data, x->scales, x->stride, x->scale_stride}; }
 
@@ -665,23 +803,25 @@ inline int64_t moc_bias_stretches(int64_t rows, int64_t cout, int units) {
 using LinearKernel = void (*)(LinearArgs);
 
 template <int TYPE, int ALAY, int BLAY, int HELD>
-LinearKernel pick_linear(int tile_m, bool direct) {
-  if (direct) {
+LinearKernel pick_linear(int tile_m, Loading how) {
+  if (how == kNarrow) return linear_ring_kernel<TYPE, ALAY, BLAY, 64, 64, 2, 2, HELD, true>;
+  if (tile_m == 64) return linear_ring_kernel<TYPE, ALAY, BLAY, 64, 64, 2, 2, HELD, false>;
+  if (how == kDirect) {
     if (tile_m == 256) return linear_kernel<TYPE, ALAY, BLAY, 256, 256, 2, 4, kDirect, HELD>;
     if (tile_m == 128) return linear_kernel<TYPE, ALAY, BLAY, 128, 128, 2, 2, kDirect, HELD>;
     return linear_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, kDirect, HELD>;
   }
   if (tile_m == 128) return linear_kernel<TYPE, ALAY, BLAY, 128, 128, 2, 2, kThroughRegisters, HELD>;
-  return linear_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, kThroughRegisters, HELD>;
+  return linear_ring_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, HELD, false>;
 }
 
 // Queues the product: `g` has the operands, sizes and epilogue; held: b's type.
 template <int ALAY, int BLAY, bool KEPT>
-int queue_linear(LinearArgs g, int type, int held, bool direct, void* work, int64_t work_bytes, void* hip_stream) {
+int queue_linear(LinearArgs g, int type, int held, Loading how, void* work, int64_t work_bytes, void* hip_stream) {
   int units = 0;
   const int rc = moc_compute_units(&units);
   if (rc != MOC_OK) return rc;
-  const LinearPlan p = linear_plan(g.m, g.n, g.k, direct, units);
+  const LinearPlan p = linear_plan(g.m, g.n, g.k, how, units);
   if (p.work_bytes > 0 && (!work || !aligned_to(work, 16) || work_bytes < p.work_bytes)) return MOC_EINVAL;
   if ((int64_t)p.tiles_m * p.tiles_n > (1 << 22)) return MOC_EOVERFLOW;   // a launch's threads
   g.tiles_m = p.tiles_m;
@@ -693,16 +833,16 @@ int queue_linear(LinearArgs g, int type, int held, bool direct, void* work, int6
   LinearKernel kern = nullptr;
   if constexpr (KEPT) {
     if (type == MOC_BF16) {
-      kern = held == MOC_E4M3 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_E4M3>(p.tile_m, direct)
-             : held == MOC_I8 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_I8>(p.tile_m, direct)
-                              : pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, direct);
+      kern = held == MOC_E4M3 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_E4M3>(p.tile_m, how)
+             : held == MOC_I8 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_I8>(p.tile_m, how)
+                              : pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, how);
     } else {
-      kern = held == MOC_E4M3 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_E4M3>(p.tile_m, direct)
-             : held == MOC_I8 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_I8>(p.tile_m, direct)
-                              : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, direct);
+      kern = held == MOC_E4M3 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_E4M3>(p.tile_m, how)
+             : held == MOC_I8 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_I8>(p.tile_m, how)
+                              : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, how);
     }
   } else {
-    kern = type == MOC_BF16 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, direct) : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, direct);
+    kern = type == MOC_BF16 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, how) : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, how);
   }
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(p.tile_m == 256 ? 512 : 256), 0, stream, g);

@@ -36,7 +36,7 @@ int moc_linear_forward(int64_t rows, int64_t cin, int64_t cout, const moc_matrix
     e.scale_stride = kept->scale_stride;
     e.most = most_kept(kept->type, x->type);
   }
-  return queue_linear<kRow, kRow, false>(g, x->type, x->type, direct_ok(x, cin) && direct_ok(w, cin), work, work_bytes, hip_stream);
+  return queue_linear<kRow, kRow, false>(g, x->type, x->type, loading_of(direct_ok(x, cin) && direct_ok(w, cin), cin, cin), work, work_bytes, hip_stream);
 }
 
 int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout) {
@@ -45,10 +45,10 @@ int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout) {
   const int rc = moc_compute_units(&units);
   if (rc != MOC_OK) return rc;
   int64_t most = cout > 0 ? moc_bias_stretches(rows, cout, units) * cout * (int64_t)sizeof(float) : 0;
-  for (int direct = 0; direct < 2; ++direct) {
+  for (const Loading how : {kDirect, kThroughRegisters, kNarrow}) {
     const int64_t sizes[3][3] = {{rows, cout, cin}, {rows, cin, cout}, {cout, cin, rows}};
     for (const auto& s : sizes) {
-      const int64_t bytes = linear_plan(s[0], s[1], s[2], direct != 0, units).work_bytes;
+      const int64_t bytes = linear_plan(s[0], s[1], s[2], how, units).work_bytes;
       most = bytes > most ? bytes : most;
     }
   }

@@ -25,5 +25,5 @@ extern "C" int moc_linear_backward_input(int64_t rows, int64_t cin, int64_t cout
     e.slope = 1;
   }
   set_out(e, dx);
-  return queue_linear<kRow, kCol, false>(g, dy->type, dy->type, direct_ok(dy, cout) && direct_ok(w, cin), work, work_bytes, hip_stream);
+  return queue_linear<kRow, kCol, false>(g, dy->type, dy->type, loading_of(direct_ok(dy, cout) && direct_ok(w, cin), cout, cin), work, work_bytes, hip_stream);
 }

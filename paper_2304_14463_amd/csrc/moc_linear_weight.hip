@@ -66,7 +66,7 @@ extern "C" int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cou
     g.k = (int)rows;
     set_out(g.e, dw);
     const bool direct = direct_ok(dy, cout) && (is_kept(x->type) ? kept_direct_ok(x, cin) : direct_ok(x, cin));
-    const int rc = queue_linear<kCol, kCol, true>(g, dy->type, x->type, direct, work, work_bytes, hip_stream);
+    const int rc = queue_linear<kCol, kCol, true>(g, dy->type, x->type, loading_of(direct, cout, cin), work, work_bytes, hip_stream);
     if (rc != MOC_OK) return rc;
   }
   if (db) {
