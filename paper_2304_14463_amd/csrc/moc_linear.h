@@ -69,8 +69,9 @@ struct LinearArgs {
   Operand a, b;
   int m, n, k;
   int tiles_m, tiles_n, splits, split_k;   // split_k: k of a split, a multiple of kStepK
-  float* partial;                          // [splits][m][partial_stride], splits > 1 only
+  float* partial;                          // [splits][m][partial_stride], then [splits][m] of `sums`; splits > 1 only
   int64_t partial_stride;                  // n up to a multiple of MOC_BLOCK
+  float* sums;                             // [m]: of a over k (the bias's gradient), col operands only; null: none
   Epilogue e;
 };
 
@@ -202,77 +203,114 @@ struct RegisterLoader {
     uint32_t w[T::kEach][kKept ? 2 : 4];
     uint8_t scale[kKept ? T::kEach : 1];
   };
+  static constexpr int kBytes = kKept ? 1 : 2;   // of a value
   Operand x;
   int first, extent, end, next;
+  // Where pieces lie from the tile's first row on, for k = 0 and in 32 bits: the address of a load is then
+  // one in scalar registers that moves with k, and this.  Room for a run that is moved down (kRow).
+  static constexpr uint32_t kRoom = kRun * kBytes;
+  uint32_t place[T::kEach], scale_place[kKept ? T::kEach : 1];
   Set own;
 
-  __device__ __forceinline__ RegisterLoader(const Operand& x_, int first_, int extent_, int begin, int end_) : x(x_), first(first_), extent(extent_), end(end_), next(begin) {}
-
-  // values of the memory's rows
-  __device__ __forceinline__ int length() const { return LAY == kRow ? end : extent; }
-
-  __device__ __forceinline__ void load(Set& s, int k) const {
-    const int last = (LAY == kRow ? extent : end) - 1, length = this->length();
+  __device__ __forceinline__ RegisterLoader(const Operand& x_, int first_, int extent_, int begin, int end_) : x(x_), first(first_), extent(extent_), end(end_), next(begin) {
+    static_assert(!kKept || LAY == kCol);
 #pragma unroll
     for (int i = 0; i < T::kEach; ++i) {
-      const int row = min((LAY == kRow ? first : k) + T::row(i), last), c = (LAY == kRow ? k : first) + T::piece(i) * kRun;
-      if constexpr (kKept) s.scale[i] = x.scales[row * x.scale_stride + min(c, length - 1) / MOC_BLOCK];
-      if constexpr (NARROW) {
-        const int n = length - c;
+      const int row = T::row(i);
+      if constexpr (LAY == kRow) {
+        place[i] = (uint32_t)min(row, extent - 1 - first) * row_bytes() + kRoom;
+      } else {
+        place[i] = (uint32_t)row * row_bytes() + column(i);
+        if constexpr (kKept) scale_place[i] = (uint32_t)row * (uint32_t)x.scale_stride + scale_column(i);
+      }
+    }
+  }
+
+  // values of the memory's rows, their bytes, and where in them a piece lies (kCol)
+  __device__ __forceinline__ int length() const { return LAY == kRow ? end : extent; }
+  __device__ __forceinline__ uint32_t row_bytes() const { return (uint32_t)x.stride * kBytes; }
+  __device__ __forceinline__ uint32_t column(int i) const { return (uint32_t)min(first + T::piece(i) * kRun, extent - kRun) * kBytes; }
+  __device__ __forceinline__ uint32_t scale_column(int i) const { return (uint32_t)min(first + T::piece(i) * kRun, extent - 1) / MOC_BLOCK; }
+
+  // k < end
+  __device__ __forceinline__ void load(Set& s, int k) const {
+    const char* const data = static_cast<const char*>(x.data);
+    if constexpr (NARROW) {
+#pragma unroll
+      for (int i = 0; i < T::kEach; ++i) {
+        const int row = min((LAY == kRow ? first : k) + T::row(i), (LAY == kRow ? extent : end) - 1), c = (LAY == kRow ? k : first) + T::piece(i) * kRun, n = length() - c;
+        const char* const at = data + row * x.stride * kBytes;
         if constexpr (kKept) {
-          const uint2 codes = load_codes(static_cast<const uint8_t*>(x.data) + row * x.stride + c, n);
+          const uint2 codes = load_codes(reinterpret_cast<const uint8_t*>(at) + c, n);
           s.w[i][0] = codes.x;
           s.w[i][1] = codes.y;
+          s.scale[i] = x.scales[row * x.scale_stride + scale_column(i)];
         } else {
-          const Raw r = load_raw<TYPE>(static_cast<const uint16_t*>(x.data) + row * x.stride, nullptr, c, n);
+          const Raw r = load_raw<TYPE>(at, nullptr, c, n);
 #pragma unroll
           for (int j = 0; j < 4; ++j) s.w[i][j] = r.a[j];
         }
-      } else {
-        const int at = min(c, length - kRun);
-        if constexpr (kKept) __builtin_memcpy(s.w[i], static_cast<const uint8_t*>(x.data) + row * x.stride + at, 8);
-        else __builtin_memcpy(s.w[i], static_cast<const uint16_t*>(x.data) + row * x.stride + at, 16);
+      }
+    } else if constexpr (LAY == kRow) {
+      const char* const from = data + first * x.stride * kBytes + (int64_t)k * kBytes - kRoom;
+      const int most = end - kRun - k;   // -7 at least
+#pragma unroll
+      for (int i = 0; i < T::kEach; ++i) __builtin_memcpy(s.w[i], from + (place[i] + (uint32_t)(min(T::piece(i) * kRun, most) * kBytes)), sizeof s.w[i]);
+    } else {
+      const char* const from = data + k * x.stride * kBytes;
+      const uint32_t below = (uint32_t)min(end - 1 - k, kStepK - 1), most = below * row_bytes();   // the last row
+#pragma unroll
+      for (int i = 0; i < T::kEach; ++i) {
+        __builtin_memcpy(s.w[i], from + min(place[i], most + column(i)), sizeof s.w[i]);
+        if constexpr (kKept) s.scale[i] = (x.scales + k * x.scale_stride)[min(scale_place[i], below * (uint32_t)x.scale_stride + scale_column(i))];
       }
     }
   }
   // Pieces from `from` on, below `to`, of what was loaded for k.
   __device__ __forceinline__ void put(const Set& s, int k, Lds* lds, int from, int to) const {
-    const int length = this->length();
     const bool edge = k + kStepK > end || (LAY == kCol && first + WIDTH > extent);   // the same for all
+    if (!edge) {
+#pragma unroll
+      for (int i = from; i < to; ++i) put_piece(s, i, s.w[i], lds);
+      return;
+    }
 #pragma unroll
     for (int i = from; i < to; ++i) {
       uint64_t v[kKept ? 1 : 2];
       __builtin_memcpy(v, s.w[i], sizeof v);
-      if (edge) {
-        const int c = (LAY == kRow ? k : first) + T::piece(i) * kRun;
-        const int n = LAY == kCol && k + T::row(i) >= end ? 0 : length - c;
-        const int down = NARROW ? 0 : kRun - n;   // values
-        if (n <= 0) {
+      const int n = LAY == kCol && k + T::row(i) >= end ? 0 : length() - (LAY == kRow ? k : first) - T::piece(i) * kRun;   // that exist
+      const int down = NARROW || n >= kRun ? 0 : kRun - n;
+      if (n <= 0) {
 #pragma unroll
-          for (uint64_t& p : v) p = 0;
-        } else if (down > 0) {
-          if constexpr (kKept) {
-            v[0] >>= 8 * down;
-          } else {
-            const int bits = 16 * down;
-            v[0] = bits >= 64 ? v[1] >> (bits - 64) : v[0] >> bits | v[1] << (64 - bits);
-            v[1] = bits >= 64 ? 0 : v[1] >> bits;
-          }
+        for (uint64_t& p : v) p = 0;
+      } else if (down > 0) {
+        if constexpr (kKept) {
+          v[0] >>= 8 * down;
+        } else {
+          const int bits = 16 * down;
+          v[0] = bits >= 64 ? v[1] >> (bits - 64) : v[0] >> bits | v[1] << (64 - bits);
+          v[1] = bits >= 64 ? 0 : v[1] >> bits;
         }
       }
-      u32x4 out;
-      if constexpr (kKept) {
-        float f[kRun];
-        decode_run<HELD>(uint2{(uint32_t)v[0], (uint32_t)(v[0] >> 32)}, scale_of(s.scale[i]), f);
-        V t[kRun];
-#pragma unroll
-        for (int j = 0; j < kRun; ++j) t[j] = (V)f[j];
-        __builtin_memcpy(&out, t, 16);
-      } else {
-        __builtin_memcpy(&out, v, 16);
-      }
-      *(__attribute__((address_space(3))) u32x4*)(lds + (i * THREADS + (int)threadIdx.x) * 16) = out;
+      uint32_t w[kKept ? 2 : 4];
+      __builtin_memcpy(w, v, sizeof w);
+      put_piece(s, i, w, lds);
     }
+  }
+  template <int N>
+  __device__ __forceinline__ void put_piece(const Set& s, int i, const uint32_t (&w)[N], Lds* lds) const {
+    u32x4 out;
+    if constexpr (kKept) {
+      float f[kRun];
+      decode_run<HELD>(uint2{w[0], w[1]}, scale_of(s.scale[i]), f);
+      V t[kRun];
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) t[j] = (V)f[j];
+      __builtin_memcpy(&out, t, 16);
+    } else {
+      __builtin_memcpy(&out, w, 16);
+    }
+    *(__attribute__((address_space(3))) u32x4*)(lds + (i * THREADS + (int)threadIdx.x) * 16) = out;
   }
   // One step after the other.
   __device__ __forceinline__ void load(Lds*) {
@@ -680,19 +718,37 @@ __global__ __launch_bounds__(WM* WN* kWave) void linear_ring_kernel(LinearArgs g
     la.put(sa[i], k, pa[i & 1], 0, LoadA::T::kEach);
     lb.put(sb[i], k, pb[i & 1], 0, LoadB::T::kEach);
   };
+  // Sums of a over k, by products with ones: in the first column of tiles, of the waves at its start.
+  const bool summing = ALAY == kCol && g.sums && at.n0 == 0 && wn == 0;
+  const uint16_t one = TYPE == MOC_BF16 ? 0x3F80 : 0x3C00;
+  const s16x8 ones = {(short)one, (short)one, (short)one, (short)one, (short)one, (short)one, (short)one, (short)one};
+  f32x16 sums[ALAY == kCol ? TM : 1];
+#pragma unroll
+  for (f32x16& x : sums)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) x[r] = 0.0f;
   const auto multiply = [&](int i) {
     __syncthreads();   // waits for what was put, not for loads
+    s16x8 fa[kStepK / 16][TM];
 #pragma unroll
     for (int s = 0; s < kStepK / 16; ++s) {
-      s16x8 fa[TM], fb[TN];
+      s16x8 fb[TN];
 #pragma unroll
       for (int j = 0; j < TN; ++j) fb[j] = rb.read(pb[i & 1], j, s);
 #pragma unroll
-      for (int c = 0; c < TM; ++c) fa[c] = ra.read(pa[i & 1], c, s);
+      for (int c = 0; c < TM; ++c) fa[s][c] = ra.read(pa[i & 1], c, s);
 #pragma unroll
       for (int c = 0; c < TM; ++c)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[c][j] = mfma<TYPE>(fb[j], fa[c], acc[c][j]);
+        for (int j = 0; j < TN; ++j) acc[c][j] = mfma<TYPE>(fb[j], fa[s][c], acc[c][j]);
+    }
+    if constexpr (ALAY == kCol) {
+      if (summing) {
+#pragma unroll
+        for (int s = 0; s < kStepK / 16; ++s)
+#pragma unroll
+          for (int c = 0; c < TM; ++c) sums[c] = mfma<TYPE>(ones, fa[s][c], sums[c]);
+      }
     }
   };
   int k = begin;
@@ -710,6 +766,17 @@ __global__ __launch_bounds__(WM* WN* kWave) void linear_ring_kernel(LinearArgs g
     put(i, k + i * kStepK);
     multiply(i);
   }
+  if constexpr (ALAY == kCol) {
+    const int lane = threadIdx.x & (kWave - 1);
+    if (summing && lane < 32) {   // a lane has one m, every n alike
+      float* const to = g.splits > 1 ? g.partial + (int64_t)g.splits * g.m * g.partial_stride + (int64_t)blockIdx.y * g.m : g.sums;
+#pragma unroll
+      for (int c = 0; c < TM; ++c) {
+        const int m = at.m0 + wm + 32 * c + lane;
+        if (m < g.m) to[m] = sums[c][0];
+      }
+    }
+  }
   __syncthreads();
   write_out<BM, BN, WM, WN>(g, acc, at.m0, at.n0, pb[0], pb[1], pa[0], pa[1]);
 }
@@ -719,7 +786,16 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs g) {
   const Epilogue& e = g.e;
   const int runs = (int)(g.partial_stride / kRun);
   const int64_t total = (int64_t)g.m * runs, i = block_of() * 256 + threadIdx.x;
-  if (i >= total) return;   // whole quads
+  if (i >= total) {   // whole quads
+    const int64_t m = i - total;
+    if (g.sums && m < g.m) {
+      const float* const from = g.partial + (int64_t)g.splits * g.m * g.partial_stride + m;
+      float sum = 0.0f;
+      for (int s = 0; s < g.splits; ++s) sum += from[(int64_t)s * g.m];
+      g.sums[m] = sum;
+    }
+    return;
+  }
   const int64_t row = i / runs;
   const int col = (int)(i - row * runs) * kRun, n = g.n - col;
   float v[kRun] = {};
@@ -771,7 +847,7 @@ inline LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, Loading how, int 
   p.splits = (int)(steps ? ceil_div(steps, each) : 1);
   p.split_k = (int)(each * kStepK);
   p.partial_stride = ceil_div(n, MOC_BLOCK) * MOC_BLOCK;
-  p.work_bytes = p.splits > 1 ? p.splits * m * p.partial_stride * (int64_t)sizeof(float) : 0;
+  p.work_bytes = p.splits > 1 ? p.splits * m * (p.partial_stride + 1) * (int64_t)sizeof(float) : 0;
   return p;
 }
 
@@ -815,9 +891,10 @@ LinearKernel pick_linear(int tile_m, Loading how) {
   return linear_ring_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, HELD, false>;
 }
 
-// Queues the product: `g` has the operands, sizes and epilogue; held: b's type.
+// Queues the product: `g` has the operands, sizes and epilogue; held: b's type.  g.sums is left out, and set to
+// null, where the kernel does not take them.
 template <int ALAY, int BLAY, bool KEPT>
-int queue_linear(LinearArgs g, int type, int held, Loading how, void* work, int64_t work_bytes, void* hip_stream) {
+int queue_linear(LinearArgs& g, int type, int held, Loading how, void* work, int64_t work_bytes, void* hip_stream) {
   int units = 0;
   const int rc = moc_compute_units(&units);
   if (rc != MOC_OK) return rc;
@@ -830,6 +907,7 @@ int queue_linear(LinearArgs g, int type, int held, Loading how, void* work, int6
   g.split_k = p.split_k;
   g.partial = static_cast<float*>(work);
   g.partial_stride = p.partial_stride;
+  if (p.tile_m != 64) g.sums = nullptr;
   LinearKernel kern = nullptr;
   if constexpr (KEPT) {
     if (type == MOC_BF16) {
@@ -848,7 +926,7 @@ int queue_linear(LinearArgs g, int type, int held, Loading how, void* work, int6
   hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(p.tile_m == 256 ? 512 : 256), 0, stream, g);
   MOC_HIP(hipGetLastError());
   if (p.splits > 1) {
-    hipLaunchKernelGGL(linear_join_kernel, grid_of(ceil_div(g.m * (p.partial_stride / kRun), 256)), dim3(256), 0, stream, g);
+    hipLaunchKernelGGL(linear_join_kernel, grid_of(ceil_div(g.m * (p.partial_stride / kRun) + (g.sums ? g.m : 0), 256)), dim3(256), 0, stream, g);
     MOC_HIP(hipGetLastError());
   }
   return MOC_OK;

@@ -3,7 +3,7 @@
 
 namespace {
 
-// db: a column sum of dy, bound by memory.  A workgroup has 512 columns, eight a lane, and a stretch of
+// db where the product does not take it along: a column sum of dy, bound by memory.  A workgroup has 512 columns, eight a lane, and a stretch of
 // rows, which its four waves take in turn, four at a time; where the rows are cut into several
 // stretches their sums meet in the workspace and are added in order.
 constexpr int kBiasCols = kWave * kRun, kBiasWaves = 4;
@@ -57,8 +57,10 @@ extern "C" int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cou
   int units = 0;
   const int asked = moc_compute_units(&units);
   if (asked != MOC_OK) return asked;
+  bool summed = false;
   if (cin > 0) {
     LinearArgs g = {};
+    g.sums = db;
     g.a = operand_of(dy);
     g.b = operand_of(x);
     g.m = (int)cout;
@@ -68,8 +70,9 @@ extern "C" int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cou
     const bool direct = direct_ok(dy, cout) && (is_kept(x->type) ? kept_direct_ok(x, cin) : direct_ok(x, cin));
     const int rc = queue_linear<kCol, kCol, true>(g, dy->type, x->type, loading_of(direct, cout, cin), work, work_bytes, hip_stream);
     if (rc != MOC_OK) return rc;
+    summed = g.sums != nullptr;
   }
-  if (db) {
+  if (db && !summed) {
     const int64_t stretches = moc_bias_stretches(rows, cout, units);
     if (stretches > 1 && (!work || !aligned_to(work, 16) || work_bytes < stretches * cout * (int64_t)sizeof(float))) return MOC_EINVAL;
     BiasArgs g = {};
