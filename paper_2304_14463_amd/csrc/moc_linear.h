@@ -12,7 +12,7 @@
 // multiplied, the loads of the next run straight into the other.
 #pragma once
 
-#include <type_traits>
+#include <algorithm>
 
 #include "moc_training.h"
 
@@ -38,7 +38,7 @@ __device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
 }
 
 enum { kRow = 0, kCol = 1 };                       // how an operand lies
-enum Loading { kDirect, kThroughRegisters, kNarrow };   // how operands get to LDS; kNarrow: some have rows of fewer than eight
+enum Loading { kDirect, kThroughRegisters, kNarrow };   // how operands can get to LDS; kNarrow: some have rows of fewer than eight
 
 struct Operand {
   const void* data;
@@ -196,7 +196,6 @@ template <int LAY, int WIDTH, int THREADS, int TYPE, int HELD, bool NARROW = fal
 struct RegisterLoader {
   using T = Tile<LAY, WIDTH, THREADS>;
   using V = typename Stored<TYPE>::type;
-  static constexpr int kLoads = 0, kWork = 0, kWrites = 0;   // left to the scheduler
   static constexpr bool kKept = HELD == MOC_E4M3 || HELD == MOC_I8;
   // A step's part of this thread: 16-bit values, or eight codes and their scale.
   struct Set {
@@ -205,14 +204,13 @@ struct RegisterLoader {
   };
   static constexpr int kBytes = kKept ? 1 : 2;   // of a value
   Operand x;
-  int first, extent, end, next;
+  int first, extent, end;
   // Where pieces lie from the tile's first row on, for k = 0 and in 32 bits: the address of a load is then
   // one in scalar registers that moves with k, and this.  Room for a run that is moved down (kRow).
   static constexpr uint32_t kRoom = kRun * kBytes;
   uint32_t place[T::kEach], scale_place[kKept ? T::kEach : 1];
-  Set own;
 
-  __device__ __forceinline__ RegisterLoader(const Operand& x_, int first_, int extent_, int begin, int end_) : x(x_), first(first_), extent(extent_), end(end_), next(begin) {
+  __device__ __forceinline__ RegisterLoader(const Operand& x_, int first_, int extent_, int end_) : x(x_), first(first_), extent(extent_), end(end_) {
     static_assert(!kKept || LAY == kCol);
 #pragma unroll
     for (int i = 0; i < T::kEach; ++i) {
@@ -266,16 +264,16 @@ struct RegisterLoader {
       }
     }
   }
-  // Pieces from `from` on, below `to`, of what was loaded for k.
-  __device__ __forceinline__ void put(const Set& s, int k, Lds* lds, int from, int to) const {
+  // What was loaded for k.
+  __device__ __forceinline__ void put(const Set& s, int k, Lds* lds) const {
     const bool edge = k + kStepK > end || (LAY == kCol && first + WIDTH > extent);   // the same for all
     if (!edge) {
 #pragma unroll
-      for (int i = from; i < to; ++i) put_piece(s, i, s.w[i], lds);
+      for (int i = 0; i < T::kEach; ++i) put_piece(s, i, s.w[i], lds);
       return;
     }
 #pragma unroll
-    for (int i = from; i < to; ++i) {
+    for (int i = 0; i < T::kEach; ++i) {
       uint64_t v[kKept ? 1 : 2];
       __builtin_memcpy(v, s.w[i], sizeof v);
       const int n = LAY == kCol && k + T::row(i) >= end ? 0 : length() - (LAY == kRow ? k : first) - T::piece(i) * kRun;   // that exist
@@ -312,13 +310,6 @@ struct RegisterLoader {
     }
     *(__attribute__((address_space(3))) u32x4*)(lds + (i * THREADS + (int)threadIdx.x) * 16) = out;
   }
-  // One step after the other.
-  __device__ __forceinline__ void load(Lds*) {
-    if (next < end) load(own, next);
-    next += kStepK;
-  }
-  __device__ __forceinline__ void put(Lds* to, int h) const { put(own, next - kStepK, to, h * T::kEach / 2, (h + 1) * T::kEach / 2); }
-  __device__ __forceinline__ void mend(Lds*) {}
 };
 
 // A checkpoint whose rows and strides are multiples of 16: a thread has the 32 values of a block in one
@@ -483,7 +474,7 @@ __device__ __forceinline__ void write_out(const LinearArgs& g, const f32x16 (&ac
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   constexpr int TH = TM < 2 ? TM : 2, kCols = TN * 32, kChunks = kCols / 4, kMove = kChunks < 16 ? kChunks - 1 : 15;
   constexpr int kStage = TH * 32 * kCols * 4, kPer = BN * kRowBytes / kStage;   // waves that one of the arrays has room for
-  static_assert(BM <= BN && kPer >= 1 && (kPer >= WM * WN || (BM == BN && 4 * kPer >= WM * WN)));
+  static_assert(kPer >= 1 && (kPer >= WM * WN || (2 * kPer >= WM * WN && BM <= BN) || (BM >= BN && 4 * kPer >= WM * WN)));
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   const int array = wave / kPer;
   Lds* const stage = (array == 0 ? s0 : array == 1 ? s1 : array == 2 ? s2 : s3) + wave % kPer * kStage;
@@ -538,14 +529,14 @@ __device__ __forceinline__ void write_out(const LinearArgs& g, const f32x16 (&ac
 
 // ---- the kernel ---------------------------------------------------------------------------------
 
-template <int TYPE, int LAY, int WIDTH, int THREADS, Loading LOAD, int HELD>
-struct PickB { using type = RegisterLoader<LAY, WIDTH, THREADS, TYPE, HELD>; };
+template <int TYPE, int LAY, int WIDTH, int THREADS, int HELD>
+struct PickB;
 template <int TYPE, int LAY, int WIDTH, int THREADS>
-struct PickB<TYPE, LAY, WIDTH, THREADS, kDirect, TYPE> { using type = DirectLoader<LAY, WIDTH, THREADS>; };
+struct PickB<TYPE, LAY, WIDTH, THREADS, TYPE> { using type = DirectLoader<LAY, WIDTH, THREADS>; };
 template <int TYPE, int WIDTH, int THREADS>
-struct PickB<TYPE, kCol, WIDTH, THREADS, kDirect, MOC_E4M3> { using type = KeptLoader<WIDTH, THREADS, TYPE, MOC_E4M3>; };
+struct PickB<TYPE, kCol, WIDTH, THREADS, MOC_E4M3> { using type = KeptLoader<WIDTH, THREADS, TYPE, MOC_E4M3>; };
 template <int TYPE, int WIDTH, int THREADS>
-struct PickB<TYPE, kCol, WIDTH, THREADS, kDirect, MOC_I8> { using type = KeptLoader<WIDTH, THREADS, TYPE, MOC_I8>; };
+struct PickB<TYPE, kCol, WIDTH, THREADS, MOC_I8> { using type = KeptLoader<WIDTH, THREADS, TYPE, MOC_I8>; };
 
 // Has the scheduler put a read from LDS behind each product, as long as there are any, then the loads
 // into it, evenly; and `WORK` vector instructions and the writes to LDS that follow from them.
@@ -564,7 +555,7 @@ __device__ __forceinline__ void interleave() {
 }
 
 // TYPE of the operands; HELD: of b, TYPE or a checkpoint's.
-template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, Loading LOAD, int HELD>
+template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int HELD>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;   // 32 x 32 outputs of a wave
@@ -574,8 +565,8 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
   const int m0 = at.m0, n0 = at.n0;
   const int begin = blockIdx.y * g.split_k, end = min(g.k, begin + g.split_k);
 
-  using LoadA = typename std::conditional<LOAD == kDirect, DirectLoader<ALAY, BM, kThreads>, RegisterLoader<ALAY, BM, kThreads, TYPE, TYPE>>::type;
-  using LoadB = typename PickB<TYPE, BLAY, BN, kThreads, LOAD, HELD>::type;
+  using LoadA = DirectLoader<ALAY, BM, kThreads>;
+  using LoadB = typename PickB<TYPE, BLAY, BN, kThreads, HELD>::type;
   LoadA la(g.a, m0, g.m, begin, end);
   LoadB lb(g.b, n0, g.n, begin, end);
 
@@ -673,11 +664,13 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
   write_out<BM, BN, WM, WN>(g, acc, m0, n0, pb0, pb1, pa0, pa1);
 }
 
-// For products of few or ragged tiles, which wait for memory: every operand goes through registers, four
+// Whether a kernel takes the sums of a along: where its registers have room.
+constexpr bool sums_along(int alay, int bm) { return alay == kCol && bm == 64; }
+
+// For products of few or ragged tiles, which wait for memory: every operand goes through registers, kRing
 // steps of it on their way, so that any alignment does and a short sum is all loaded at once.
-constexpr int kRing = 4;
-template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int HELD, bool NARROW>
-__global__ __launch_bounds__(WM* WN* kWave) void linear_ring_kernel(LinearArgs g) {
+template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int kRing, int HELD, bool NARROW>
+__global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
   constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
   __shared__ __attribute__((aligned(1024))) uint8_t a0[BM * kRowBytes], a1[BM * kRowBytes], b0[BN * kRowBytes], b1[BN * kRowBytes];
@@ -685,8 +678,8 @@ __global__ __launch_bounds__(WM* WN* kWave) void linear_ring_kernel(LinearArgs g
   const int begin = blockIdx.y * g.split_k, end = min(g.k, begin + g.split_k);
   using LoadA = RegisterLoader<ALAY, BM, kThreads, TYPE, TYPE, NARROW>;
   using LoadB = RegisterLoader<BLAY, BN, kThreads, TYPE, HELD, NARROW>;
-  const LoadA la(g.a, at.m0, g.m, begin, end);
-  const LoadB lb(g.b, at.n0, g.n, begin, end);
+  const LoadA la(g.a, at.m0, g.m, end);
+  const LoadB lb(g.b, at.n0, g.n, end);
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   const Reader<ALAY, BM, TM> ra(wm);
   const Reader<BLAY, BN, TN> rb(wn);
@@ -715,14 +708,15 @@ __global__ __launch_bounds__(WM* WN* kWave) void linear_ring_kernel(LinearArgs g
   }
   // Two buffers and a barrier a step: what is put into one was last read before the barrier in between.
   const auto put = [&](int i, int k) {
-    la.put(sa[i], k, pa[i & 1], 0, LoadA::T::kEach);
-    lb.put(sb[i], k, pb[i & 1], 0, LoadB::T::kEach);
+    la.put(sa[i], k, pa[i & 1]);
+    lb.put(sb[i], k, pb[i & 1]);
   };
   // Sums of a over k, by products with ones: in the first column of tiles, of the waves at its start.
-  const bool summing = ALAY == kCol && g.sums && at.n0 == 0 && wn == 0;
+  constexpr bool kSums = sums_along(ALAY, BM);
+  const bool summing = kSums && g.sums && at.n0 == 0 && wn == 0;
   const uint16_t one = TYPE == MOC_BF16 ? 0x3F80 : 0x3C00;
   const s16x8 ones = {(short)one, (short)one, (short)one, (short)one, (short)one, (short)one, (short)one, (short)one};
-  f32x16 sums[ALAY == kCol ? TM : 1];
+  f32x16 sums[kSums ? TM : 1];
 #pragma unroll
   for (f32x16& x : sums)
 #pragma unroll
@@ -742,7 +736,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void linear_ring_kernel(LinearArgs g
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[c][j] = mfma<TYPE>(fb[j], fa[s][c], acc[c][j]);
     }
-    if constexpr (ALAY == kCol) {
+    if constexpr (kSums) {
       if (summing) {
 #pragma unroll
         for (int s = 0; s < kStepK / 16; ++s)
@@ -766,7 +760,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void linear_ring_kernel(LinearArgs g
     put(i, k + i * kStepK);
     multiply(i);
   }
-  if constexpr (ALAY == kCol) {
+  if constexpr (kSums) {
     const int lane = threadIdx.x & (kWave - 1);
     if (summing && lane < 32) {   // a lane has one m, every n alike
       float* const to = g.splits > 1 ? g.partial + (int64_t)g.splits * g.m * g.partial_stride + (int64_t)blockIdx.y * g.m : g.sums;
@@ -813,37 +807,60 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearArgs g) {
 
 // ---- dispatch -----------------------------------------------------------------------------------
 
+// The kernels: linear_kernel (operands straight into LDS) and linear_ring_kernel (through registers).
+enum Shape { kDirect128, kDirect256, kRing64, kRing256, kRingNarrow };
+struct ShapeSize {
+  int tile, threads;
+};
+constexpr ShapeSize kShapes[] = {{128, 256}, {256, 512}, {64, 256}, {256, 512}, {64, 256}};
+
 // How a product is cut up.
 struct LinearPlan {
-  int tile_m, tile_n;
+  Shape shape;
   int tiles_m, tiles_n, splits, split_k;
   int64_t partial_stride, work_bytes;
 };
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-inline LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, Loading how, int units) {
-  LinearPlan p = {};
-  if (how == kNarrow) {
-    p.tile_m = p.tile_n = 64;
-  } else if (m <= 32) {
-    p.tile_m = 32;
-    p.tile_n = 128;
-  } else if (how == kDirect && ceil_div(m, 256) * ceil_div(n, 256) * 4 >= 3 * (int64_t)units) {
-    p.tile_m = p.tile_n = 256;
-  } else if (ceil_div(m, 128) * ceil_div(n, 128) >= 2 * (int64_t)units) {
-    p.tile_m = p.tile_n = 128;
-  } else {
-    p.tile_m = p.tile_n = 64;
+// Microseconds that a product takes in tiles of a shape with k cut into `splits`, as measured over 30 sizes from 1 x 1000 x
+// 1000 to 16384 x 8192 x 2048 in all three layouts (`cols`: how many operands lie in columns).  A step of a workgroup of
+// 64 x 64 takes 0.27 us and 0.1 more for an operand in columns, waiting for memory, or 0.25 (0.36 of ragged rows) for each
+// of those that share a compute unit; of 128 x 128 0.65 (two in columns: 0.95) and 0.7 (1.0); 256 x 256 have a unit to
+// themselves, 1.85 (2.0), through registers 2.2 (2.8).  Cutting k costs a launch and the sums, written and read.
+inline double linear_cost(Shape shape, int64_t m, int64_t n, int64_t k, int cols, bool ragged, int64_t splits, int units) {
+  const double groups = (double)(ceil_div(m, kShapes[shape].tile) * ceil_div(n, kShapes[shape].tile) * splits) / units;
+  const double steps = (double)ceil_div(ceil_div(k, kStepK), splits), rounds = groups > (int64_t)groups ? (double)((int64_t)groups + 1) : groups;
+  const bool columns = cols == 2;
+  double at = 0.0;
+  switch (shape) {
+    case kDirect128: at = steps * std::max(columns ? 0.95 : 0.65, (columns ? 1.0 : 0.7) * groups); break;
+    case kDirect256: at = steps * rounds * (columns ? 2.0 : 1.85); break;
+    case kRing256: at = steps * rounds * (columns ? 2.8 : 2.2); break;
+    default: at = steps * std::max(0.27 + 0.1 * cols, (ragged ? 0.36 : 0.25) * groups); break;
   }
-  p.tiles_m = (int)ceil_div(m, p.tile_m);
-  p.tiles_n = (int)ceil_div(n, p.tile_n);
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, steps = ceil_div(k, kStepK);
-  // Few tiles: k is cut too, at least four steps a split, until every compute unit has the workgroups that it holds.
-  int64_t splits = tiles ? (p.tile_m == 256 ? 1 : p.tile_m == 64 ? 4 : 2) * (int64_t)units / tiles : 1;
-  if (splits > steps / 4) splits = steps / 4;
-  if (splits < 1) splits = 1;
-  const int64_t each = ceil_div(steps, splits);
+  at = std::max(at, ((double)m * k + (double)n * k) * 2 / 5.5e6);   // memory
+  return at + (splits > 1 ? 5.0 + (double)splits * m * n * 8 / 4e6 : 0.0);
+}
+
+inline LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, int cols, Loading how, int units) {
+  LinearPlan p = {};
+  const int64_t steps = ceil_div(k, kStepK);
+  double best = 0.0;
+  p.splits = 0;
+  for (const Shape shape : {kDirect256, kDirect128, kRing256, kRing64, kRingNarrow}) {
+    if ((shape == kRingNarrow) != (how == kNarrow) || (shape <= kDirect256 && how != kDirect) || (shape == kRing256 && how == kDirect)) continue;
+    for (int64_t splits = 1; splits <= 32 && (splits == 1 || steps / splits >= 4); splits += splits < 4 ? 1 : splits / 2) {
+      const double cost = linear_cost(shape, m, n, k, cols, how != kDirect, splits, units);
+      if (p.splits && cost >= best) continue;
+      best = cost;
+      p.shape = shape;
+      p.splits = (int)splits;
+    }
+  }
+  p.tiles_m = (int)ceil_div(m, kShapes[p.shape].tile);
+  p.tiles_n = (int)ceil_div(n, kShapes[p.shape].tile);
+  const int64_t each = ceil_div(steps, p.splits);
   p.splits = (int)(steps ? ceil_div(steps, each) : 1);
   p.split_k = (int)(each * kStepK);
   p.partial_stride = ceil_div(n, MOC_BLOCK) * MOC_BLOCK;
@@ -879,16 +896,15 @@ inline int64_t moc_bias_stretches(int64_t rows, int64_t cout, int units) {
 using LinearKernel = void (*)(LinearArgs);
 
 template <int TYPE, int ALAY, int BLAY, int HELD>
-LinearKernel pick_linear(int tile_m, Loading how) {
-  if (how == kNarrow) return linear_ring_kernel<TYPE, ALAY, BLAY, 64, 64, 2, 2, HELD, true>;
-  if (tile_m == 64) return linear_ring_kernel<TYPE, ALAY, BLAY, 64, 64, 2, 2, HELD, false>;
-  if (how == kDirect) {
-    if (tile_m == 256) return linear_kernel<TYPE, ALAY, BLAY, 256, 256, 2, 4, kDirect, HELD>;
-    if (tile_m == 128) return linear_kernel<TYPE, ALAY, BLAY, 128, 128, 2, 2, kDirect, HELD>;
-    return linear_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, kDirect, HELD>;
+LinearKernel pick_linear(Shape shape) {
+  switch (shape) {
+    case kDirect128: return linear_kernel<TYPE, ALAY, BLAY, 128, 128, 2, 2, HELD>;
+    case kDirect256: return linear_kernel<TYPE, ALAY, BLAY, 256, 256, 2, 4, HELD>;
+    case kRing64: return linear_ring_kernel<TYPE, ALAY, BLAY, 64, 64, 2, 2, 4, HELD, false>;
+    case kRing256: return linear_ring_kernel<TYPE, ALAY, BLAY, 256, 256, 2, 4, 2, HELD, false>;
+    case kRingNarrow: return linear_ring_kernel<TYPE, ALAY, BLAY, 64, 64, 2, 2, 4, HELD, true>;
   }
-  if (tile_m == 128) return linear_kernel<TYPE, ALAY, BLAY, 128, 128, 2, 2, kThroughRegisters, HELD>;
-  return linear_ring_kernel<TYPE, ALAY, BLAY, 32, 128, 1, 4, HELD, false>;
+  return nullptr;
 }
 
 // Queues the product: `g` has the operands, sizes and epilogue; held: b's type.  g.sums is left out, and set to
@@ -898,7 +914,7 @@ int queue_linear(LinearArgs& g, int type, int held, Loading how, void* work, int
   int units = 0;
   const int rc = moc_compute_units(&units);
   if (rc != MOC_OK) return rc;
-  const LinearPlan p = linear_plan(g.m, g.n, g.k, how, units);
+  const LinearPlan p = linear_plan(g.m, g.n, g.k, (ALAY == kCol) + (BLAY == kCol), how, units);
   if (p.work_bytes > 0 && (!work || !aligned_to(work, 16) || work_bytes < p.work_bytes)) return MOC_EINVAL;
   if ((int64_t)p.tiles_m * p.tiles_n > (1 << 22)) return MOC_EOVERFLOW;   // a launch's threads
   g.tiles_m = p.tiles_m;
@@ -907,23 +923,23 @@ int queue_linear(LinearArgs& g, int type, int held, Loading how, void* work, int
   g.split_k = p.split_k;
   g.partial = static_cast<float*>(work);
   g.partial_stride = p.partial_stride;
-  if (p.tile_m != 64) g.sums = nullptr;
+  if (kShapes[p.shape].tile != 64) g.sums = nullptr;
   LinearKernel kern = nullptr;
   if constexpr (KEPT) {
     if (type == MOC_BF16) {
-      kern = held == MOC_E4M3 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_E4M3>(p.tile_m, how)
-             : held == MOC_I8 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_I8>(p.tile_m, how)
-                              : pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, how);
+      kern = held == MOC_E4M3 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_E4M3>(p.shape)
+             : held == MOC_I8 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_I8>(p.shape)
+                              : pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.shape);
     } else {
-      kern = held == MOC_E4M3 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_E4M3>(p.tile_m, how)
-             : held == MOC_I8 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_I8>(p.tile_m, how)
-                              : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, how);
+      kern = held == MOC_E4M3 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_E4M3>(p.shape)
+             : held == MOC_I8 ? pick_linear<MOC_F16, ALAY, BLAY, MOC_I8>(p.shape)
+                              : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.shape);
     }
   } else {
-    kern = type == MOC_BF16 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.tile_m, how) : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.tile_m, how);
+    kern = type == MOC_BF16 ? pick_linear<MOC_BF16, ALAY, BLAY, MOC_BF16>(p.shape) : pick_linear<MOC_F16, ALAY, BLAY, MOC_F16>(p.shape);
   }
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(p.tile_m == 256 ? 512 : 256), 0, stream, g);
+  hipLaunchKernelGGL(kern, dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), dim3(kShapes[p.shape].threads), 0, stream, g);
   MOC_HIP(hipGetLastError());
   if (p.splits > 1) {
     hipLaunchKernelGGL(linear_join_kernel, grid_of(ceil_div(g.m * (p.partial_stride / kRun) + (g.sums ? g.m : 0), 256)), dim3(256), 0, stream, g);

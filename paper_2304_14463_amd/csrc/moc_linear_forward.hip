@@ -47,8 +47,8 @@ int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout) {
   int64_t most = cout > 0 ? moc_bias_stretches(rows, cout, units) * cout * (int64_t)sizeof(float) : 0;
   for (const Loading how : {kDirect, kThroughRegisters, kNarrow}) {
     const int64_t sizes[3][3] = {{rows, cout, cin}, {rows, cin, cout}, {cout, cin, rows}};
-    for (const auto& s : sizes) {
-      const int64_t bytes = linear_plan(s[0], s[1], s[2], how, units).work_bytes;
+    for (int cols = 0; cols < 3; ++cols) {
+      const int64_t bytes = linear_plan(sizes[cols][0], sizes[cols][1], sizes[cols][2], cols, how, units).work_bytes;
       most = bytes > most ? bytes : most;
     }
   }
