@@ -722,7 +722,6 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArg
 #pragma unroll
     for (int r = 0; r < 16; ++r) x[r] = 0.0f;
   const auto multiply = [&](int i) {
-    __syncthreads();   // waits for what was put, not for loads
     s16x8 fa[kStepK / 16][TM];
 #pragma unroll
     for (int s = 0; s < kStepK / 16; ++s) {
@@ -745,20 +744,30 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArg
       }
     }
   };
-  int k = begin;
-  for (; k + (kRing - 1) * kStepK < end; k += kRing * kStepK) {
-#pragma unroll
-    for (int i = 0; i < kRing; ++i) {
-      put(i, k + i * kStepK);
-      load(i, k + (i + kRing) * kStepK);
-      multiply(i);
+  // A step is put while the one before is multiplied.
+  const auto step = [&](int i, int k, bool more) {
+    const int next = (i + 1) % kRing;
+    if (more) {
+      put(next, k + kStepK);
+      load(next, k + (kRing + 1) * kStepK);
     }
+    multiply(i);
+    __syncthreads();   // waits for what was put, not for loads
+  };
+  int k = begin;
+  if (begin < end) {
+    put(0, begin);
+    load(0, begin + kRing * kStepK);
+    __syncthreads();
+  }
+  for (; k + kRing * kStepK < end; k += kRing * kStepK) {
+#pragma unroll
+    for (int i = 0; i < kRing; ++i) step(i, k + i * kStepK, true);
   }
 #pragma unroll
-  for (int i = 0; i < kRing - 1; ++i) {
+  for (int i = 0; i < kRing; ++i) {
     if (k + i * kStepK >= end) break;
-    put(i, k + i * kStepK);
-    multiply(i);
+    step(i, k + i * kStepK, k + (i + 1) * kStepK < end);
   }
   if constexpr (kSums) {
     const int lane = threadIdx.x & (kWave - 1);
@@ -771,7 +780,6 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArg
       }
     }
   }
-  __syncthreads();
   write_out<BM, BN, WM, WN>(g, acc, at.m0, at.n0, pb[0], pb[1], pa[0], pa[1]);
 }
 

@@ -3,9 +3,14 @@
 // Bound by memory: every value is read once and written once.  T threads take a row and hold it in
 // registers, CH runs of eight values each, so the variance is that of the differences from the mean
 // and nothing is read again; rows longer than 16384 columns are read again from cache.  A wave a row
-// up to 512 columns (no barrier), then the fewest threads that hold it.  Workgroups go over many rows:
-// gamma and beta stay in registers, and in the backward pass so do a column's two sums; they meet in
-// the workspace, one row of sums a workgroup, and a second kernel adds those in their order.
+// up to 1024 columns (no barrier: 65536 x 1024 forward 77 -> 53 us, 5.0 TB/s), then 256 threads, then two
+// runs a thread in the forward pass (32768 x 4096 bf16 116 us, 4.6 TB/s, and 139, 4.9, with an e4m3
+// checkpoint; one run and two rows at a time 124 and 174).  The backward pass has no registers for two:
+// 153 us, 5.3 TB/s, against 226.  The last run of a ragged row is loaded whole and moved down when it is
+// used, since a load in parts would be waited for (4999 x 1247, backward from int8: 32 -> 25 us).
+// Workgroups go over many rows: gamma and beta stay in registers, and in the backward pass so do a
+// column's two sums; they meet in the workspace, one row of sums a workgroup, and a second kernel adds
+// those in their order.
 #include "moc_training.h"
 
 namespace {
@@ -110,11 +115,13 @@ __device__ __forceinline__ void load_x(const NormArgs& g, int64_t row, int col, 
 }
 __device__ __forceinline__ bool whole_runs(const NormArgs& g) { return g.cols % kRun == 0; }
 
-// 1 / sqrt(x), 1 ulp, subnormal arguments too.
+// 1 / sqrt(x), subnormal arguments too: the hardware's, 1 ulp off, and a step of Newton's method, which leaves
+// little but the last rounding (an error of rstd moves a whole row's values, and codes of its checkpoint with them).
 __device__ __forceinline__ float inverse_root(float x) {
   const bool small = x < 0x1p-100f;
-  const float r = __builtin_amdgcn_rsqf(small ? x * 0x1p64f : x);
-  return small ? r * 0x1p32f : r;
+  const float a = small ? x * 0x1p64f : x, r = __builtin_amdgcn_rsqf(a);
+  const float better = __builtin_fmaf(0.5f * r, __builtin_fmaf(-a * r, r, 1.0f), r), root = r > 0.0f && r < kInf ? better : r;
+  return small ? root * 0x1p32f : root;
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -137,7 +144,7 @@ template <int X, int T, int CH>
 __device__ __forceinline__ void load_row(const NormArgs& g, int64_t row, int lane, Raw (&w)[CH]) {
   const void* const x = row_of<X>(g.x, row, g.x_stride);
   const uint8_t* const scales = g.x_scales + row * g.x_scale_stride;
-  if (whole_runs(g)) {
+  if (g.cols >= kRun) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) w[c] = load_raw_whole<X>(x, scales, (c * T + lane) * kRun, g.cols);
   } else {
@@ -148,7 +155,7 @@ __device__ __forceinline__ void load_row(const NormArgs& g, int64_t row, int lan
 
 // Workgroups go over rows with gamma and beta in registers (from cache they would be four times the
 // bytes of a row), R rows at a time, whose sums are taken together, and the next R on their way.  16
-// waves a compute unit at least.
+// waves a compute unit; 32 gain 6 % at 1024 columns and lose 10 % at 2048.
 template <int X, int T, int CH, int R>
 __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_forward_kernel(NormArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;   // groups of R rows of a workgroup at a time
@@ -181,6 +188,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_forward_kernel(Norm
       mean[r] = 0.0f;
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
+        if (!whole) settle<X>(w[r][c], (c * T + lane) * kRun, g.cols);
         values_of<X>(w[r][c], v[r][c]);
         float s = 0.0f;   // 0 where a row ends inside a run
 #pragma unroll
@@ -251,7 +259,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_forward_long_kernel(NormArgs
       for (int i = 0; i < kRun; ++i) q[0] += i < g.cols - col ? (v[i] - mean) * (v[i] - mean) : 0.0f;
     }
     sums(q);
-    const float rstd = 1.0f / __builtin_sqrtf(q[0] / count + g.eps);
+    const float rstd = inverse_root(q[0] / count + g.eps);
     if (threadIdx.x == 0) {
       g.mean[row] = mean;
       g.rstd[row] = rstd;
@@ -290,7 +298,7 @@ __device__ __forceinline__ GradRaw load_grad(const NormArgs& g, int64_t row, int
 }
 template <int X, int D, int T, int CH>
 __device__ __forceinline__ void load_grads(const NormArgs& g, int64_t row, int lane, GradRaw (&w)[CH]) {
-  if (whole_runs(g)) {
+  if (g.cols >= kRun) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) w[c] = load_grad<X, D, true>(g, row, (c * T + lane) * kRun);
   } else {
@@ -379,7 +387,7 @@ __device__ __forceinline__ void store_sums(const NormArgs& g, const float (&sg)[
 // 16 waves a compute unit, 128 registers a thread.  The next row is on its way while the sums over this
 // one are taken.
 template <int X, int D, int T, int CH>
-__global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(NormArgs g) {
+__global__ __launch_bounds__(T < 256 ? 256 : T, CH > 1 && T == kWave ? 3 : 4) void norm_backward_kernel(NormArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
   static_assert(T <= kWave || kRows == 1);
   using Sums = RowSums<T, 2>;
@@ -387,22 +395,26 @@ __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(Nor
   Sums sums{room};
   __shared__ float stage[kRows > 1 ? kRows * 16 * T : 1];
   const int lane = threadIdx.x % T;
-  constexpr bool kHold = CH == 1;   // gamma, in registers; from cache where two runs leave none
-  float held[kRun], sg[CH][kRun], sb[CH][kRun];
+  constexpr bool kHold = CH == 1 || T == kWave;   // gamma, in registers; from cache where two runs leave none
+  float held[CH][kRun], sg[CH][kRun], sb[CH][kRun];
   const auto gamma_of = [&](int c, float(&ga)[kRun]) {
     const int col = (c * T + lane) * kRun;
     load_param(g.gamma, g.param_type, min(col, g.cols - 1), g.cols - col, 1.0f, ga);
   };
-  if constexpr (kHold) gamma_of(0, held);
+  if constexpr (kHold) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) gamma_of(c, held[c]);
+  }
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
 #pragma unroll
     for (int i = 0; i < kRun; ++i) sg[c][i] = sb[c][i] = 0.0f;
   }
   const float part = 1.0f / (float)g.cols;
+  const bool whole = whole_runs(g);
   const int64_t step = (int64_t)gridDim.x * kRows;
   int64_t row = (int64_t)blockIdx.x * kRows + (kRows > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / T) : 0);
-  constexpr bool kAhead = CH == 1;   // two runs a thread: no registers for it
+  constexpr bool kAhead = CH == 1 || T == kWave;   // two runs a thread: no registers for it
   GradRaw w[CH];
   float mean = 0.0f, rstd = 0.0f;
   if (kAhead && row < g.rows) {
@@ -420,6 +432,15 @@ __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(Nor
     GradRaw now[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) now[c] = w[c];
+    if (!whole) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const int col = (c * T + lane) * kRun;
+        settle<X>(now[c].x, col, g.cols);
+        settle<D>(now[c].d, col, g.cols);
+        settle<D>(now[c].r, col, g.cols);
+      }
+    }
     const float mu = mean, scale = rstd;
     const int64_t next = row + step;
     if (kAhead && next < g.rows) {
@@ -435,7 +456,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(Nor
       if constexpr (!kHold) gamma_of(c, ga);
 #pragma unroll
       for (int i = 0; i < kRun; ++i) {
-        if constexpr (kHold) ga[i] = held[i];
+        if constexpr (kHold) ga[i] = held[c][i];
         const float p = d[i] * ga[i];
         m[0] += p;
         m[1] += p * h[i];
@@ -456,7 +477,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T, 4) void norm_backward_kernel(Nor
       if constexpr (!kHold) gamma_of(c, ga);
 #pragma unroll
       for (int i = 0; i < kRun; ++i)
-        if constexpr (kHold) ga[i] = held[i];
+        if constexpr (kHold) ga[i] = held[c][i];
       store_dx<D>(g, row, (c * T + lane) * kRun, scale, a, b, h, d, ga, now[c].r);
     }
     row = next;
@@ -528,9 +549,10 @@ struct Shape {
 template <int X>
 Shape forward_shape(int64_t cols) {
   if (cols <= 512) return {norm_forward_kernel<X, 64, 1, 2>, 256, 8};
+  if (cols <= 1024) return {norm_forward_kernel<X, 64, 2, 2>, 256, 8};
   if (cols <= 2048) return {norm_forward_kernel<X, 256, 1, 2>, 256, 2};
-  if (cols <= 4096) return {norm_forward_kernel<X, 512, 1, 2>, 512, 2};
-  if (cols <= 8192) return {norm_forward_kernel<X, 1024, 1, 2>, 1024, 2};
+  if (cols <= 4096) return {norm_forward_kernel<X, 256, 2, 1>, 256, 1};
+  if (cols <= 8192) return {norm_forward_kernel<X, 512, 2, 1>, 512, 1};
   if (cols <= 16384) return {norm_forward_kernel<X, 1024, 2, 1>, 1024, 1};
   return {norm_forward_long_kernel<X>, kMaxThreads, 1};
 }
@@ -546,6 +568,7 @@ Shape forward_shape_of(int type, int64_t cols) {
 template <int X, int D>
 Shape backward_shape(int64_t cols) {
   if (cols <= 512) return {norm_backward_kernel<X, D, 64, 1>, 256, 4};
+  if (cols <= 1024) return {norm_backward_kernel<X, D, 64, 2>, 256, 4};
   if (cols <= 2048) return {norm_backward_kernel<X, D, 256, 1>, 256, 1};
   if (cols <= 4096) return {norm_backward_kernel<X, D, 512, 1>, 512, 1};
   if (cols <= 8192) return {norm_backward_kernel<X, D, 1024, 1>, 1024, 1};

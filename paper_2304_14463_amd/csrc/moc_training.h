@@ -314,11 +314,40 @@ __device__ __forceinline__ Raw load_raw(const void* row, const uint8_t* scales, 
   return x;
 }
 
-// Where every run is whole (a multiple of eight columns): no branch, so that many are under way at once.
-// Beyond the row the last run is read, and not used.
+// Of a row of eight columns at least: no branch, so that many are under way at once.  Beyond the row its
+// last eight are read, and not used; where it ends in a run, too, and settle() moves them down.
 template <int TYPE>
 __device__ __forceinline__ Raw load_raw_whole(const void* row, const uint8_t* scales, int col, int cols) {
-  return load_raw<TYPE>(row, scales, min(col, cols - kRun), kRun);
+  Raw x = load_raw<TYPE>(row, scales, min(col, cols - kRun), kRun);
+  if constexpr (TYPE == MOC_E4M3 || TYPE == MOC_I8) x.scale = scales[min(col, cols - 1) / MOC_BLOCK];
+  return x;
+}
+
+// What load_raw_whole has loaded for `col` becomes that run, with zeros beyond the row.
+template <int TYPE>
+__device__ __forceinline__ void settle(Raw& x, int col, int cols) {
+  const int n = cols - col;
+  if (n >= kRun || n <= 0 || cols < kRun) return;
+  const int down = kRun - n;
+  if constexpr (TYPE == MOC_F32) {
+    uint32_t w[2 * kRun] = {x.a[0], x.a[1], x.a[2], x.a[3], x.b[0], x.b[1], x.b[2], x.b[3]};   // and zeros
+#pragma unroll
+    for (int by = 1; by < kRun; by *= 2)
+#pragma unroll
+      for (int i = 0; i < 2 * kRun - by; ++i) w[i] = down & by ? w[i + by] : w[i];
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) (i < 4 ? x.a : x.b)[i & 3] = w[i];
+  } else {
+    uint64_t lo = x.a[0] | (uint64_t)x.a[1] << 32, hi = x.a[2] | (uint64_t)x.a[3] << 32;
+    if constexpr (TYPE == MOC_E4M3 || TYPE == MOC_I8) {
+      lo >>= 8 * down;
+    } else {
+      const int bits = 16 * down;   // 16 .. 112
+      lo = bits >= 64 ? hi >> (bits - 64) : lo >> bits | hi << (64 - bits);
+      hi = bits >= 64 ? 0 : hi >> bits;
+    }
+    x.a = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+  }
 }
 
 template <int TYPE>
