@@ -16,7 +16,8 @@
  * `stride` elements apart (stride >= cols).  Every alignment to the element's
  * size is taken; the matrix products load 16 bytes at a time straight into
  * LDS where operands start on 16 bytes and strides and contiguous sizes are
- * multiples of 8 elements, and through registers otherwise.
+ * multiples of 8 elements, and through registers otherwise.  A product of more
+ * than 2^22 tiles is refused with MOC_EOVERFLOW.
  *
  * Checkpoints.  32 consecutive columns of a row share a scale 2^k, held as the
  * byte k + 127 at scales[row * scale_stride + col / 32]; one byte a value, at
