@@ -4,7 +4,7 @@
 // Operands lie in memory either with k running along a row ("row": x and w of the forward pass, dy of
 // the input's gradient) or with m or n running along it ("col": w of the input's gradient, dy and x of
 // the weight's).  Both go to LDS as they lie, 16 bytes a lane, and come out of it as the matrix cores
-// want them: a lane of v_mfma_f32_32x32x16 holds eight consecutive k of one m or n, which a row operand
+// want them: a lane holds eight consecutive k of one m or n, which a row operand
 // has next to each other (one 16-byte read) and a col operand below each other (two reads that
 // transpose 4 x 16 values among 16 lanes, ds_read_b64_tr_b16).
 //
@@ -24,17 +24,35 @@ constexpr int kWindow = 0x7FFFFFF0;             // bytes a buffer descriptor cov
 
 using bf16x8 = __bf16 __attribute__((ext_vector_type(8)));
 using f16x8 = _Float16 __attribute__((ext_vector_type(8)));
-using f32x16 = float __attribute__((ext_vector_type(16)));
+using f32x4 = float __attribute__((ext_vector_type(4)));
 using s16x4 = short __attribute__((ext_vector_type(4)));
 using s16x8 = short __attribute__((ext_vector_type(8)));
-using f32x4 = float __attribute__((ext_vector_type(4)));
+
+// S x S of the result, 512 / S of k: with operands in registers and normally distributed values 16 x 16 x 32 reaches
+// 2.0 PFLOP/s and 32 x 32 x 16, which reads and writes the sums twice as often, 1.3; but it needs half the registers for
+// operands, so it is taken where a loader needs them.
+template <int S> struct Sums;
+template <> struct Sums<16> { using type = float __attribute__((ext_vector_type(4))); };
+template <> struct Sums<32> { using type = float __attribute__((ext_vector_type(16))); };
 
 template <int TYPE>
-__device__ __forceinline__ f32x16 mfma(s16x8 a, s16x8 b, f32x16 c) {
+__device__ __forceinline__ Sums<16>::type mfma(s16x8 a, s16x8 b, Sums<16>::type c) {
+  if constexpr (TYPE == MOC_BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <int TYPE>
+__device__ __forceinline__ Sums<32>::type mfma(s16x8 a, s16x8 b, Sums<32>::type c) {
   if constexpr (TYPE == MOC_BF16)
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   else
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+template <class V>
+__device__ __forceinline__ void clear(V& x) {
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof x / 4); ++i) x[i] = 0.0f;
 }
 
 enum { kRow = 0, kCol = 1 };                       // how an operand lies
@@ -413,36 +431,39 @@ struct KeptLoader {
 
 // ---- LDS to the matrix cores --------------------------------------------------------------------
 
-// 32 x 16 pieces of an operand for one wave, whose m or n start at `first` in the tile.
-template <int LAY, int WIDTH, int COUNT>
+// S x 512 / S pieces of an operand for one wave, whose m or n start at `first` in the tile: a lane has eight k
+// of one m or n, lane % S.
+template <int S, int LAY, int WIDTH, int COUNT>
 struct Reader {
-  int at[COUNT][LAY == kRow ? 4 : 1];
+  static constexpr int kK = 512 / S, kParts = kStepK / kK;
+  static constexpr int kEach = LAY == kRow ? 1 : 2;   // instructions of a read
+  static constexpr int kSame = 32 / S;                // pieces that lie alike: the swizzle moves 32 columns at least
+  int at[LAY == kRow ? 1 : (COUNT + kSame - 1) / kSame][LAY == kRow ? kParts : 1];
 
   __device__ __forceinline__ explicit Reader(int first) {
     const int lane = threadIdx.x & (kWave - 1);
-    if constexpr (LAY == kRow) {
-      const int row = first + (lane & 31);
+    if constexpr (LAY == kRow) {   // 16 rows further on the swizzle is the same
+      const int row = first + lane % S;
 #pragma unroll
-      for (int c = 0; c < COUNT; ++c)
-#pragma unroll
-        for (int s = 0; s < 4; ++s) at[c][s] = (row + 32 * c) * kRowBytes + ((2 * s + (lane >> 5)) ^ swizzle<LAY, WIDTH>(row)) * 16;
+      for (int s = 0; s < kParts; ++s) at[0][s] = row * kRowBytes + ((kK / 8 * s + lane / S) ^ swizzle<LAY, WIDTH>(row)) * 16;
     } else {
-      const int in = lane & 15, k = (lane >> 5) * 8 + (in >> 2);   // swizzle() looks at k % 4 only
+      const int in = lane & 15, k = lane / S * 8 + (in >> 2);   // swizzle() looks at k % 4 only
 #pragma unroll
-      for (int c = 0; c < COUNT; ++c) {
-        const int col = first + 32 * c + ((lane >> 4) & 1) * 16 + (in & 3) * 4;
-        at[c][0] = k * WIDTH * 2 + ((col >> 3) ^ swizzle<LAY, WIDTH>(in >> 2)) * 16 + (col & 7) * 2;
+      for (int c = 0; c < COUNT; c += kSame) {
+        const int col = first + S * c + (lane & (S - 16)) + (in & 3) * 4;
+        at[c / kSame][0] = k * WIDTH * 2 + ((col >> 3) ^ swizzle<LAY, WIDTH>(in >> 2)) * 16 + (col & 7) * 2;
       }
     }
   }
-  // k of 16 * s .. 16 * s + 15
+  // k of kK * s and on
   __device__ __forceinline__ s16x8 read(const Lds* from, int c, int s) const {
     if constexpr (LAY == kRow) {
-      return *(const __attribute__((address_space(3))) s16x8*)(from + at[c][s]);
+      return *(const __attribute__((address_space(3))) s16x8*)(from + at[0][s] + S * c * kRowBytes);
     } else {
       using P = __attribute__((address_space(3))) s16x4*;
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(from + at[c][0] + 16 * s * WIDTH * 2));
-      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(from + at[c][0] + (16 * s + 4) * WIDTH * 2));
+      const Lds* const p = from + at[c / kSame][0] + c % kSame * S * 2 + kK * s * WIDTH * 2;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(p + 4 * WIDTH * 2));
       return s16x8{lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     }
   }
@@ -465,15 +486,15 @@ __device__ __forceinline__ TileAt tile_of(const LinearArgs& g) {
 }
 
 // Out by way of LDS, so that lanes next to each other have runs next to each other and a quad has a
-// block of 32.  A lane has 16 of the 32 n of one m: 8 * (r / 4) + 4 * (lane / 32) + r % 4.  Every
+// block of 32.  A lane has runs of four n of one m, lane % S.  Every
 // wave stages its own outputs, 64 rows at a time, in memory of its own; 16 bytes of a row are moved
-// by the row's number, so that writes (32 rows at once) and reads (whole rows) meet all banks.
+// by the row's number, so that writes (16 rows at once) and reads (whole rows) meet all banks.
 // s0 .. s3: BN, BN, BM and BM rows of an operand's tile, nothing in them still wanted.
-template <int BM, int BN, int WM, int WN>
-__device__ __forceinline__ void write_out(const LinearArgs& g, const f32x16 (&acc)[BM / WM / 32][BN / WN / 32], int m0, int n0, Lds* s0, Lds* s1, Lds* s2, Lds* s3) {
-  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
-  constexpr int TH = TM < 2 ? TM : 2, kCols = TN * 32, kChunks = kCols / 4, kMove = kChunks < 16 ? kChunks - 1 : 15;
-  constexpr int kStage = TH * 32 * kCols * 4, kPer = BN * kRowBytes / kStage;   // waves that one of the arrays has room for
+template <int S, int BM, int BN, int WM, int WN>
+__device__ __forceinline__ void write_out(const LinearArgs& g, const typename Sums<S>::type (&acc)[BM / WM / S][BN / WN / S], int m0, int n0, Lds* s0, Lds* s1, Lds* s2, Lds* s3) {
+  constexpr int TM = BM / WM / S, TN = BN / WN / S;
+  constexpr int TH = TM < 64 / S ? TM : 64 / S, kCols = TN * S, kChunks = kCols / 4, kMove = kChunks < 16 ? kChunks - 1 : 15;
+  constexpr int kStage = TH * S * kCols * 4, kPer = BN * kRowBytes / kStage;   // waves that one of the arrays has room for
   static_assert(kPer >= 1 && (kPer >= WM * WN || (2 * kPer >= WM * WN && BM <= BN) || (BM >= BN && 4 * kPer >= WM * WN)));
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
   const int array = wave / kPer;
@@ -489,8 +510,8 @@ __device__ __forceinline__ void write_out(const LinearArgs& g, const f32x16 (&ac
   Raw ahead[kAhead];
 #pragma unroll
   for (int half = 0; half < TM / TH; ++half) {
-    const int row0 = m0 + wm + half * TH * 32 + lane / kRuns;
-    const auto extra = [&](int at) { return row0 + at * kRowsAt < g.m && at * kRowsAt < TH * 32 && g.splits == 1 ? load_extra(g.e, row0 + at * kRowsAt, col, n) : Raw{}; };
+    const int row0 = m0 + wm + half * TH * S + lane / kRuns;
+    const auto extra = [&](int at) { return row0 + at * kRowsAt < g.m && at * kRowsAt < TH * S && g.splits == 1 ? load_extra(g.e, row0 + at * kRowsAt, col, n) : Raw{}; };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) ahead[i] = extra(i);
 #pragma unroll
@@ -498,13 +519,13 @@ __device__ __forceinline__ void write_out(const LinearArgs& g, const f32x16 (&ac
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int m = 32 * i + (lane & 31), chunk = 8 * j + 2 * q + (lane >> 5);
-          const f32x16& c = acc[half * TH + i][j];
+        for (int q = 0; q < S * S / 256; ++q) {   // 64 / S lanes have the next runs
+          const int m = S * i + lane % S, chunk = S / 4 * j + 64 / S * q + lane / S;
+          const auto& c = acc[half * TH + i][j];
           *(__attribute__((address_space(3))) f32x4*)(stage + m * (kCols * 4) + (chunk ^ (m & kMove)) * 16) = f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
         }
 #pragma unroll 1
-    for (int at = 0; at < TH * 32 / kRowsAt; ++at) {
+    for (int at = 0; at < TH * S / kRowsAt; ++at) {
       const int row = row0 + at * kRowsAt, m = lane / kRuns + at * kRowsAt;
       if (row >= g.m) break;   // all lanes of a row, and of a quad
       const Raw now = ahead[0];
@@ -558,7 +579,9 @@ __device__ __forceinline__ void interleave() {
 template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int HELD>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
-  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;   // 32 x 32 outputs of a wave
+  constexpr int S = HELD == TYPE ? 16 : 32;
+  constexpr int TM = BM / WM / S, TN = BN / WN / S;   // S x S outputs of a wave
+  constexpr int kParts = S == 16 ? 2 : 4, TH = TM * kParts / 4;   // of k in a step; outputs down of a quarter of a step
   __shared__ __attribute__((aligned(1024))) uint8_t a0[BM * kRowBytes], a1[BM * kRowBytes], b0[BN * kRowBytes], b1[BN * kRowBytes];
 
   const TileAt at = tile_of<BM, BN>(g);
@@ -571,29 +594,34 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
   LoadB lb(g.b, n0, g.n, begin, end);
 
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-  const Reader<ALAY, BM, TM> ra(wm);
-  const Reader<BLAY, BN, TN> rb(wn);
+  const Reader<S, ALAY, BM, TM> ra(wm);
+  const Reader<S, BLAY, BN, TN> rb(wn);
 
-  f32x16 acc[TM][TN];
+  typename Sums<S>::type acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    for (int j = 0; j < TN; ++j) clear(acc[i][j]);
 
-  s16x8 fa[2][TM], fb[2][TN];
-  const auto fetch = [&](const Lds* a, const Lds* b, int s) {
+  // A quarter of a step: 16 of k, or 32 of k by half of the wave's rows.
+  s16x8 fa[2][TH], fb[2][TN];
+  const auto part = [](int q) { return q * kParts / 4; };
+  const auto fetch = [&](const Lds* a, const Lds* b, int q) {
+    if (q * kParts % 4 == 0) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) fb[s & 1][j] = rb.read(b, j, s);
+      for (int j = 0; j < TN; ++j) fb[part(q) & 1][j] = rb.read(b, j, part(q));
+    }
 #pragma unroll
-    for (int i = 0; i < TM; ++i) fa[s & 1][i] = ra.read(a, i, s);
+    for (int i = 0; i < TH; ++i) fa[q & 1][i] = ra.read(a, q * TH % TM + i, part(q));
   };
-  const auto multiply = [&](int s) {
+  const auto multiply = [&](int q) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TH; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = mfma<TYPE>(fb[s & 1][j], fa[s & 1][i], acc[i][j]);   // rows of the result: n
+      for (int j = 0; j < TN; ++j) {
+        auto& c = acc[q * TH % TM + i][j];
+        c = mfma<TYPE>(fb[part(q) & 1][j], fa[q & 1][i], c);   // rows of the result: n
+      }
   };
   const auto load = [&](Lds* a, Lds* b) {
     la.load(a);
@@ -607,21 +635,22 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
     __builtin_amdgcn_s_waitcnt(0x0070);   // vmcnt(0), lgkmcnt(0): this wave's loads into LDS, its reads and writes
     __syncthreads();
   };
-  constexpr int kReads = TM * (ALAY == kRow ? 1 : 2) + TN * (BLAY == kRow ? 1 : 2);
-  // A step on what lies in (a, b), with the next step's operands on their way to (c, d): every 16 of k
-  // are read while the 16 before are multiplied.  The last multiplication comes after the barrier, to
+  constexpr int kReadsA = TH * decltype(ra)::kEach, kReads = kReadsA + TN * decltype(rb)::kEach;   // with a's part of k the same, and another
+  // A step on what lies in (a, b), with the next step's operands on their way to (c, d): every quarter
+  // is read while the one before is multiplied.  The last multiplication comes after the barrier, to
   // cover the first reads of the next step; (a, b), all read, take the step after that.  What lies
   // beyond the last step is not read from memory (its window is empty) and not used.
   const auto step = [&](Lds* a, Lds* b, Lds* c, Lds* d) {
 #pragma unroll
-    for (int s = 0; s < 3; ++s) {
-      fetch(a, b, s + 1);
-      multiply(s);
-      if (s == 0) {
-        interleave<TM * TN, kReads, 0, 0, 0>();
+    for (int q = 0; q < 3; ++q) {
+      fetch(a, b, q + 1);
+      multiply(q);
+      if (q == 0) {
+        interleave<TH * TN, kParts == 4 ? kReads : kReadsA, 0, 0, 0>();
       } else {
-        put(c, d, s - 1);
-        interleave<TM * TN, kReads, 0, LoadB::kWork, LoadB::kWrites / 2>();
+        put(c, d, q - 1);
+        if (q == 1) interleave<TH * TN, kReads, 0, LoadB::kWork, LoadB::kWrites / 2>();
+        else interleave<TH * TN, kParts == 4 ? kReads : kReadsA, 0, LoadB::kWork, LoadB::kWrites / 2>();
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -630,7 +659,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
     fetch(c, d, 0);
     load(a, b);
     multiply(3);
-    interleave<TM * TN, kReads, LoadA::kLoads + LoadB::kLoads, 0, 0>();
+    interleave<TH * TN, kReads, LoadA::kLoads + LoadB::kLoads, 0, 0>();
     __builtin_amdgcn_sched_barrier(0);
   };
   // Steps in pairs, so that each buffer has its own code (and the compiler sees that the loads do not
@@ -661,7 +690,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
   }
 
   arrived();   // the last reads; and the loads of nothing that write zeros
-  write_out<BM, BN, WM, WN>(g, acc, m0, n0, pb0, pb1, pa0, pa1);
+  write_out<S, BM, BN, WM, WN>(g, acc, m0, n0, pb0, pb1, pa0, pa1);
 }
 
 // Whether a kernel takes the sums of a along: where its registers have room.
@@ -672,7 +701,7 @@ constexpr bool sums_along(int alay, int bm) { return alay == kCol && bm == 64; }
 template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int kRing, int HELD, bool NARROW>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
-  constexpr int TM = BM / WM / 32, TN = BN / WN / 32;
+  constexpr int S = 32, TM = BM / WM / S, TN = BN / WN / S;
   __shared__ __attribute__((aligned(1024))) uint8_t a0[BM * kRowBytes], a1[BM * kRowBytes], b0[BN * kRowBytes], b1[BN * kRowBytes];
   const TileAt at = tile_of<BM, BN>(g);
   const int begin = blockIdx.y * g.split_k, end = min(g.k, begin + g.split_k);
@@ -681,16 +710,14 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArg
   const LoadA la(g.a, at.m0, g.m, end);
   const LoadB lb(g.b, at.n0, g.n, end);
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wm = wave / WN * (BM / WM), wn = wave % WN * (BN / WN);
-  const Reader<ALAY, BM, TM> ra(wm);
-  const Reader<BLAY, BN, TN> rb(wn);
+  const Reader<S, ALAY, BM, TM> ra(wm);
+  const Reader<S, BLAY, BN, TN> rb(wn);
 
-  f32x16 acc[TM][TN];
+  typename Sums<S>::type acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+    for (int j = 0; j < TN; ++j) clear(acc[i][j]);
 
   typename LoadA::Set sa[kRing];
   typename LoadB::Set sb[kRing];
@@ -716,15 +743,14 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArg
   const bool summing = kSums && g.sums && at.n0 == 0 && wn == 0;
   const uint16_t one = TYPE == MOC_BF16 ? 0x3F80 : 0x3C00;
   const s16x8 ones = {(short)one, (short)one, (short)one, (short)one, (short)one, (short)one, (short)one, (short)one};
-  f32x16 sums[kSums ? TM : 1];
+  typename Sums<S>::type sums[kSums ? TM : 1];
 #pragma unroll
-  for (f32x16& x : sums)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) x[r] = 0.0f;
+  for (auto& x : sums) clear(x);
   const auto multiply = [&](int i) {
-    s16x8 fa[kStepK / 16][TM];
+    constexpr int kParts = decltype(ra)::kParts;
+    s16x8 fa[kParts][TM];
 #pragma unroll
-    for (int s = 0; s < kStepK / 16; ++s) {
+    for (int s = 0; s < kParts; ++s) {
       s16x8 fb[TN];
 #pragma unroll
       for (int j = 0; j < TN; ++j) fb[j] = rb.read(pb[i & 1], j, s);
@@ -738,7 +764,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArg
     if constexpr (kSums) {
       if (summing) {
 #pragma unroll
-        for (int s = 0; s < kStepK / 16; ++s)
+        for (int s = 0; s < kParts; ++s)
 #pragma unroll
           for (int c = 0; c < TM; ++c) sums[c] = mfma<TYPE>(ones, fa[s][c], sums[c]);
       }
@@ -771,16 +797,16 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArg
   }
   if constexpr (kSums) {
     const int lane = threadIdx.x & (kWave - 1);
-    if (summing && lane < 32) {   // a lane has one m, every n alike
+    if (summing && lane < S) {   // a lane has one m, every n alike
       float* const to = g.splits > 1 ? g.partial + (int64_t)g.splits * g.m * g.partial_stride + (int64_t)blockIdx.y * g.m : g.sums;
 #pragma unroll
       for (int c = 0; c < TM; ++c) {
-        const int m = at.m0 + wm + 32 * c + lane;
+        const int m = at.m0 + wm + S * c + lane;
         if (m < g.m) to[m] = sums[c][0];
       }
     }
   }
-  write_out<BM, BN, WM, WN>(g, acc, at.m0, at.n0, pb[0], pb[1], pa[0], pa[1]);
+  write_out<S, BM, BN, WM, WN>(g, acc, at.m0, at.n0, pb[0], pb[1], pa[0], pa[1]);
 }
 
 // The sum of the splits, in their order, and the epilogue; a thread has a run, a quad a block.
