@@ -4,12 +4,13 @@
 // Operands lie in memory either with k running along a row ("row": x and w of the forward pass, dy of
 // the input's gradient) or with m or n running along it ("col": w of the input's gradient, dy and x of
 // the weight's).  Both go to LDS as they lie, 16 bytes a lane, and come out of it as the matrix cores
-// want them: a lane holds eight consecutive k of one m or n, which a row operand
-// has next to each other (one 16-byte read) and a col operand below each other (two reads that
-// transpose 4 x 16 values among 16 lanes, ds_read_b64_tr_b16).
+// want them: a lane holds eight consecutive k of one m or n, which a row operand has next to each
+// other (one 16-byte read) and a col operand below each other (two reads that transpose 4 x 16 values
+// among 16 lanes, ds_read_b64_tr_b16).
 //
-// A workgroup computes BM x BN of the output, 64 of k at a time, in two buffers: while one is
-// multiplied, the loads of the next run straight into the other.
+// A workgroup computes BM x BN of the output, 64 of k at a time, in two buffers.  Two kernels: one whose
+// loads run straight into LDS while the other buffer is multiplied, for large products of aligned
+// operands, and one whose loads wait in registers, for everything else.
 #pragma once
 
 #include <algorithm>
@@ -575,7 +576,11 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-// TYPE of the operands; HELD: of b, TYPE or a checkpoint's.
+// TYPE of the operands; HELD: of b, TYPE or a checkpoint's.  256 x 256 by eight waves, two on a SIMD, 128 x 64
+// each: 64 KB come from L2 for every 8 MFLOP.  16384 x 4096 x 16384 in bf16: 1.76 to 1.83 ms (1.22 PFLOP/s; a library's
+// product 1.49 to 1.58 beside it), by columns 1.69 (w) and 1.65 (both), from e4m3 1.92, int8 2.06.  Bound by the board's
+// power, at 1.5 to 1.7 GHz and with the matrix cores busy 66 to 77 % of the time (32 x 32 x 16); with x all zeros the same
+// kernel takes 10 % less.  Tried and slower: four waves of 128 x 128, lines brought to L2 a step ahead.
 template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int HELD>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
@@ -697,7 +702,10 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
 constexpr bool sums_along(int alay, int bm) { return alay == kCol && bm == 64; }
 
 // For products of few or ragged tiles, which wait for memory: every operand goes through registers, kRing
-// steps of it on their way, so that any alignment does and a short sum is all loaded at once.
+// steps of it on their way, so that any alignment does and a short sum is all loaded at once.  1247 x 442 x 1000
+// 9.8 us (23.8 with one step on its way), 1 x 4096 x 16384 31 us, 4.3 TB/s of weights; 9001 x 5001 x 5003 in tiles of
+// 256 x 256 530 us, 0.85 PFLOP/s.  Bound by what L2 hands out in 64 x 64 (11 TB/s; 128 x 64 and 128 x 128 are never
+// 10 % faster), eight steps on their way are 5 to 10 % slower.
 template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int kRing, int HELD, bool NARROW>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;

@@ -384,10 +384,11 @@ __device__ __forceinline__ void store_sums(const NormArgs& g, const float (&sg)[
   }
 }
 
-// 16 waves a compute unit, 128 registers a thread.  The next row is on its way while the sums over this
-// one are taken.
+// 16 waves a compute unit, 128 registers a thread; a wave a row with two runs a lane has 12, or 8 where x is float32 or
+// a checkpoint (65536 x 1024 float32 168 us, 310 with 12 and what that spills).  The next row is on its way while the
+// sums over this one are taken.
 template <int X, int D, int T, int CH>
-__global__ __launch_bounds__(T < 256 ? 256 : T, CH > 1 && T == kWave ? 3 : 4) void norm_backward_kernel(NormArgs g) {
+__global__ __launch_bounds__(T < 256 ? 256 : T, CH > 1 && T == kWave ? (X == MOC_F32 || X == MOC_E4M3 || X == MOC_I8 ? 2 : 3) : 4) void norm_backward_kernel(NormArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
   static_assert(T <= kWave || kRows == 1);
   using Sums = RowSums<T, 2>;
@@ -549,7 +550,7 @@ struct Shape {
 template <int X>
 Shape forward_shape(int64_t cols) {
   if (cols <= 512) return {norm_forward_kernel<X, 64, 1, 2>, 256, 8};
-  if (cols <= 1024) return {norm_forward_kernel<X, 64, 2, 2>, 256, 8};
+  if (cols <= 1024) return {norm_forward_kernel<X, 64, 2, X == MOC_F32 ? 1 : 2>, 256, X == MOC_F32 ? 4 : 8};   // two rows of float32 do not fit the registers
   if (cols <= 2048) return {norm_forward_kernel<X, 256, 1, 2>, 256, 2};
   if (cols <= 4096) return {norm_forward_kernel<X, 256, 2, 1>, 256, 1};
   if (cols <= 8192) return {norm_forward_kernel<X, 512, 2, 1>, 512, 1};
