@@ -58,7 +58,7 @@
 extern "C" {
 #endif
 
-#define MOC_TRAINING_VERSION 1
+#define MOC_TRAINING_VERSION 2
 
 #define MOC_F32  0
 #define MOC_F16  1
@@ -189,6 +189,20 @@ int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cout, const mo
 /* Bytes of workspace that the three calls above need for these sizes on the
  * current device (the largest of the three), or a negative error code. */
 int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout);
+
+/*
+ * How a product is cut up, for tests and tuning: no device is used where `units` says for how many compute units (0: the
+ * current device's).
+ *   product  which call: MOC_LINEAR_FORWARD, MOC_LINEAR_BACKWARD_INPUT or MOC_LINEAR_BACKWARD_WEIGHT
+ *   aligned  whether operands start on 16 bytes and strides are multiples of 8 elements (of a checkpoint 16, and cin too)
+ *   out      host, [5]: rows and columns of the output that a workgroup computes; 1 where operands go straight into LDS, else
+ *            0; the parts that the sum is cut into; terms of a part; terms of the last one
+ * Errors: MOC_EINVAL, MOC_EHIP.
+ */
+#define MOC_LINEAR_FORWARD         0
+#define MOC_LINEAR_BACKWARD_INPUT  1
+#define MOC_LINEAR_BACKWARD_WEIGHT 2
+int moc_linear_parts(int32_t product, int64_t rows, int64_t cin, int64_t cout, int32_t aligned, int32_t units, int64_t* out);
 
 /* The MOC_TRAINING_VERSION that the library was built with. */
 int moc_training_version(void);

@@ -84,6 +84,9 @@ struct Epilogue {
   float most;
 };
 
+// Where the part of k ends that starts at `begin` < k: begin + each can be past 2^31 where k is a weight gradient's rows.
+__host__ __device__ inline int part_end(int k, int begin, int each) { return k - begin < each ? k : begin + each; }
+
 struct LinearArgs {
   Operand a, b;
   int m, n, k;
@@ -591,7 +594,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) 
 
   const TileAt at = tile_of<BM, BN>(g);
   const int m0 = at.m0, n0 = at.n0;
-  const int begin = blockIdx.y * g.split_k, end = min(g.k, begin + g.split_k);
+  const int begin = blockIdx.y * g.split_k, end = part_end(g.k, begin, g.split_k);
 
   using LoadA = DirectLoader<ALAY, BM, kThreads>;
   using LoadB = typename PickB<TYPE, BLAY, BN, kThreads, HELD>::type;
@@ -712,7 +715,7 @@ __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArg
   constexpr int S = 32, TM = BM / WM / S, TN = BN / WN / S;
   __shared__ __attribute__((aligned(1024))) uint8_t a0[BM * kRowBytes], a1[BM * kRowBytes], b0[BN * kRowBytes], b1[BN * kRowBytes];
   const TileAt at = tile_of<BM, BN>(g);
-  const int begin = blockIdx.y * g.split_k, end = min(g.k, begin + g.split_k);
+  const int begin = blockIdx.y * g.split_k, end = part_end(g.k, begin, g.split_k);
   using LoadA = RegisterLoader<ALAY, BM, kThreads, TYPE, TYPE, NARROW>;
   using LoadB = RegisterLoader<BLAY, BN, kThreads, TYPE, HELD, NARROW>;
   const LoadA la(g.a, at.m0, g.m, end);

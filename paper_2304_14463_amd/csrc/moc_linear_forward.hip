@@ -55,4 +55,22 @@ int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout) {
   return most;
 }
 
+int moc_linear_parts(int32_t product, int64_t rows, int64_t cin, int64_t cout, int32_t aligned, int32_t units, int64_t* out) {
+  if (!sizes_ok(rows, cin) || !sizes_ok(rows, cout) || product < MOC_LINEAR_FORWARD || product > MOC_LINEAR_BACKWARD_WEIGHT || units < 0 || !out) return MOC_EINVAL;
+  int there = units;
+  const int rc = units > 0 ? MOC_OK : moc_compute_units(&there);
+  if (rc != MOC_OK) return rc;
+  const int64_t sizes[3][3] = {{rows, cout, cin}, {rows, cin, cout}, {cout, cin, rows}}, along = product == MOC_LINEAR_FORWARD ? cin : cout;
+  const Loading how = loading_of(aligned && along % 8 == 0 && cin % 8 == 0, along, cin);
+  const int64_t* const s = sizes[product];
+  const LinearPlan p = linear_plan(s[0], s[1], s[2], product, how, there);   // as many operands lie in columns
+  const int last = (p.splits - 1) * p.split_k;
+  out[0] = kShapes[p.shape].tile;
+  out[1] = p.shape == kDirect128 || p.shape == kDirect256;
+  out[2] = p.splits;
+  out[3] = p.split_k;
+  out[4] = part_end((int)s[2], last, p.split_k) - last;
+  return MOC_OK;
+}
+
 }  // extern "C"

@@ -10,18 +10,20 @@ A `Checkpoint` is an activation kept in 8 bits: a byte a value and a scale for 3
 """
 from __future__ import annotations
 
+import collections
 import ctypes
 
 from . import moccasin as moc
 
-MOC_TRAINING_VERSION = 1
+MOC_TRAINING_VERSION = 2
 MOC_F32, MOC_F16, MOC_BF16, MOC_E4M3, MOC_I8 = range(5)
 FORMATS = {"e4m3": MOC_E4M3, "int8": MOC_I8}
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+PRODUCTS = {"forward": 0, "backward_input": 1, "backward_weight": 2}
 BLOCK = 32
 
 EXPORTS = ("moc_checkpoint_write", "moc_checkpoint_read", "moc_norm_forward", "moc_norm_backward", "moc_norm_backward_work", "moc_linear_forward",
-           "moc_linear_backward_input", "moc_linear_backward_weight", "moc_linear_work", "moc_training_version")
+           "moc_linear_backward_input", "moc_linear_backward_weight", "moc_linear_work", "moc_linear_parts", "moc_training_version")
 
 
 class Matrix(ctypes.Structure):
@@ -74,6 +76,7 @@ def lib():
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
         for name, args in (("moc_norm_backward_work", [I64, I64]), ("moc_linear_work", [I64, I64, I64])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, I64
+        L.moc_linear_parts.argtypes, L.moc_linear_parts.restype = [I32, I64, I64, I64, I32, I32, ctypes.POINTER(I64)], ctypes.c_int
         _lib = L
     return _lib
 
@@ -170,3 +173,17 @@ def moc_linear_backward_weight(dy, x, dtype=None, want_bias=True, out=None, work
     code, out, db = _call("linear_backward_weight", stream, dy, x, dtype, want_bias, out, work)
     moc._check(code, "moc_linear_backward_weight")
     return out, db
+
+
+Parts = collections.namedtuple("Parts", "tile direct parts terms last")
+
+
+def moc_linear_parts(product, rows, cin, cout, aligned=True, units=0):
+    """How the product of moc_linear_`product` ("forward", "backward_input", "backward_weight") is cut up on a device of `units`
+    compute units (0: the current one): rows and columns of a workgroup's tile, whether operands go straight into LDS, the
+    parts of the sum, terms of a part and of the last one."""
+    if product not in PRODUCTS:
+        raise ValueError(f"product {product!r}: expected one of {', '.join(PRODUCTS)}")
+    out = (ctypes.c_int64 * 5)()
+    moc._check(lib().moc_linear_parts(PRODUCTS[product], rows, cin, cout, int(aligned), units, out), "moc_linear_parts")
+    return Parts(out[0], bool(out[1]), *out[2:])
