@@ -952,14 +952,11 @@ LinearKernel pick_linear(Shape shape) {
   return nullptr;
 }
 
-// Queues the product: `g` has the operands, sizes and epilogue; held: b's type.  g.sums is left out, and set to
-// null, where the kernel does not take them.
-template <int ALAY, int BLAY, bool KEPT>
-int queue_linear(LinearArgs& g, int type, int held, Loading how, void* work, int64_t work_bytes, void* hip_stream) {
-  int units = 0;
-  const int rc = moc_compute_units(&units);
-  if (rc != MOC_OK) return rc;
-  const LinearPlan p = linear_plan(g.m, g.n, g.k, (ALAY == kCol) + (BLAY == kCol), how, units);
+// Cuts the product up, as far as its workspace and a launch go: `g` has the operands, sizes and epilogue.  g.sums is set
+// to null where the kernel does not take them.
+template <int ALAY, int BLAY>
+int cut_linear(LinearArgs& g, Loading how, int units, void* work, int64_t work_bytes, LinearPlan& p) {
+  p = linear_plan(g.m, g.n, g.k, (ALAY == kCol) + (BLAY == kCol), how, units);
   if (p.work_bytes > 0 && (!work || !aligned_to(work, 16) || work_bytes < p.work_bytes)) return MOC_EINVAL;
   if ((int64_t)p.tiles_m * p.tiles_n > (1 << 22)) return MOC_EOVERFLOW;   // a launch's threads
   g.tiles_m = p.tiles_m;
@@ -969,6 +966,12 @@ int queue_linear(LinearArgs& g, int type, int held, Loading how, void* work, int
   g.partial = static_cast<float*>(work);
   g.partial_stride = p.partial_stride;
   if (kShapes[p.shape].tile != 64) g.sums = nullptr;
+  return MOC_OK;
+}
+
+// Queues what cut_linear has cut up; held: b's type.
+template <int ALAY, int BLAY, bool KEPT>
+int queue_linear(const LinearArgs& g, const LinearPlan& p, int type, int held, void* hip_stream) {
   LinearKernel kern = nullptr;
   if constexpr (KEPT) {
     if (type == MOC_BF16) {

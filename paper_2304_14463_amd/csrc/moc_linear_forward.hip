@@ -36,7 +36,11 @@ int moc_linear_forward(int64_t rows, int64_t cin, int64_t cout, const moc_matrix
     e.scale_stride = kept->scale_stride;
     e.most = most_kept(kept->type, x->type);
   }
-  return queue_linear<kRow, kRow, false>(g, x->type, x->type, loading_of(direct_ok(x, cin) && direct_ok(w, cin), cin, cin), work, work_bytes, hip_stream);
+  int units = 0;
+  LinearPlan p;
+  int rc = moc_compute_units(&units);
+  if (rc == MOC_OK) rc = cut_linear<kRow, kRow>(g, loading_of(direct_ok(x, cin) && direct_ok(w, cin), cin, cin), units, work, work_bytes, p);
+  return rc == MOC_OK ? queue_linear<kRow, kRow, false>(g, p, x->type, x->type, hip_stream) : rc;
 }
 
 int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout) {

@@ -25,5 +25,9 @@ extern "C" int moc_linear_backward_input(int64_t rows, int64_t cin, int64_t cout
     e.slope = 1;
   }
   set_out(e, dx);
-  return queue_linear<kRow, kCol, false>(g, dy->type, dy->type, loading_of(direct_ok(dy, cout) && direct_ok(w, cin), cout, cin), work, work_bytes, hip_stream);
+  int units = 0;
+  LinearPlan p;
+  int rc = moc_compute_units(&units);
+  if (rc == MOC_OK) rc = cut_linear<kRow, kCol>(g, loading_of(direct_ok(dy, cout) && direct_ok(w, cin), cout, cin), units, work, work_bytes, p);
+  return rc == MOC_OK ? queue_linear<kRow, kCol, false>(g, p, dy->type, dy->type, hip_stream) : rc;
 }

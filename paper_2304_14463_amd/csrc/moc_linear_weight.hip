@@ -57,9 +57,12 @@ extern "C" int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cou
   int units = 0;
   const int asked = moc_compute_units(&units);
   if (asked != MOC_OK) return asked;
-  bool summed = false;
+  // Everything is checked before the product is queued: the bias's gradient has a need of its own where the product does not
+  // take it along.
+  LinearArgs product = {};
+  LinearPlan plan;
   if (cin > 0) {
-    LinearArgs g = {};
+    LinearArgs& g = product;
     g.sums = db;
     g.a = operand_of(dy);
     g.b = operand_of(x);
@@ -68,13 +71,17 @@ extern "C" int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cou
     g.k = (int)rows;
     set_out(g.e, dw);
     const bool direct = direct_ok(dy, cout) && (is_kept(x->type) ? kept_direct_ok(x, cin) : direct_ok(x, cin));
-    const int rc = queue_linear<kCol, kCol, true>(g, dy->type, x->type, loading_of(direct, cout, cin), work, work_bytes, hip_stream);
+    const int rc = cut_linear<kCol, kCol>(g, loading_of(direct, cout, cin), units, work, work_bytes, plan);
     if (rc != MOC_OK) return rc;
-    summed = g.sums != nullptr;
   }
-  if (db && !summed) {
-    const int64_t stretches = moc_bias_stretches(rows, cout, units);
-    if (stretches > 1 && (!work || !aligned_to(work, 16) || work_bytes < stretches * cout * (int64_t)sizeof(float))) return MOC_EINVAL;
+  const bool apart = db && !product.sums;
+  const int64_t stretches = apart ? moc_bias_stretches(rows, cout, units) : 1;
+  if (stretches > 1 && (!work || !aligned_to(work, 16) || work_bytes < stretches * cout * (int64_t)sizeof(float))) return MOC_EINVAL;
+  if (cin > 0) {
+    const int rc = queue_linear<kCol, kCol, true>(product, plan, dy->type, x->type, hip_stream);
+    if (rc != MOC_OK) return rc;
+  }
+  if (apart) {
     BiasArgs g = {};
     g.dy = dy->data;
     g.type = dy->type;
