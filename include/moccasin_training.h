@@ -129,7 +129,7 @@ int moc_norm_forward(int64_t rows, int64_t cols, const moc_matrix* x, const void
  *             checkpoint of it
  *   residual  of dy's type, added to dx (the gradient of a branch around the
  *             norm), or NULL
- *   dx        of dy's type; may be dy's or residual's own memory (same stride)
+ *   dx        of dy's type; may be dy's, x's or residual's own memory (same stride)
  *   dgamma, dbeta  device, float [cols]; both or neither (NULL).  With rows ==
  *             0 they are set to zero.
  *   work      moc_norm_backward_work(rows, cols) bytes; NULL without dgamma
@@ -167,7 +167,8 @@ int moc_linear_forward(int64_t rows, int64_t cin, int64_t cout, const moc_matrix
  *   pre  [rows][cin], a tensor of dy's type or float32, or a checkpoint; NULL
  *        with MOC_ACT_NONE only.  Where pre is NaN, dx is NaN; act' of
  *        MOC_ACT_RELU is 0 at pre <= 0 whatever dy is.
- *   dx   [rows][cin], dy's type or float32
+ *   dx   [rows][cin], dy's type or float32; may be pre's own memory (same type
+ *        and stride)
  * Errors: MOC_EINVAL, MOC_EHIP.
  */
 int moc_linear_backward_input(int64_t rows, int64_t cin, int64_t cout, const moc_matrix* dy, const moc_matrix* w,

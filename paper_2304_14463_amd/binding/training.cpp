@@ -10,6 +10,7 @@
 #include <torch/csrc/utils/object_ptr.h>
 
 #include <stdint.h>
+#include <algorithm>
 #include <string>
 
 #include "moccasin_training.h"
@@ -84,6 +85,33 @@ int64_t stride_of(const at::Tensor& x, const char* what) {
   return x.stride(0) > 1 ? x.stride(0) : 1;
 }
 
+// ---- memory that an output shares with an input -------------------------------------------------
+
+// `rows` of `bytes`, `step` apart.
+struct Span {
+  uintptr_t at = 0;
+  int64_t rows = 0, bytes = 0, step = 1;
+};
+
+// Of matrices with one step: whether a row of b begins before the end of a row of a and ends behind its start, d rows further on
+// than it; the smallest d that is far enough is looked at.
+bool shared_at_one_step(const Span& a, const Span& b, int64_t step) {
+  const int64_t gap = (int64_t)(b.at - a.at), least = -b.bytes - gap;   // d * step > least
+  const int64_t below = least / step - (least % step < 0 ? 1 : 0), d = std::max(below + 1, 1 - a.rows);
+  return d < b.rows && gap + d * step < a.bytes;
+}
+
+bool shared(const Span& a, const Span& b) {
+  if (a.rows < 1 || a.bytes < 1 || b.rows < 1 || b.bytes < 1) return false;
+  if (b.at >= a.at + (a.rows - 1) * a.step + a.bytes || a.at >= b.at + (b.rows - 1) * b.step + b.bytes) return false;
+  if (a.rows == 1) return shared_at_one_step(a, b, b.step);
+  if (b.rows == 1 || a.step == b.step) return shared_at_one_step(a, b, a.step);
+  const Span &few = a.rows < b.rows ? a : b, &many = a.rows < b.rows ? b : a;
+  for (int64_t i = 0; i < few.rows; ++i)
+    if (shared_at_one_step(Span{few.at + i * few.step, 1, few.bytes, 1}, many, many.step)) return true;
+  return false;
+}
+
 // A tensor or a checkpoint, or nothing (None where that is allowed), as the library takes it.
 struct Held {
   moc_matrix m = {};
@@ -91,7 +119,23 @@ struct Held {
   at::Tensor values;   // or the codes
   bool there = false, kept = false;
   const moc_matrix* get() const { return there ? &m : nullptr; }
+  Span span() const {
+    if (!there) return Span{};
+    const int64_t each = values.element_size();
+    return Span{reinterpret_cast<uintptr_t>(m.data), rows, cols * each, m.stride * each};
+  }
+  Span scale_span() const { return kept ? Span{reinterpret_cast<uintptr_t>(m.scales), rows, (cols + MOC_BLOCK - 1) / MOC_BLOCK, m.scale_stride} : Span{}; }
+  // the very matrix
+  bool is(const Held& o) const { return there && o.there && !kept && !o.kept && m.data == o.m.data && m.stride == o.m.stride && m.type == o.m.type; }
 };
+
+// Results are computed in any order: an output that shares memory with an input is refused, unless it is the input and each of
+// its values is read before it is written (`in_place`).
+void apart(const Held& out, const char* name, const Held& in, const char* what, bool in_place = false) {
+  if (!out.there || !in.there || (in_place && out.is(in))) return;
+  for (const Span& o : {out.span(), out.scale_span()})
+    if (shared(o, in.span()) || shared(o, in.scale_span())) bad(name, std::string("shares memory with ") + what);
+}
 
 at::Tensor attribute(PyObject* x, PyObject* name, const char* what) {
   THPObjectPtr got(PyObject_GetAttr(x, name));
@@ -249,6 +293,7 @@ PyObject* checkpoint_write(PyObject*, PyObject* const* a, Py_ssize_t count) {
   THPObjectPtr out = room_kept(a[2] == Py_None ? a[1] : a[2], x.values, x.rows, x.cols);
   const Held k = held(out, "out", x.rows, x.cols);
   same_device(x.values, k.values);
+  apart(k, "out", x, "x");
   void* const stream = stream_of(a[3]);
   const int code = released([&] { return calls.checkpoint_write(x.rows, x.cols, x.get(), k.get(), stream); });
   return Py_BuildValue("iN", code, out.release());
@@ -265,6 +310,7 @@ PyObject* checkpoint_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
   THPObjectPtr out = result(a[3], k.values, dtype_of(a[1], at::kFloat), k.rows, k.cols);
   const Held y = held(out, "out", k.rows, k.cols);
   same_device(k.values, y.values);
+  apart(y, "out", k, "kept");
   void* const stream = stream_of(a[4]);
   const int code = released([&] { return calls.checkpoint_read(k.rows, k.cols, k.get(), act, y.get(), stream); });
   return Py_BuildValue("iN", code, out.release());
@@ -284,6 +330,9 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const Held y = held(out, "out", x.rows, x.cols), k = held(kept, "keep", x.rows, x.cols, true);
   same_device(x.values, y.values);
   same_device(x.values, k.values);
+  apart(y, "out", x, "x", true);
+  apart(k, "keep", x, "x");
+  apart(k, "keep", y, "out");
   at::Tensor mean = room_for(x.values, at::kFloat, {x.rows}), rstd = room_for(x.values, at::kFloat, {x.rows});
   void* const stream = stream_of(a[7]);
   const int code = released([&] {
@@ -305,6 +354,9 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   THPObjectPtr out = result(a[7], d.values, d.values.scalar_type(), d.rows, d.cols);
   const Held dx = held(out, "out", d.rows, d.cols);
   same_device(d.values, dx.values);
+  apart(dx, "out", d, "dy", true);
+  apart(dx, "out", x, "x", true);
+  apart(dx, "out", r, "residual", true);
   const bool params = truth(a[6]);
   Work work;
   THPObjectPtr dgamma, dbeta;
@@ -347,6 +399,13 @@ PyObject* linear_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const Held y = held(out, "out", rows, cout), k = held(kept, "keep", rows, cout, true);
   same_device(x.values, y.values);
   same_device(x.values, k.values);
+  apart(y, "out", x, "x");
+  apart(y, "out", w, "w");
+  apart(y, "out", r, "residual", true);
+  apart(k, "keep", x, "x");
+  apart(k, "keep", w, "w");
+  apart(k, "keep", r, "residual");
+  apart(k, "keep", y, "out");
   const Work work = workspace(a[8], a[8] == Py_None ? calls.linear_work(rows, cin, cout) : 0, x.values);
   void* const stream = stream_of(a[9]);
   const int code =
@@ -369,6 +428,9 @@ PyObject* linear_backward_input(PyObject*, PyObject* const* a, Py_ssize_t count)
   THPObjectPtr out = result(a[5], d.values, dtype_of(a[4], d.values.scalar_type()), rows, cin);
   const Held dx = held(out, "out", rows, cin);
   same_device(d.values, dx.values);
+  apart(dx, "out", d, "dy");
+  apart(dx, "out", w, "w");
+  apart(dx, "out", pre, "pre", true);
   const Work work = workspace(a[6], a[6] == Py_None ? calls.linear_work(rows, cin, cout) : 0, d.values);
   void* const stream = stream_of(a[7]);
   const int code = released([&] { return calls.linear_backward_input(rows, cin, cout, d.get(), w.get(), act, pre.get(), dx.get(), work.data, work.bytes, stream); });
@@ -386,6 +448,8 @@ PyObject* linear_backward_weight(PyObject*, PyObject* const* a, Py_ssize_t count
   THPObjectPtr out = result(a[4], d.values, dtype_of(a[2], at::kFloat), cout, cin);
   const Held dw = held(out, "out", cout, cin);
   same_device(d.values, dw.values);
+  apart(dw, "out", d, "dy");
+  apart(dw, "out", x, "x");
   THPObjectPtr db;
   float* bias = nullptr;
   if (truth(a[3])) {
@@ -400,6 +464,17 @@ PyObject* linear_backward_weight(PyObject*, PyObject* const* a, Py_ssize_t count
   void* const stream = stream_of(a[6]);
   const int code = released([&] { return calls.linear_backward_weight(rows, cin, cout, d.get(), x.get(), dw.get(), bias, work.data, work.bytes, stream); });
   return Py_BuildValue("iNN", code, out.release(), db.release());
+  END_HANDLE_TH_ERRORS
+}
+
+// shares((address, rows, bytes of a row, from one row to the next) twice): whether two matrices share memory
+PyObject* shares(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  if (count != 8) refuse(PyExc_TypeError, "shares: 8 arguments");
+  int64_t v[8];
+  for (int i = 0; i < 8; ++i) v[i] = (int64_t)address(a[i]);
+  if (v[3] < 1 || v[7] < 1) refuse(PyExc_ValueError, "shares: rows are apart");
+  return PyBool_FromLong(shared(Span{(uintptr_t)v[0], v[1], v[2], v[3]}, Span{(uintptr_t)v[4], v[5], v[6], v[7]}));
   END_HANDLE_TH_ERRORS
 }
 
@@ -435,7 +510,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
 
 #define MOC_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MOC_METHOD(bind), MOC_METHOD(checkpoint_write), MOC_METHOD(checkpoint_read), MOC_METHOD(norm_forward), MOC_METHOD(norm_backward), MOC_METHOD(linear_forward),
-                         MOC_METHOD(linear_backward_input), MOC_METHOD(linear_backward_weight), {nullptr, nullptr, 0, nullptr}};
+                         MOC_METHOD(linear_backward_input), MOC_METHOD(linear_backward_weight), MOC_METHOD(shares), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_training", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -4,7 +4,9 @@ include/moccasin_training.h, in the same library as the evaluator).
 Argument marshalling only, as in `moccasin`: tensors are checked and turned into descriptors (natively,
 binding/training.cpp), results and workspaces are torch tensors, everything is asynchronous on `stream`
 (default: torch's current stream).  Matrices are two-dimensional CUDA tensors whose values of a row lie next to each other; rows
-may be any distance apart.  There is no CPU fallback: a missing library or GPU raises.
+may be any distance apart.  An `out` or `keep` that shares memory with an input is refused; it may be x of
+moc_norm_forward, dy, x or residual of moc_norm_backward, residual of moc_linear_forward and pre of
+moc_linear_backward_input themselves (same type and strides).  There is no CPU fallback: a missing library or GPU raises.
 
 A `Checkpoint` is an activation kept in 8 bits: a byte a value and a scale for 32 columns of a row.
 """
