@@ -5,7 +5,10 @@ residual) becomes a compute graph: node i is block i's forward pass, whose outpu
 keeps for the backward pass in 8 bits; node 2L - 1 - i is its backward pass.  The search brings the plain
 schedule below a memory budget by computing blocks again, the decoder turns what it found into a sequence,
 and the sequence is run with the operators of `paper_2304_14463_amd.training`.  They give the same bits for the
-same inputs, so every gradient is that of the plain schedule.
+same inputs (torch's allocator gives every tensor one alignment), so every gradient is that of the plain schedule.
+
+The graph's sizes are those of the blocks' outputs and gradients.  What a block needs while it runs and the parameters' gradients
+are not in it, so the allocator's peak is above the plan's.
 
     python examples/planned_step.py [blocks] [rows] [width] [budget as a share of the plain schedule's peak]
 """

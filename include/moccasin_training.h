@@ -5,11 +5,15 @@
  * (gfx950).
  *
  * A plan says of every output of a training step whether it stays in memory or
- * is computed again.  These calls are the steps of such a plan, and the third
- * choice beside the two: an activation may be kept in 8 bits and used in the
- * backward pass as it is kept.  Every call gives the same bits for the same
- * inputs, whatever else runs (no atomics, a fixed order of every sum), so an
- * activation that is computed again is the one that was dropped.
+ * is computed again.  These calls are the steps of such a plan; what stays may
+ * be kept in 8 bits and used in the backward pass as it is kept (the search
+ * knows one size of an output: which are kept so is up to the caller).  Every
+ * call gives the same bits for the same values at the same alignments and
+ * strides on one kind of device, whatever else runs (no atomics, a fixed order
+ * of every sum), so an activation that is computed again from operands that lie
+ * alike is the one that was dropped.  Alignment, strides and sizes choose a
+ * product's kernel and with it the order of its sums: operands that lie
+ * otherwise can change the last bit of a sum.
  *
  * Matrices.  moc_matrix describes rows x cols values: float32, float16 or
  * bfloat16, or a checkpoint.  Values of a row lie next to each other, rows are

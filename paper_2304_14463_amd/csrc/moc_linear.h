@@ -581,9 +581,12 @@ __device__ __forceinline__ void interleave() {
 
 // TYPE of the operands; HELD: of b, TYPE or a checkpoint's.  256 x 256 by eight waves, two on a SIMD, 128 x 64
 // each: 64 KB come from L2 for every 8 MFLOP.  16384 x 4096 x 16384 in bf16: 1.76 to 1.83 ms (1.22 PFLOP/s; a library's
-// product 1.49 to 1.58 beside it), by columns 1.69 (w) and 1.65 (both), from e4m3 1.92, int8 2.06.  Bound by the board's
-// power, at 1.5 to 1.7 GHz and with the matrix cores busy 66 to 77 % of the time (32 x 32 x 16); with x all zeros the same
-// kernel takes 10 % less.  Tried and slower: four waves of 128 x 128, lines brought to L2 a step ahead.
+// product 1.49 to 1.58 beside it), by columns 1.69 (w) and 1.65 (both), from e4m3 1.93, int8 2.12.  The matrix cores are busy
+// 63 % of the clocks (w by columns 70, both 73, e4m3 57, int8 52), of which power leaves 1.8 to 1.9 GHz (x all zeros: 10 %
+// less time).  The rest: one workgroup has a compute unit's LDS, so nothing is multiplied while 256 x 256 results go out (the
+// input's gradient 1.69 ms with 4096 columns of output, 1.71 to 2.0 with 16384); reads by columns conflict in LDS for 25 %
+// (one operand) and 50 % (both) of its clocks; 52 bytes a lane are spilled where w lies by columns.  Tried and slower: four
+// waves of 128 x 128, lines brought to L2 a step ahead.
 template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int HELD>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
@@ -707,8 +710,10 @@ constexpr bool sums_along(int alay, int bm) { return alay == kCol && bm == 64; }
 // For products of few or ragged tiles, which wait for memory: every operand goes through registers, kRing
 // steps of it on their way, so that any alignment does and a short sum is all loaded at once.  1247 x 442 x 1000
 // 9.8 us (23.8 with one step on its way), 1 x 4096 x 16384 31 us, 4.3 TB/s of weights; 9001 x 5001 x 5003 in tiles of
-// 256 x 256 530 us, 0.85 PFLOP/s.  Bound by what L2 hands out in 64 x 64 (11 TB/s; 128 x 64 and 128 x 128 are never
-// 10 % faster), eight steps on their way are 5 to 10 % slower.
+// 256 x 256 530 us, 0.85 PFLOP/s (from checkpoints 28 and 16 bytes a lane are spilled).  Bound by what L2 hands out in
+// 64 x 64 (11 TB/s).  128 x 128 through registers is not among the shapes: of twenty sizes in three layouts it was more than 6 %
+// faster than both others at one (4099 x 4097 x 1027 84 us against 94, its input gradient 87 against 96), 128 x 64 at none;
+// eight steps on their way are 5 to 10 % slower.
 template <int TYPE, int ALAY, int BLAY, int BM, int BN, int WM, int WN, int kRing, int HELD, bool NARROW>
 __global__ __launch_bounds__(WM* WN* kWave, 2) void linear_ring_kernel(LinearArgs g) {
   constexpr int kThreads = WM * WN * kWave;
@@ -869,7 +874,9 @@ struct LinearPlan {
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Microseconds that a product takes in tiles of a shape with k cut into `splits`, as measured over 30 sizes from 1 x 1000 x
-// 1000 to 16384 x 8192 x 2048 in all three layouts (`cols`: how many operands lie in columns).  A step of a workgroup of
+// 1000 to 16384 x 8192 x 2048 in all three layouts (`cols`: how many operands lie in columns).  The smallest k of a weight
+// gradient among them is 442, and the output's bytes are not counted: of few rows, whose gradient is bound by what it writes,
+// the choice is not measured (8 rows, 8192 x 8192: 82 us in 256 x 256, 3.3 TB/s written).  A step of a workgroup of
 // 64 x 64 takes 0.27 us and 0.1 more for an operand in columns, waiting for memory, or 0.25 (0.36 of ragged rows) for each
 // of those that share a compute unit; of 128 x 128 0.65 (two in columns: 0.95) and 0.7 (1.0); 256 x 256 have a unit to
 // themselves, 1.85 (2.0), through registers 2.2 (2.8).  Cutting k costs a launch and the sums, written and read.

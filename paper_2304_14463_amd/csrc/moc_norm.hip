@@ -6,7 +6,8 @@
 // up to 1024 columns (no barrier: 65536 x 1024 forward 77 -> 53 us, 5.0 TB/s), then 256 threads, then two
 // runs a thread in the forward pass (32768 x 4096 bf16 116 us, 4.6 TB/s, and 139, 4.9, with an e4m3
 // checkpoint; one run and two rows at a time 124 and 174).  The backward pass has no registers for two:
-// 153 us, 5.3 TB/s, against 226.  The last run of a ragged row is loaded whole and moved down when it is
+// 153 us, 5.3 TB/s, against 226.  Of 8193 to 16384 columns it has them all the same and spills 56 to 152 bytes a lane: 8192 x
+// 16384 248 us, 3.3 TB/s, from int8 308, 2.2 (a quarter of a gigabyte read and a tenth written for it).  The last run of a ragged row is loaded whole and moved down when it is
 // used, since a load in parts would be waited for (4999 x 1247, backward from int8: 32 -> 25 us).
 // Workgroups go over many rows: gamma and beta stay in registers, and in the backward pass so do a
 // column's two sums; they meet in the workspace, one row of sums a workgroup, and a second kernel adds

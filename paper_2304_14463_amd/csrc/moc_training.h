@@ -229,8 +229,9 @@ __device__ __forceinline__ void keep_any(int fmt, const float (&v)[kRun], int64_
 
 // ---- activations --------------------------------------------------------------------------------
 
-// exp2 and the reciprocal are the hardware's (1 ulp each): what is left of that after the rounding to
-// the output's type is below 2^-20 of a value.
+// exp2 and the reciprocal are the hardware's (1 ulp each), and exp2's argument z is rounded to 32 bits: a value is off by 2^-21 +
+// 2^-22 |z| of itself.  Next to a rounding to 16 bits that is nothing; float32 outputs hold 2^-16 where gelu or silu is
+// smallest (gelu at -9: 2^-16.8).
 __device__ __forceinline__ float over_one_plus(float u, float e) { return u * __builtin_amdgcn_rcpf(1.0f + e); }
 __device__ __forceinline__ float exp_minus(float z) { return __builtin_amdgcn_exp2f(z * -1.4426950408889634f); }
 

@@ -8,6 +8,9 @@ may be any distance apart.  An `out` or `keep` that shares memory with an input 
 moc_norm_forward, dy, x or residual of moc_norm_backward, residual of moc_linear_forward and pre of
 moc_linear_backward_input themselves (same type and strides).  There is no CPU fallback: a missing library or GPU raises.
 
+No call records a graph: results never require gradients, those of tensors that do included.  The gradients are calls of their
+own (moc_*_backward*); inside torch's autograd they belong into the backward of a torch.autograd.Function.
+
 A `Checkpoint` is an activation kept in 8 bits: a byte a value and a scale for 32 columns of a row.
 """
 from __future__ import annotations
