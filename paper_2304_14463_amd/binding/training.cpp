@@ -17,7 +17,7 @@
 
 namespace {
 
-// What bind() was given: the class of checkpoints, what says the current stream, and the library's calls.
+// What bind() was given: the class of checkpoints, what says the current stream of a device, and the library's calls.
 PyObject *checkpoint_class = nullptr, *current_stream = nullptr;
 struct Calls {
   decltype(&moc_checkpoint_write) checkpoint_write;
@@ -265,11 +265,13 @@ void arguments(Py_ssize_t count, Py_ssize_t wanted, const char* name) {
   if (count != wanted) refuse(PyExc_TypeError, std::string(name) + ": " + std::to_string(wanted) + " arguments");
   if (!checkpoint_class) refuse(PyExc_RuntimeError, "bind() comes first");
 }
-// A stream's handle; None: the current stream's, asked for when the arguments have been checked.
-void* stream_of(PyObject* x) {
-  if (x != Py_None) return reinterpret_cast<void*>(address(x));
-  PyObject* const none[1] = {Py_None};
-  THPObjectPtr handle(PyObject_Vectorcall(current_stream, none, 1, nullptr));
+// The handle of the current stream, asked for when the arguments have been checked; refused where these are not on the current
+// device, on which the kernels would run.
+void* stream_for(const at::Tensor& x) {
+  THPObjectPtr device(PyLong_FromLong(x.device().index()));
+  if (!device) throw python_error();
+  PyObject* const args[1] = {device.get()};
+  THPObjectPtr handle(PyObject_Vectorcall(current_stream, args, 1, nullptr));
   if (!handle) throw python_error();
   return reinterpret_cast<void*>(address(handle));
 }
@@ -285,25 +287,25 @@ int released(const F& f) {
 
 // ---- the calls: each returns (code, results..) --------------------------------------------------
 
-// checkpoint_write(x, fmt, out, stream) -> (code, out)
+// checkpoint_write(x, fmt, out) -> (code, out)
 PyObject* checkpoint_write(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
-  arguments(count, 4, "checkpoint_write");
+  arguments(count, 3, "checkpoint_write");
   const Held x = held(a[0], "x");
   THPObjectPtr out = room_kept(a[2] == Py_None ? a[1] : a[2], x.values, x.rows, x.cols);
   const Held k = held(out, "out", x.rows, x.cols);
   same_device(x.values, k.values);
   apart(k, "out", x, "x");
-  void* const stream = stream_of(a[3]);
+  void* const stream = stream_for(x.values);
   const int code = released([&] { return calls.checkpoint_write(x.rows, x.cols, x.get(), k.get(), stream); });
   return Py_BuildValue("iN", code, out.release());
   END_HANDLE_TH_ERRORS
 }
 
-// checkpoint_read(kept, dtype, act, out, stream) -> (code, out)
+// checkpoint_read(kept, dtype, act, out) -> (code, out)
 PyObject* checkpoint_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
-  arguments(count, 5, "checkpoint_read");
+  arguments(count, 4, "checkpoint_read");
   const Held k = held(a[0], "kept");
   if (!k.kept) bad("kept", "a Checkpoint expected");
   const int32_t act = act_of(a[2]);
@@ -311,16 +313,16 @@ PyObject* checkpoint_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const Held y = held(out, "out", k.rows, k.cols);
   same_device(k.values, y.values);
   apart(y, "out", k, "kept");
-  void* const stream = stream_of(a[4]);
+  void* const stream = stream_for(k.values);
   const int code = released([&] { return calls.checkpoint_read(k.rows, k.cols, k.get(), act, y.get(), stream); });
   return Py_BuildValue("iN", code, out.release());
   END_HANDLE_TH_ERRORS
 }
 
-// norm_forward(x, gamma, beta, eps, keep, dtype, out, stream) -> (code, y, mean, rstd, kept)
+// norm_forward(x, gamma, beta, eps, keep, dtype, out) -> (code, y, mean, rstd, kept)
 PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
-  arguments(count, 8, "norm_forward");
+  arguments(count, 7, "norm_forward");
   const Held x = held(a[0], "x");
   const Vector gamma = vector(a[1], x.cols, "gamma", x.values), beta = vector(a[2], x.cols, "beta", x.values);
   if (gamma.data && beta.data && gamma.type != beta.type) refuse(PyExc_ValueError, "gamma and beta must have one type");
@@ -334,7 +336,7 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   apart(k, "keep", x, "x");
   apart(k, "keep", y, "out");
   at::Tensor mean = room_for(x.values, at::kFloat, {x.rows}), rstd = room_for(x.values, at::kFloat, {x.rows});
-  void* const stream = stream_of(a[7]);
+  void* const stream = stream_for(x.values);
   const int code = released([&] {
     return calls.norm_forward(x.rows, x.cols, x.get(), gamma.data, beta.data, gamma.data ? gamma.type : beta.type, (float)eps, y.get(), k.get(),
                               static_cast<float*>(mean.data_ptr()), static_cast<float*>(rstd.data_ptr()), stream);
@@ -343,10 +345,10 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   END_HANDLE_TH_ERRORS
 }
 
-// norm_backward(dy, x, gamma, mean, rstd, residual, want_params, out, work, stream) -> (code, dx, dgamma, dbeta)
+// norm_backward(dy, x, gamma, mean, rstd, residual, want_params, out, work) -> (code, dx, dgamma, dbeta)
 PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
-  arguments(count, 10, "norm_backward");
+  arguments(count, 9, "norm_backward");
   const Held d = held(a[0], "dy"), x = held(a[1], "x", d.rows, d.cols), r = held(a[5], "residual", d.rows, d.cols, true);
   const Vector gamma = vector(a[2], d.cols, "gamma", d.values), mean = vector(a[3], d.rows, "mean", d.values, true), rstd = vector(a[4], d.rows, "rstd", d.values, true);
   same_device(d.values, x.values);
@@ -374,7 +376,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
     dgamma = Py_None;
     dbeta = Py_None;
   }
-  void* const stream = stream_of(a[9]);
+  void* const stream = stream_for(d.values);
   const int code = released([&] {
     return calls.norm_backward(d.rows, d.cols, d.get(), x.get(), gamma.data, gamma.type, static_cast<const float*>(mean.data), static_cast<const float*>(rstd.data), r.get(), dx.get(),
                                pg, pb, work.data, work.bytes, stream);
@@ -383,10 +385,10 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   END_HANDLE_TH_ERRORS
 }
 
-// linear_forward(x, w, bias, act, residual, keep, dtype, out, work, stream) -> (code, y, kept)
+// linear_forward(x, w, bias, act, residual, keep, dtype, out, work) -> (code, y, kept)
 PyObject* linear_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
-  arguments(count, 10, "linear_forward");
+  arguments(count, 9, "linear_forward");
   const Held x = held(a[0], "x"), w = held(a[1], "w", -1, x.cols);
   const int64_t rows = x.rows, cin = x.cols, cout = w.rows;
   const Held r = held(a[4], "residual", rows, cout, true);
@@ -407,17 +409,17 @@ PyObject* linear_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   apart(k, "keep", r, "residual");
   apart(k, "keep", y, "out");
   const Work work = workspace(a[8], a[8] == Py_None ? calls.linear_work(rows, cin, cout) : 0, x.values);
-  void* const stream = stream_of(a[9]);
+  void* const stream = stream_for(x.values);
   const int code =
       released([&] { return calls.linear_forward(rows, cin, cout, x.get(), w.get(), bias.data, bias.type, act, r.get(), y.get(), k.get(), work.data, work.bytes, stream); });
   return Py_BuildValue("iNN", code, out.release(), kept.release());
   END_HANDLE_TH_ERRORS
 }
 
-// linear_backward_input(dy, w, act, pre, dtype, out, work, stream) -> (code, dx)
+// linear_backward_input(dy, w, act, pre, dtype, out, work) -> (code, dx)
 PyObject* linear_backward_input(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
-  arguments(count, 8, "linear_backward_input");
+  arguments(count, 7, "linear_backward_input");
   const Held d = held(a[0], "dy"), w = held(a[1], "w", d.cols);
   const int64_t rows = d.rows, cout = d.cols, cin = w.cols;
   const Held pre = held(a[3], "pre", rows, cin, true);
@@ -432,16 +434,16 @@ PyObject* linear_backward_input(PyObject*, PyObject* const* a, Py_ssize_t count)
   apart(dx, "out", w, "w");
   apart(dx, "out", pre, "pre", true);
   const Work work = workspace(a[6], a[6] == Py_None ? calls.linear_work(rows, cin, cout) : 0, d.values);
-  void* const stream = stream_of(a[7]);
+  void* const stream = stream_for(d.values);
   const int code = released([&] { return calls.linear_backward_input(rows, cin, cout, d.get(), w.get(), act, pre.get(), dx.get(), work.data, work.bytes, stream); });
   return Py_BuildValue("iN", code, out.release());
   END_HANDLE_TH_ERRORS
 }
 
-// linear_backward_weight(dy, x, dtype, want_bias, out, work, stream) -> (code, dw, db)
+// linear_backward_weight(dy, x, dtype, want_bias, out, work) -> (code, dw, db)
 PyObject* linear_backward_weight(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
-  arguments(count, 7, "linear_backward_weight");
+  arguments(count, 6, "linear_backward_weight");
   const Held d = held(a[0], "dy"), x = held(a[1], "x", d.rows);
   const int64_t rows = d.rows, cout = d.cols, cin = x.cols;
   same_device(d.values, x.values);
@@ -461,7 +463,7 @@ PyObject* linear_backward_weight(PyObject*, PyObject* const* a, Py_ssize_t count
     db = Py_None;
   }
   const Work work = workspace(a[5], a[5] == Py_None ? calls.linear_work(rows, cin, cout) : 0, d.values);
-  void* const stream = stream_of(a[6]);
+  void* const stream = stream_for(d.values);
   const int code = released([&] { return calls.linear_backward_weight(rows, cin, cout, d.get(), x.get(), dw.get(), bias, work.data, work.bytes, stream); });
   return Py_BuildValue("iNN", code, out.release(), db.release());
   END_HANDLE_TH_ERRORS
@@ -478,7 +480,7 @@ PyObject* shares(PyObject*, PyObject* const* a, Py_ssize_t count) {
   END_HANDLE_TH_ERRORS
 }
 
-// bind(class of checkpoints, current stream's handle as a function of None, {name of a call: its address})
+// bind(class of checkpoints, current stream's handle as a function of the operands' device, {name of a call: its address})
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
   if (count != 3 || !PyType_Check(a[0]) || !PyCallable_Check(a[1]) || !PyDict_Check(a[2])) refuse(PyExc_TypeError, "bind: a class, a function and a dict");

@@ -3,8 +3,8 @@ include/moccasin_training.h, in the same library as the evaluator).
 
 Argument marshalling only, as in `moccasin`: tensors are checked and turned into descriptors (natively,
 binding/training.cpp), results and workspaces are torch tensors, everything is asynchronous on `stream`
-(default: torch's current stream).  Matrices are two-dimensional CUDA tensors whose values of a row lie next to each other; rows
-may be any distance apart.  An `out` or `keep` that shares memory with an input is refused; it may be x of
+(default: torch's current stream) on the current device, where the tensors have to be.  Matrices are
+two-dimensional CUDA tensors whose values of a row lie next to each other; rows may be any distance apart.  An `out` or `keep` that shares memory with an input is refused; it may be x of
 moc_norm_forward, dy, x or residual of moc_norm_backward, residual of moc_linear_forward and pre of
 moc_linear_backward_input themselves (same type and strides).  There is no CPU fallback: a missing library or GPU raises.
 
@@ -99,7 +99,7 @@ def _bound():
         if getattr(native, "training_version", None) != MOC_TRAINING_VERSION:
             raise RuntimeError(f"{native.__file__}: version {getattr(native, 'training_version', None)} of the training operators, expected "
                                f"{MOC_TRAINING_VERSION}; run python -m paper_2304_14463_amd.build")
-        native.bind(Checkpoint, moc._stream_handle, {name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in EXPORTS})
+        native.bind(Checkpoint, _current_stream, {name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in EXPORTS})
         _native = native
     return _native
 
@@ -110,13 +110,23 @@ def _act(act):
     return ACTS[act]
 
 
+def _current_stream(device):
+    """Handle of the current stream.  Kernels run on the current device, as with moc_eval_batch's graph: tensors on another are
+    refused."""
+    torch = moc._tc()
+    current = torch.cuda.current_device()
+    if device != current:
+        raise ValueError(f"tensors on cuda:{device}, the current device is cuda:{current}")
+    return torch._C._cuda_getCurrentRawStream(current)
+
+
 def _call(name, stream, *args):
-    """(code, results..) of a native call; what it allocates belongs to `stream`."""
+    """(code, results..) of a native call; what it allocates belongs to `stream`, which is the current one meanwhile."""
     call = getattr(_native or _bound(), name)
     if stream is None:
-        return call(*args, None)
+        return call(*args)
     with moc._on(stream):
-        return call(*args, stream.cuda_stream)
+        return call(*args)
 
 
 def empty_checkpoint(rows, cols, fmt, device):
