@@ -158,7 +158,7 @@ int moc_norm_backward(int64_t rows, int64_t cols, const moc_matrix* dy, const mo
  *   work      moc_linear_work bytes (may be 0)
  * Products are exact, sums are held in 32 bits; u is rounded once to the
  * checkpoint, act(u) + residual once to y.  cin == 0: u = bias.
- * Errors: MOC_EINVAL, MOC_EHIP.
+ * Errors: MOC_EINVAL, MOC_EOVERFLOW, MOC_EHIP.
  */
 int moc_linear_forward(int64_t rows, int64_t cin, int64_t cout, const moc_matrix* x, const moc_matrix* w, const void* bias,
                        int32_t bias_type, int32_t act, const moc_matrix* residual, const moc_matrix* y,
@@ -173,7 +173,7 @@ int moc_linear_forward(int64_t rows, int64_t cin, int64_t cout, const moc_matrix
  *        MOC_ACT_RELU is 0 at pre <= 0 whatever dy is.
  *   dx   [rows][cin], dy's type or float32; may be pre's own memory (same type
  *        and stride)
- * Errors: MOC_EINVAL, MOC_EHIP.
+ * Errors: MOC_EINVAL, MOC_EOVERFLOW, MOC_EHIP.
  */
 int moc_linear_backward_input(int64_t rows, int64_t cin, int64_t cout, const moc_matrix* dy, const moc_matrix* w,
                               int32_t act, const moc_matrix* pre, const moc_matrix* dx, void* work, int64_t work_bytes,
@@ -186,7 +186,7 @@ int moc_linear_backward_input(int64_t rows, int64_t cin, int64_t cout, const moc
  *        taken in dy's type)
  *   dw   [cout][cin], float32 or dy's type
  *   db   device, float [cout], or NULL
- * rows == 0 sets dw and db to zero.  Errors: MOC_EINVAL, MOC_EHIP.
+ * rows == 0 sets dw and db to zero.  Errors: MOC_EINVAL, MOC_EOVERFLOW, MOC_EHIP.
  */
 int moc_linear_backward_weight(int64_t rows, int64_t cin, int64_t cout, const moc_matrix* dy, const moc_matrix* x,
                                const moc_matrix* dw, float* db, void* work, int64_t work_bytes, void* hip_stream);
