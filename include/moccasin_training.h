@@ -1,8 +1,10 @@
 /*
  * moccasin_training.h -- C ABI of the operators that a rematerialisation plan
  * is run with (libmoccasin_hip.so, next to moccasin.h): activation checkpoints
- * in 8 bits, layer norm, linear layers, and their gradients, on one AMD MI355X
- * (gfx950).
+ * in 8 bits, layer norm, linear layers, and their gradients; what joins the
+ * layers to a training step: the residual connection with its norms and gate,
+ * log probabilities and their gradient, and AdamW over many tensors; on one AMD
+ * MI355X (gfx950).
  *
  * A plan says of every output of a training step whether it stays in memory or
  * is computed again.  These calls are the steps of such a plan; what stays may
@@ -62,7 +64,7 @@
 extern "C" {
 #endif
 
-#define MOC_TRAINING_VERSION 2
+#define MOC_TRAINING_VERSION 3
 
 #define MOC_F32  0
 #define MOC_F16  1
@@ -208,6 +210,76 @@ int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout);
 #define MOC_LINEAR_BACKWARD_INPUT  1
 #define MOC_LINEAR_BACKWARD_WEIGHT 2
 int moc_linear_parts(int32_t product, int64_t rows, int64_t cin, int64_t cout, int32_t aligned, int32_t units, int64_t* out);
+
+/*
+ * AdamW over many tensors at once, in place:
+ *   g = grad_scale * grad
+ *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2
+ *   param -= lr * decay * param + lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * computed in 32 bits from what is stored, param and `copy` rounded once from
+ * the result.
+ *
+ * Moments are float32, or take 8 bits (moment_type MOC_E4M3): 32 consecutive
+ * values of the tensor share a scale 2^k, held as the byte k + 127 at
+ * scales[place / 32], with k as in a checkpoint in MOC_E4M3.  A code of m is one
+ * of MOC_E4M3; a code of v has no sign, 5 exponent and 3 fraction bits, is
+ * normal from 2^-22 on, 448 at its largest (254), and 255 is NaN.  Zeroed codes
+ * and scales are zeros.  v changes by a thousandth a step and codes are 6 to 12 %
+ * apart, so nearest codes would never fall: a value between two codes goes to
+ * the upper one where its distance from the lower, in parts of 2^20 of the
+ * codes' distance and rounded down, plus 16 b + 8 reaches 2^20, with b 16 random bits;
+ * the mean of what is stored is the value.  A positive v takes no code below
+ * 1.  What is not finite becomes NaN; magnitudes above 1.875 * 2^127 are taken for
+ * that.  Random bits of the value at place i of the tensor of number t:
+ *   mix(low(i) ^ mix(high(i) ^ mix(t ^ mix(low(step) ^ mix(high(seed) ^ mix(low(seed)))))))
+ * with low and high halves of 32 bits, the lower 16 for m, the upper for v, and
+ *   mix(h):  h ^= h >> 16, h *= 0xF704BB15, h ^= h >> 15, h *= 0x371E2E67, h ^= h >> 16.
+ *
+ * v below 2^-126 may count as 0.  All memory that is written is apart from all
+ * other memory of the call.  A tensor of no values is left out.  No tensors:
+ * a no-op.  Errors: MOC_EINVAL, MOC_EHIP.
+ */
+typedef struct {
+  void* param;          /* device, [count], contiguous, float32, float16 or bfloat16 */
+  const void* grad;     /* the same of grad_type */
+  void *m, *v;          /* float32, or bytes */
+  uint8_t *m_scales, *v_scales; /* 8 bits: ceil(count / 32) bytes each */
+  void* copy;           /* param's new values in copy_type (float16 or bfloat16), or NULL */
+  int64_t count;
+  int32_t param_type, grad_type;
+  int32_t moment_type;  /* MOC_F32, or MOC_E4M3 for 8 bits */
+  int32_t copy_type;
+  float decay;          /* >= 0 */
+  int32_t reserved;     /* 0 */
+} moc_adamw_tensor;
+
+typedef struct {
+  double lr, beta1, beta2, eps;   /* finite in float; 0 <= beta < 1; eps >= 2^-126 */
+  double grad_scale;
+  int64_t step;                   /* >= 1 */
+  uint64_t seed;                  /* of moments in 8 bits */
+  const float* lr_at;             /* device: read instead of lr, or NULL */
+  const float* grad_scale_at;     /* device: read instead of grad_scale, or NULL */
+  const int64_t* step_at;         /* device: read instead of step, or NULL (a captured call finds each replay's step there) */
+} moc_adamw_rule;
+
+int moc_adamw_step(int64_t tensors, const moc_adamw_tensor* tensor, const moc_adamw_rule* rule, void* hip_stream);
+
+/*
+ * What moments stand for: m and v of each tensor as values.
+ *   m, v, scales, count, moment_type  as above
+ *   m_values, v_values  device, [count] of value_type (float32 or bfloat16, which
+ *                       have every value of a code; float16)
+ * Errors: MOC_EINVAL, MOC_EHIP.
+ */
+typedef struct {
+  const void *m, *v;
+  const uint8_t *m_scales, *v_scales;
+  void *m_values, *v_values;
+  int64_t count;
+  int32_t moment_type, value_type;
+} moc_moments_tensor;
+int moc_moments_read(int64_t tensors, const moc_moments_tensor* tensor, void* hip_stream);
 
 /* The MOC_TRAINING_VERSION that the library was built with. */
 int moc_training_version(void);

@@ -12,6 +12,8 @@
 #include <stdint.h>
 #include <algorithm>
 #include <string>
+#include <utility>
+#include <vector>
 
 #include "moccasin_training.h"
 
@@ -29,8 +31,10 @@ struct Calls {
   decltype(&moc_linear_backward_input) linear_backward_input;
   decltype(&moc_linear_backward_weight) linear_backward_weight;
   decltype(&moc_linear_work) linear_work;
+  decltype(&moc_adamw_step) adamw_step;
+  decltype(&moc_moments_read) moments_read;
 } calls;
-PyObject *name_codes, *name_scales, *name_fmt;   // interned
+PyObject *name_codes, *name_scales, *name_fmt, *name_m, *name_v, *name_m_scales, *name_v_scales;   // interned
 
 [[noreturn]] void refuse(PyObject* type, const std::string& what) {
   PyErr_SetString(type, what.c_str());
@@ -469,6 +473,207 @@ PyObject* linear_backward_weight(PyObject*, PyObject* const* a, Py_ssize_t count
   END_HANDLE_TH_ERRORS
 }
 
+// ---- many tensors at once -----------------------------------------------------------------------
+
+// The items of a sequence.
+struct Items {
+  THPObjectPtr seq;
+  int64_t count = 0;
+  Items(PyObject* x, const char* what, int64_t wanted = -1) : seq(PySequence_Fast(x, "")) {
+    if (!seq) {
+      PyErr_Clear();
+      refuse(PyExc_TypeError, std::string(what) + ": a sequence expected");
+    }
+    count = PySequence_Fast_GET_SIZE(seq.get());
+    if (wanted >= 0 && count != wanted) bad(what, std::to_string(wanted) + " items expected, got " + std::to_string(count));
+  }
+  PyObject* operator[](int64_t i) const { return PySequence_Fast_GET_ITEM(seq.get(), i); }
+};
+
+std::string item(const char* what, int64_t i) { return std::string(what) + "[" + std::to_string(i) + "]"; }
+
+// What a call over many tensors has in hand: their device, and which memory it reads and writes.
+struct Many {
+  struct Piece {
+    uintptr_t at, end;
+    bool written;
+  };
+  std::vector<Piece> pieces;
+  at::Tensor like;
+  // A contiguous CUDA tensor of n values (n < 0: any number).
+  at::Tensor take(PyObject* x, const char* what, int64_t i, int64_t n, bool written) {
+    if (!THPVariable_Check(x)) refuse(PyExc_TypeError, item(what, i) + ": a CUDA tensor expected");
+    const at::Tensor& t = THPVariable_Unpack(x);
+    if (!t.is_cuda() || !t.is_contiguous() || (n >= 0 && t.numel() != n)) bad(item(what, i).c_str(), n >= 0 ? "a contiguous CUDA tensor of " + std::to_string(n) + " values expected" : "a contiguous CUDA tensor expected");
+    if (!like.defined()) like = t;
+    same_device(like, t);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(t.data_ptr());
+    if (t.numel() > 0) pieces.push_back({at, at + t.nbytes(), written});
+    return t;
+  }
+  // What is written is apart from everything else.
+  void check(const char* what) {
+    std::sort(pieces.begin(), pieces.end(), [](const Piece& a, const Piece& b) { return a.at < b.at; });
+    uintptr_t any = 0, written = 0;
+    for (const Piece& p : pieces) {
+      if (p.at < written || (p.written && p.at < any)) bad(what, "memory that is written is shared between the tensors of a call");
+      any = std::max(any, p.end);
+      if (p.written) written = std::max(written, p.end);
+    }
+  }
+};
+
+struct Pair {   // a tensor's moments
+  at::Tensor m, v, m_scales, v_scales;
+  int32_t type;
+};
+Pair moments_of(PyObject* x, int64_t i, int64_t n, Many& many, bool written) {
+  PyObject* const names[4] = {name_m, name_v, name_m_scales, name_v_scales};
+  THPObjectPtr got[4];
+  for (int k = 0; k < 4; ++k) {
+    got[k] = THPObjectPtr(PyObject_GetAttr(x, names[k]));
+    if (!got[k]) {
+      PyErr_Clear();
+      refuse(PyExc_TypeError, item("moments", i) + ": Moments expected");
+    }
+  }
+  Pair p;
+  p.m = many.take(got[0], "moments", i, n, written);
+  p.v = many.take(got[1], "moments", i, p.m.numel(), written);
+  const auto kind = p.m.scalar_type();
+  if (kind != p.v.scalar_type() || (kind != at::kFloat && kind != at::kByte)) bad(item("moments", i).c_str(), "both float32, or both bytes");
+  p.type = kind == at::kFloat ? MOC_F32 : MOC_E4M3;
+  if (p.type == MOC_E4M3) {
+    const int64_t blocks = (p.m.numel() + MOC_BLOCK - 1) / MOC_BLOCK;
+    p.m_scales = many.take(got[2], "moments", i, blocks, written);
+    p.v_scales = many.take(got[3], "moments", i, blocks, written);
+    if (p.m_scales.scalar_type() != at::kByte || p.v_scales.scalar_type() != at::kByte) bad(item("moments", i).c_str(), "scales are bytes");
+  } else if (got[2] != Py_None || got[3] != Py_None) {
+    bad(item("moments", i).c_str(), "moments in 32 bits have no scales");
+  }
+  return p;
+}
+
+double number(PyObject* x) {
+  const double v = PyFloat_AsDouble(x);
+  if (v == -1.0 && PyErr_Occurred()) throw python_error();
+  return v;
+}
+
+// A number, or where the device finds it: a tensor of one value.
+template <class T>
+const T* on_device(PyObject* x, const char* what, at::ScalarType type, Many& many) {
+  if (!THPVariable_Check(x)) return nullptr;
+  const at::Tensor t = many.take(x, what, 0, 1, false);
+  if (t.scalar_type() != type) bad(what, std::string("a number or a ") + c10::toString(type) + " tensor of one value expected");
+  return static_cast<const T*>(t.data_ptr());
+}
+
+// adamw_step(params, grads, moments, copies, decay, lr, step, beta1, beta2, eps, grad_scale, seed) -> code
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  arguments(count, 12, "adamw_step");
+  const Items params(a[0], "params"), grads(a[1], "grads", params.count), moments(a[2], "moments", params.count);
+  const int64_t tensors = params.count;
+  const bool copied = a[3] != Py_None, same_decay = PyFloat_Check(a[4]) || PyLong_Check(a[4]);
+  const Items copies(copied ? a[3] : a[0], "copies", tensors), decay(same_decay ? a[0] : a[4], "weight_decay", tensors);
+  Many many;
+  std::vector<moc_adamw_tensor> list((size_t)tensors);
+  for (int64_t i = 0; i < tensors; ++i) {
+    moc_adamw_tensor& t = list[(size_t)i];
+    t = {};
+    const at::Tensor p = many.take(params[i], "params", i, -1, true), g = many.take(grads[i], "grads", i, p.numel(), false);
+    if (p.sizes() != g.sizes()) bad(item("grads", i).c_str(), "of params' shape expected");
+    t.param_type = type_of(p.scalar_type(), "params");
+    t.grad_type = type_of(g.scalar_type(), "grads");
+    t.param = p.data_ptr();
+    t.grad = g.data_ptr();
+    t.count = p.numel();
+    const Pair pair = moments_of(moments[i], i, t.count, many, true);
+    t.m = pair.m.data_ptr();
+    t.v = pair.v.data_ptr();
+    t.moment_type = pair.type;
+    if (pair.type == MOC_E4M3) {
+      t.m_scales = static_cast<uint8_t*>(pair.m_scales.data_ptr());
+      t.v_scales = static_cast<uint8_t*>(pair.v_scales.data_ptr());
+    }
+    if (copied && copies[i] != Py_None) {
+      const at::Tensor c = many.take(copies[i], "copies", i, t.count, true);
+      if (p.sizes() != c.sizes()) bad(item("copies", i).c_str(), "of params' shape expected");
+      t.copy_type = type_of(c.scalar_type(), "copies");
+      if (t.copy_type == MOC_F32) bad(item("copies", i).c_str(), "float16 or bfloat16 expected");
+      t.copy = c.data_ptr();
+    }
+    const double d = number(same_decay ? a[4] : decay[i]);
+    if (!(d >= 0.0)) bad("weight_decay", "a number of 0 or more expected");
+    t.decay = (float)d;
+  }
+  moc_adamw_rule rule = {};
+  rule.lr_at = on_device<float>(a[5], "lr", at::kFloat, many);
+  rule.step_at = on_device<int64_t>(a[6], "step", at::kLong, many);
+  rule.grad_scale_at = a[10] == Py_None ? nullptr : on_device<float>(a[10], "grad_scale", at::kFloat, many);
+  rule.lr = rule.lr_at ? 0.0 : number(a[5]);
+  rule.step = rule.step_at ? 1 : PyLong_AsLongLong(a[6]);
+  if (rule.step == -1 && PyErr_Occurred()) throw python_error();
+  rule.grad_scale = a[10] == Py_None || rule.grad_scale_at ? 1.0 : number(a[10]);
+  rule.beta1 = number(a[7]);
+  rule.beta2 = number(a[8]);
+  rule.eps = number(a[9]);
+  rule.seed = PyLong_AsUnsignedLongLongMask(a[11]);
+  if (PyErr_Occurred()) throw python_error();
+  if (tensors == 0) return PyLong_FromLong(MOC_OK);
+  many.check("adamw_step");
+  void* const stream = stream_for(many.like);
+  return PyLong_FromLong(released([&] { return calls.adamw_step(tensors, list.data(), &rule, stream); }));
+  END_HANDLE_TH_ERRORS
+}
+
+// moments_read(moments, dtype, out) -> (code, [(m, v)..])
+PyObject* moments_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  arguments(count, 3, "moments_read");
+  const Items moments(a[0], "moments"), out(a[2] == Py_None ? a[0] : a[2], "out", moments.count);
+  Many many;
+  std::vector<moc_moments_tensor> list((size_t)moments.count);
+  THPObjectPtr results(PyList_New(moments.count));
+  if (!results) throw python_error();
+  for (int64_t i = 0; i < moments.count; ++i) {
+    moc_moments_tensor& t = list[(size_t)i];
+    t = {};
+    const Pair pair = moments_of(moments[i], i, -1, many, false);
+    t.m = pair.m.data_ptr();
+    t.v = pair.v.data_ptr();
+    t.count = pair.m.numel();
+    t.moment_type = pair.type;
+    if (pair.type == MOC_E4M3) {
+      t.m_scales = static_cast<const uint8_t*>(pair.m_scales.data_ptr());
+      t.v_scales = static_cast<const uint8_t*>(pair.v_scales.data_ptr());
+    }
+    THPObjectPtr made;
+    if (a[2] == Py_None) {
+      const at::ScalarType type = dtype_of(a[1], at::kFloat);
+      made = THPObjectPtr(PyTuple_Pack(2, wrapped(room_for(pair.m, type, pair.m.sizes())).get(), wrapped(room_for(pair.m, type, pair.m.sizes())).get()));
+      if (!made) throw python_error();
+    } else {
+      Py_INCREF(out[i]);
+      made = THPObjectPtr(out[i]);
+    }
+    const Items two(made, "out", 2);
+    const at::Tensor m = many.take(two[0], "out", i, t.count, true), v = many.take(two[1], "out", i, t.count, true);
+    if (m.scalar_type() != v.scalar_type()) bad(item("out", i).c_str(), "tensors of one type expected");
+    t.value_type = type_of(m.scalar_type(), "out");
+    t.m_values = m.data_ptr();
+    t.v_values = v.data_ptr();
+    PyList_SET_ITEM(results.get(), i, made.release());
+  }
+  if (moments.count == 0) return Py_BuildValue("iN", MOC_OK, results.release());
+  many.check("moments_read");
+  void* const stream = stream_for(many.like);
+  const int code = released([&] { return calls.moments_read(moments.count, list.data(), stream); });
+  return Py_BuildValue("iN", code, results.release());
+  END_HANDLE_TH_ERRORS
+}
+
 // shares((address, rows, bytes of a row, from one row to the next) twice): whether two matrices share memory
 PyObject* shares(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
@@ -499,6 +704,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
   take(c.linear_backward_input, "moc_linear_backward_input");
   take(c.linear_backward_weight, "moc_linear_backward_weight");
   take(c.linear_work, "moc_linear_work");
+  take(c.adamw_step, "moc_adamw_step");
+  take(c.moments_read, "moc_moments_read");
   calls = c;
   Py_INCREF(a[0]);
   Py_INCREF(a[1]);
@@ -512,7 +719,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
 
 #define MOC_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MOC_METHOD(bind), MOC_METHOD(checkpoint_write), MOC_METHOD(checkpoint_read), MOC_METHOD(norm_forward), MOC_METHOD(norm_backward), MOC_METHOD(linear_forward),
-                         MOC_METHOD(linear_backward_input), MOC_METHOD(linear_backward_weight), MOC_METHOD(shares), {nullptr, nullptr, 0, nullptr}};
+                         MOC_METHOD(linear_backward_input), MOC_METHOD(linear_backward_weight), MOC_METHOD(adamw_step), MOC_METHOD(moments_read), MOC_METHOD(shares), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_training", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -522,7 +729,11 @@ PyMODINIT_FUNC PyInit__training() {
   name_codes = PyUnicode_InternFromString("codes");
   name_scales = PyUnicode_InternFromString("scales");
   name_fmt = PyUnicode_InternFromString("fmt");
-  PyObject* const made = name_codes && name_scales && name_fmt ? PyModule_Create(&module) : nullptr;
+  name_m = PyUnicode_InternFromString("m");
+  name_v = PyUnicode_InternFromString("v");
+  name_m_scales = PyUnicode_InternFromString("m_scales");
+  name_v_scales = PyUnicode_InternFromString("v_scales");
+  PyObject* const made = name_codes && name_scales && name_fmt && name_m && name_v && name_m_scales && name_v_scales ? PyModule_Create(&module) : nullptr;
   if (made && PyModule_AddIntConstant(made, "training_version", MOC_TRAINING_VERSION) != 0) {
     Py_DECREF(made);
     return nullptr;

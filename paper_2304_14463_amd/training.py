@@ -20,7 +20,7 @@ import ctypes
 
 from . import moccasin as moc
 
-MOC_TRAINING_VERSION = 2
+MOC_TRAINING_VERSION = 3
 MOC_F32, MOC_F16, MOC_BF16, MOC_E4M3, MOC_I8 = range(5)
 FORMATS = {"e4m3": MOC_E4M3, "int8": MOC_I8}
 ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -28,7 +28,8 @@ PRODUCTS = {"forward": 0, "backward_input": 1, "backward_weight": 2}
 BLOCK = 32
 
 EXPORTS = ("moc_checkpoint_write", "moc_checkpoint_read", "moc_norm_forward", "moc_norm_backward", "moc_norm_backward_work", "moc_linear_forward",
-           "moc_linear_backward_input", "moc_linear_backward_weight", "moc_linear_work", "moc_linear_parts", "moc_training_version")
+           "moc_linear_backward_input", "moc_linear_backward_weight", "moc_linear_work", "moc_linear_parts",
+           "moc_adamw_step", "moc_moments_read", "moc_training_version")
 
 
 class Matrix(ctypes.Structure):
@@ -57,6 +58,20 @@ class Checkpoint:
         return self.codes.numel() + self.scales.numel()
 
 
+class Moments:
+    """A tensor's two moments: float32 `m` and `v`, or in 8 bits uint8 `m` and `v` of as many values, and the scales of 32 of
+    them each, uint8 `m_scales` and `v_scales`."""
+
+    __slots__ = ("m", "v", "m_scales", "v_scales")
+
+    def __init__(self, m, v, m_scales=None, v_scales=None):
+        self.m, self.v, self.m_scales, self.v_scales = m, v, m_scales, v_scales
+
+    @property
+    def nbytes(self):
+        return sum(x.numel() * x.element_size() for x in (self.m, self.v, self.m_scales, self.v_scales) if x is not None)
+
+
 _lib = None
 _native = None
 
@@ -81,6 +96,8 @@ def lib():
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
         for name, args in (("moc_norm_backward_work", [I64, I64]), ("moc_linear_work", [I64, I64, I64])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, I64
+        for name, args in (("moc_adamw_step", [I64, VP, VP, VP]), ("moc_moments_read", [I64, VP, VP])):
+            getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
         L.moc_linear_parts.argtypes, L.moc_linear_parts.restype = [I32, I64, I64, I64, I32, I32, ctypes.POINTER(I64)], ctypes.c_int
         _lib = L
     return _lib
@@ -202,3 +219,30 @@ def moc_linear_parts(product, rows, cin, cout, aligned=True, units=0):
     out = (ctypes.c_int64 * 5)()
     moc._check(lib().moc_linear_parts(PRODUCTS[product], rows, cin, cout, int(aligned), units, out), "moc_linear_parts")
     return Parts(out[0], bool(out[1]), *out[2:])
+
+
+def zero_moments(param, bits=8):
+    """Moments of zeros for a parameter, in 32 or 8 bits a value."""
+    torch = moc._tc()
+    if bits not in (8, 32):
+        raise ValueError(f"bits {bits!r}: expected 8 or 32")
+    dtype = torch.float32 if bits == 32 else torch.uint8
+    scales = lambda: torch.zeros(-(-param.numel() // BLOCK), dtype=torch.uint8, device=param.device) if bits == 8 else None   # noqa: E731
+    return Moments(*(torch.zeros(param.shape, dtype=dtype, device=param.device) for _ in range(2)), scales(), scales())
+
+
+def moc_adamw_step(params, grads, moments, lr, step, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, copies=None, grad_scale=None, seed=0, stream=None):
+    """A step of AdamW over many tensors, in place: `params`, `moments` (a Moments each) and `copies`, whose items are float16 or
+    bfloat16 tensors for the parameters' new values, or None.  Tensors are contiguous.  `step` counts from 1; `weight_decay`
+    is a number, or one for each tensor; gradients are taken times `grad_scale`.  `lr`, `step` and `grad_scale` may be CUDA tensors of one
+    value (float32, int64, float32), which are read when the step runs: a captured call then finds each replay's own.
+    `seed`: of the random bits that moments in 8 bits are rounded with (the step is mixed in)."""
+    code = _call("adamw_step", stream, params, grads, moments, copies, weight_decay, lr, step, *betas, eps, grad_scale, seed)
+    moc._check(code, "moc_adamw_step")
+
+
+def moc_moments_read(moments, dtype=None, out=None, stream=None):
+    """[(m, v)..]: what the moments stand for, as tensors of `dtype` (default float32) or in those of `out`, pairs of tensors."""
+    code, out = _call("moments_read", stream, moments, dtype, out)
+    moc._check(code, "moc_moments_read")
+    return out

@@ -1,0 +1,82 @@
+"""What the C ABI of the operators around a plan's layers refuses before anything touches a device.  No GPU."""
+import ctypes
+
+import pytest
+
+F32, F16, BF16, E4M3, I8 = range(5)
+A = 1 << 20   # an aligned address; nothing looks at it
+P, I32, I64, U64, D, F = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_uint64, ctypes.c_double, ctypes.c_float
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2304_14463_amd import training
+    return training.lib()
+
+
+class Tensor(ctypes.Structure):
+    """moc_adamw_tensor"""
+    _fields_ = [("param", P), ("grad", P), ("m", P), ("v", P), ("m_scales", P), ("v_scales", P), ("copy", P), ("count", I64), ("param_type", I32), ("grad_type", I32),
+                ("moment_type", I32), ("copy_type", I32), ("decay", F), ("reserved", I32)]
+
+
+class Rule(ctypes.Structure):
+    """moc_adamw_rule"""
+    _fields_ = [("lr", D), ("beta1", D), ("beta2", D), ("eps", D), ("grad_scale", D), ("step", I64), ("seed", U64), ("lr_at", P), ("grad_scale_at", P), ("step_at", P)]
+
+
+class Read(ctypes.Structure):
+    """moc_moments_tensor"""
+    _fields_ = [("m", P), ("v", P), ("m_scales", P), ("v_scales", P), ("m_values", P), ("v_values", P), ("count", I64), ("moment_type", I32), ("value_type", I32)]
+
+
+def test_adamw(lib):
+    def call(tensors=1, rule=None, **changed):
+        t = Tensor(A, A, A, A, A, A, None, 64, F32, BF16, E4M3, F16, 0.1, 0)
+        r = Rule(1e-3, 0.9, 0.999, 1e-8, 1.0, 1, 0, None, None, None)
+        for k, v in changed.items():
+            setattr(r if k in dict(Rule._fields_) else t, k, v)
+        return lib.moc_adamw_step(tensors, ctypes.byref(t), ctypes.byref(r) if rule is None else rule, None)
+
+    nan, inf = float("nan"), float("inf")
+    for bad in (dict(param=None), dict(grad=None), dict(m=None), dict(v=None), dict(m_scales=None), dict(v_scales=None), dict(param=A + 2), dict(grad=A + 1), dict(param_type=E4M3), dict(grad_type=5),
+                dict(moment_type=F16), dict(moment_type=I8), dict(moment_type=F32, m=A + 2), dict(moment_type=F32, v=A + 1), dict(copy=A, copy_type=F32), dict(copy=A + 1), dict(count=-1),
+                dict(count=(1 << 40) + 1), dict(decay=-0.1), dict(decay=nan), dict(decay=inf), dict(reserved=1), dict(lr=nan), dict(lr=1e300), dict(beta1=1.0), dict(beta1=-0.1), dict(beta2=1.5), dict(beta2=nan),
+                dict(eps=0.0), dict(eps=-1.0), dict(eps=1e-50), dict(eps=nan), dict(grad_scale=inf), dict(step=0), dict(step=-5), dict(lr_at=A + 2), dict(step_at=A + 4), dict(grad_scale_at=A + 1),
+                dict(tensors=-1)):
+        assert call(**bad) == -1, bad
+    assert lib.moc_adamw_step(1, None, ctypes.byref(Rule(1e-3, 0.9, 0.999, 1e-8, 1.0, 1)), None) == -1
+    assert lib.moc_adamw_step(1, ctypes.byref(Tensor()), None, None) == -1
+    # nothing to do: no device is asked
+    assert call(tensors=0) == 0 and call(count=0, param=None, m=None) == 0
+
+
+def test_moments_read(lib):
+    def call(tensors=1, **changed):
+        t = Read(A, A, A, A, A, A, 64, E4M3, BF16)
+        for k, v in changed.items():
+            setattr(t, k, v)
+        return lib.moc_moments_read(tensors, ctypes.byref(t), None)
+
+    for bad in (dict(m=None), dict(v=None), dict(m_scales=None), dict(v_scales=None), dict(m_values=None), dict(v_values=None), dict(m_values=A + 1), dict(v_values=A + 2, value_type=F32), dict(count=-1),
+                dict(moment_type=BF16), dict(value_type=E4M3), dict(value_type=-1), dict(moment_type=F32, m=A + 2), dict(tensors=-1)):
+        assert call(**bad) == -1, bad
+    assert lib.moc_moments_read(1, None, None) == -1
+    assert call(count=0, m=None) == 0 and call(tensors=0) == 0
+
+
+def test_what_is_on_no_gpu(lib):
+    import torch
+
+    from paper_2304_14463_amd import training as tr
+    x = torch.zeros(64)
+    with pytest.raises(ValueError):
+        tr.moc_adamw_step([x], [x], [tr.zero_moments(x)], 1e-3, 1)
+    with pytest.raises(ValueError):
+        tr.moc_moments_read([tr.zero_moments(x)])
+    with pytest.raises(ValueError):
+        tr.zero_moments(x, 16)
+    assert tr.zero_moments(x).nbytes == 132 and tr.zero_moments(x, 32).nbytes == 512
+    for bad in (None, 3, [3], [x, "y"]):
+        with pytest.raises((TypeError, ValueError)):
+            tr.moc_adamw_step(bad, [x], [tr.zero_moments(x)], 1e-3, 1)
