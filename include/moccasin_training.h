@@ -212,6 +212,45 @@ int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout);
 int moc_linear_parts(int32_t product, int64_t rows, int64_t cin, int64_t cout, int32_t aligned, int32_t units, int64_t* out);
 
 /*
+ * Log probabilities of rows of logits, z = scale * logits:
+ *   lse = log sum over the columns of exp(z),  logp = z[token] - lse,
+ *   entropy = lse - sum of p z  with p = exp(z - lse),
+ * and the `top` most likely columns: the largest logits in falling order, equal
+ * ones by column (-0 equals 0).
+ *   logits  [rows][vocab], float32, float16 or bfloat16
+ *   scale   2^-64 .. 2^64 (of a temperature, its inverse)
+ *   tokens  device, [rows] of token_bytes (4 or 8), signed, or NULL.  Below 0: no
+ *           token, logp is 0 and has no gradient; from vocab on: logp and the
+ *           row's gradient are NaN
+ *   top     0 .. 64, at most vocab
+ *   logp    device, float [rows], NULL without tokens;  lse, entropy  float [rows]
+ *   top_logp, top_tokens  device, float and int64 [rows][top], NULL where top is 0
+ *   work    moc_logprob_forward_work(rows, vocab, top) bytes (may be 0)
+ * Logits of -infinity have p = 0; a p below 2^-126 may count as 0.  A row of nothing else: lse and logp
+ * -infinity, entropy 0, no gradient.  A row with NaN or +infinity: all NaN, columns -1.
+ * Sums are held in 32 bits.  vocab >= 1; rows == 0 is a no-op.
+ * Errors: MOC_EINVAL, MOC_EHIP.
+ */
+int64_t moc_logprob_forward_work(int64_t rows, int64_t vocab, int32_t top);
+int moc_logprob_forward(int64_t rows, int64_t vocab, const moc_matrix* logits, const void* tokens, int32_t token_bytes,
+                        float scale, int32_t top, float* logp, float* lse, float* entropy, float* top_logp,
+                        int64_t* top_tokens, void* work, int64_t work_bytes, void* hip_stream);
+
+/*
+ * The gradient of logp and entropy with regard to the logits:
+ *   out = scale * (dlogp * ([column == token] - p) - dentropy * p * (z - lse + entropy))
+ *   lse, entropy     as the forward pass has left them; entropy NULL without dentropy
+ *   tokens, dlogp    device, float [rows]: both or neither
+ *   dentropy         device, float [rows], or NULL
+ *   out              [rows][vocab], the logits' type or float32; may be the logits' own
+ *                    memory (same type and stride)
+ * Errors: MOC_EINVAL, MOC_EHIP.
+ */
+int moc_logprob_backward(int64_t rows, int64_t vocab, const moc_matrix* logits, const float* lse, const float* entropy,
+                         const void* tokens, int32_t token_bytes, const float* dlogp, const float* dentropy, float scale,
+                         const moc_matrix* out, void* hip_stream);
+
+/*
  * AdamW over many tensors at once, in place:
  *   g = grad_scale * grad
  *   m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2

@@ -31,6 +31,9 @@ struct Calls {
   decltype(&moc_linear_backward_input) linear_backward_input;
   decltype(&moc_linear_backward_weight) linear_backward_weight;
   decltype(&moc_linear_work) linear_work;
+  decltype(&moc_logprob_forward_work) logprob_forward_work;
+  decltype(&moc_logprob_forward) logprob_forward;
+  decltype(&moc_logprob_backward) logprob_backward;
   decltype(&moc_adamw_step) adamw_step;
   decltype(&moc_moments_read) moments_read;
 } calls;
@@ -473,6 +476,100 @@ PyObject* linear_backward_weight(PyObject*, PyObject* const* a, Py_ssize_t count
   END_HANDLE_TH_ERRORS
 }
 
+// ---- log probabilities --------------------------------------------------------------------------
+
+double number(PyObject* x) {
+  const double v = PyFloat_AsDouble(x);
+  if (v == -1.0 && PyErr_Occurred()) throw python_error();
+  return v;
+}
+
+// A vector of floats that may be missing.
+Vector floats_or_none(PyObject* p, int64_t n, const char* what, const at::Tensor& beside) { return p == Py_None ? Vector{} : vector(p, n, what, beside, true); }
+
+void apart(const Held& out, const char* name, const Vector& in, const char* what) {
+  if (!out.there || !in.data || in.x.numel() == 0) return;
+  if (shared(out.span(), Span{reinterpret_cast<uintptr_t>(in.data), 1, (int64_t)in.x.nbytes(), 1})) bad(name, std::string("shares memory with ") + what);
+}
+
+// n signed numbers of 4 or 8 bytes, or none.
+struct Tokens {
+  Vector v;
+  int32_t bytes = 0;
+};
+Tokens tokens_of(PyObject* p, int64_t n, const at::Tensor& beside) {
+  Tokens t;
+  if (p == Py_None) return t;
+  if (THPVariable_Check(p)) t.v.x = THPVariable_Unpack(p);
+  const at::Tensor& x = t.v.x;
+  if (!x.defined() || !x.is_cuda() || !x.is_contiguous() || x.dim() != 1 || x.numel() != n || (x.scalar_type() != at::kInt && x.scalar_type() != at::kLong))
+    bad("tokens", "a contiguous int32 or int64 CUDA tensor of " + std::to_string(n) + " values expected");
+  same_device(beside, x);
+  t.v.data = x.data_ptr();
+  t.bytes = (int32_t)x.element_size();
+  return t;
+}
+
+PyObject* none() {
+  Py_INCREF(Py_None);
+  return Py_None;
+}
+
+// logprob_forward(logits, tokens, scale, top, work) -> (code, logp, lse, entropy, top_logp, top_tokens)
+PyObject* logprob_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  arguments(count, 5, "logprob_forward");
+  const Held x = held(a[0], "logits");
+  if (x.kept) bad("logits", "a tensor expected");
+  const Tokens tokens = tokens_of(a[1], x.rows, x.values);
+  const double scale = number(a[2]);
+  const long top = PyLong_AsLong(a[3]);
+  if (top == -1 && PyErr_Occurred()) throw python_error();
+  if (top < 0 || top > 64 || top > x.cols) bad("top", "a number from 0 to 64, at most that of the columns, expected");
+  at::Tensor sums = room_for(x.values, at::kFloat, {3, x.rows}), top_logp, top_tokens;
+  if (top > 0) {
+    top_logp = room_for(x.values, at::kFloat, {x.rows, top});
+    top_tokens = room_for(x.values, at::kLong, {x.rows, top});
+  }
+  const Work work = workspace(a[4], a[4] == Py_None ? calls.logprob_forward_work(x.rows, x.cols, (int32_t)top) : 0, x.values);
+  float* const room = static_cast<float*>(sums.data_ptr());
+  void* const stream = stream_for(x.values);
+  const int code = released([&] {
+    return calls.logprob_forward(x.rows, x.cols, x.get(), tokens.v.data, tokens.bytes, (float)scale, (int32_t)top, tokens.bytes ? room : nullptr, room + x.rows, room + 2 * x.rows,
+                                 top > 0 ? static_cast<float*>(top_logp.data_ptr()) : nullptr, top > 0 ? static_cast<int64_t*>(top_tokens.data_ptr()) : nullptr, work.data, work.bytes,
+                                 stream);
+  });
+  return Py_BuildValue("iNNNNN", code, tokens.bytes ? wrapped(sums.select(0, 0)).release() : none(), wrapped(sums.select(0, 1)).release(), wrapped(sums.select(0, 2)).release(),
+                       top > 0 ? wrapped(std::move(top_logp)).release() : none(), top > 0 ? wrapped(std::move(top_tokens)).release() : none());
+  END_HANDLE_TH_ERRORS
+}
+
+// logprob_backward(logits, lse, tokens, dlogp, entropy, dentropy, scale, dtype, out) -> (code, out)
+PyObject* logprob_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  arguments(count, 9, "logprob_backward");
+  const Held x = held(a[0], "logits");
+  if (x.kept) bad("logits", "a tensor expected");
+  const Vector lse = vector(a[1], x.rows, "lse", x.values, true), dlogp = floats_or_none(a[3], x.rows, "dlogp", x.values), entropy = floats_or_none(a[4], x.rows, "entropy", x.values),
+               dentropy = floats_or_none(a[5], x.rows, "dentropy", x.values);
+  const Tokens tokens = tokens_of(a[2], x.rows, x.values);
+  if (a[2] == Py_None && a[3] != Py_None) bad("dlogp", "tokens are missing");
+  if (a[5] != Py_None && a[4] == Py_None) bad("dentropy", "the entropy is missing");
+  const double scale = number(a[6]);
+  THPObjectPtr out = result(a[8], x.values, dtype_of(a[7], x.values.scalar_type()), x.rows, x.cols);
+  const Held d = held(out, "out", x.rows, x.cols);
+  same_device(x.values, d.values);
+  apart(d, "out", x, "logits", true);
+  for (const Vector* v : {&lse, &dlogp, &entropy, &dentropy, &tokens.v}) apart(d, "out", *v, "a vector of the call");
+  void* const stream = stream_for(x.values);
+  const int code = released([&] {
+    return calls.logprob_backward(x.rows, x.cols, x.get(), static_cast<const float*>(lse.data), static_cast<const float*>(entropy.data), dlogp.data ? tokens.v.data : nullptr, tokens.bytes,
+                                  static_cast<const float*>(dlogp.data), static_cast<const float*>(dentropy.data), (float)scale, d.get(), stream);
+  });
+  return Py_BuildValue("iN", code, out.release());
+  END_HANDLE_TH_ERRORS
+}
+
 // ---- many tensors at once -----------------------------------------------------------------------
 
 // The items of a sequence.
@@ -552,12 +649,6 @@ Pair moments_of(PyObject* x, int64_t i, int64_t n, Many& many, bool written) {
     bad(item("moments", i).c_str(), "moments in 32 bits have no scales");
   }
   return p;
-}
-
-double number(PyObject* x) {
-  const double v = PyFloat_AsDouble(x);
-  if (v == -1.0 && PyErr_Occurred()) throw python_error();
-  return v;
 }
 
 // A number, or where the device finds it: a tensor of one value.
@@ -704,6 +795,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
   take(c.linear_backward_input, "moc_linear_backward_input");
   take(c.linear_backward_weight, "moc_linear_backward_weight");
   take(c.linear_work, "moc_linear_work");
+  take(c.logprob_forward_work, "moc_logprob_forward_work");
+  take(c.logprob_forward, "moc_logprob_forward");
+  take(c.logprob_backward, "moc_logprob_backward");
   take(c.adamw_step, "moc_adamw_step");
   take(c.moments_read, "moc_moments_read");
   calls = c;
@@ -719,7 +813,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
 
 #define MOC_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MOC_METHOD(bind), MOC_METHOD(checkpoint_write), MOC_METHOD(checkpoint_read), MOC_METHOD(norm_forward), MOC_METHOD(norm_backward), MOC_METHOD(linear_forward),
-                         MOC_METHOD(linear_backward_input), MOC_METHOD(linear_backward_weight), MOC_METHOD(adamw_step), MOC_METHOD(moments_read), MOC_METHOD(shares), {nullptr, nullptr, 0, nullptr}};
+                         MOC_METHOD(linear_backward_input), MOC_METHOD(linear_backward_weight), MOC_METHOD(logprob_forward), MOC_METHOD(logprob_backward), MOC_METHOD(adamw_step), MOC_METHOD(moments_read), MOC_METHOD(shares), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_training", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -29,7 +29,7 @@ BLOCK = 32
 
 EXPORTS = ("moc_checkpoint_write", "moc_checkpoint_read", "moc_norm_forward", "moc_norm_backward", "moc_norm_backward_work", "moc_linear_forward",
            "moc_linear_backward_input", "moc_linear_backward_weight", "moc_linear_work", "moc_linear_parts",
-           "moc_adamw_step", "moc_moments_read", "moc_training_version")
+           "moc_logprob_forward_work", "moc_logprob_forward", "moc_logprob_backward", "moc_adamw_step", "moc_moments_read", "moc_training_version")
 
 
 class Matrix(ctypes.Structure):
@@ -94,9 +94,10 @@ def lib():
                            ("moc_linear_backward_input", [I64, I64, I64, M, M, I32, M, M, VP, I64, VP]),
                            ("moc_linear_backward_weight", [I64, I64, I64, M, M, M, VP, VP, I64, VP])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
-        for name, args in (("moc_norm_backward_work", [I64, I64]), ("moc_linear_work", [I64, I64, I64])):
+        for name, args in (("moc_norm_backward_work", [I64, I64]), ("moc_linear_work", [I64, I64, I64]), ("moc_logprob_forward_work", [I64, I64, I32])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, I64
-        for name, args in (("moc_adamw_step", [I64, VP, VP, VP]), ("moc_moments_read", [I64, VP, VP])):
+        for name, args in (("moc_logprob_forward", [I64, I64, M, VP, I32, F32, I32, VP, VP, VP, VP, VP, VP, I64, VP]),
+                           ("moc_logprob_backward", [I64, I64, M, VP, VP, VP, I32, VP, VP, F32, M, VP]), ("moc_adamw_step", [I64, VP, VP, VP]), ("moc_moments_read", [I64, VP, VP])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
         L.moc_linear_parts.argtypes, L.moc_linear_parts.restype = [I32, I64, I64, I64, I32, I32, ctypes.POINTER(I64)], ctypes.c_int
         _lib = L
@@ -219,6 +220,26 @@ def moc_linear_parts(product, rows, cin, cout, aligned=True, units=0):
     out = (ctypes.c_int64 * 5)()
     moc._check(lib().moc_linear_parts(PRODUCTS[product], rows, cin, cout, int(aligned), units, out), "moc_linear_parts")
     return Parts(out[0], bool(out[1]), *out[2:])
+
+
+LogProbs = collections.namedtuple("LogProbs", "logp lse entropy top_logp top_tokens")
+
+
+def moc_logprob_forward(logits, tokens=None, scale=1.0, top=0, work=None, stream=None):
+    """Log probabilities of the rows of `logits` times `scale`: (logp of `tokens` (int32 or int64 [rows]; below 0: none), lse, entropy, float32
+    [rows]; log probabilities and columns of the `top` most likely ones, float32 and int64 [rows, top]); None for what is not
+    asked for."""
+    code, *out = _call("logprob_forward", stream, logits, tokens, scale, top, work)
+    moc._check(code, "moc_logprob_forward")
+    return LogProbs(*out)
+
+
+def moc_logprob_backward(logits, lse, tokens=None, dlogp=None, entropy=None, dentropy=None, scale=1.0, dtype=None, out=None, stream=None):
+    """The gradient with regard to the logits from those of logp and of the entropy, float32 [rows], and what the forward pass has
+    left.  `dtype`: the logits' (default) or float32; `out` may be the logits."""
+    code, out = _call("logprob_backward", stream, logits, lse, tokens, dlogp, entropy, dentropy, scale, dtype, out)
+    moc._check(code, "moc_logprob_backward")
+    return out
 
 
 def zero_moments(param, bits=8):

@@ -65,6 +65,34 @@ def test_moments_read(lib):
     assert call(count=0, m=None) == 0 and call(tensors=0) == 0
 
 
+def test_logprob(lib):
+    from paper_2304_14463_amd.training import Matrix
+
+    def mat(type_=BF16, cols=64, stride=None, data=A, reserved=0):
+        return Matrix(data, A if type_ >= E4M3 else None, cols if stride is None else stride, 2, type_, reserved)
+
+    def forward(rows=4, vocab=64, logits=mat(), tokens=A, bytes_=8, scale=1.0, top=5, logp=A, lse=A, entropy=A, top_logp=A, top_tokens=A):
+        return lib.moc_logprob_forward(rows, vocab, logits, tokens, bytes_, scale, top, logp, lse, entropy, top_logp, top_tokens, None, 0, None)
+
+    def backward(rows=4, vocab=64, logits=mat(), lse=A, entropy=A, tokens=A, bytes_=8, dlogp=A, dentropy=A, scale=1.0, out=mat()):
+        return lib.moc_logprob_backward(rows, vocab, logits, lse, entropy, tokens, bytes_, dlogp, dentropy, scale, out, None)
+
+    matrices = [None, mat(7), mat(E4M3), mat(I8), mat(stride=63), mat(data=None), mat(data=A + 1), mat(F32, data=A + 2), mat(stride=1 << 23), mat(reserved=1)]
+    nan, inf = float("nan"), float("inf")
+    for bad in [dict(logits=x) for x in matrices] + [dict(rows=-1), dict(rows=1 << 31), dict(vocab=0), dict(vocab=-1), dict(vocab=1 << 23), dict(bytes_=2), dict(tokens=A + 4), dict(tokens=A + 2, bytes_=4),
+                                                     dict(scale=0.0), dict(scale=-1.0), dict(scale=nan), dict(scale=inf), dict(scale=1e30), dict(scale=1e-30)]:
+        assert forward(**bad) == -1 and backward(**bad) == -1, bad
+    for bad in (dict(top=-1), dict(top=65), dict(vocab=4, logits=mat(cols=4)), dict(logp=None), dict(tokens=None), dict(lse=None), dict(entropy=None), dict(top_logp=None), dict(top_tokens=None),
+                dict(logp=A + 2), dict(lse=A + 1), dict(entropy=A + 2), dict(top_logp=A + 2), dict(top_tokens=A + 4)):
+        assert forward(**bad) == -1, bad
+    for bad in [dict(out=x) for x in matrices] + [dict(out=mat(F16)), dict(lse=None), dict(lse=A + 2), dict(tokens=None), dict(dlogp=None), dict(dlogp=A + 1), dict(entropy=None), dict(entropy=A + 2), dict(dentropy=A + 2)]:
+        assert backward(**bad) == -1, bad
+    none = mat(data=None)
+    assert forward(rows=0, logits=none, tokens=None, logp=None, lse=None, entropy=None) == 0 and backward(rows=0, logits=none, out=none, lse=None) == 0
+    for sizes in ((-1, 64, 0), (4, 0, 0), (4, 64, 65), (4, 8, 9), (4, 64, -1)):
+        assert lib.moc_logprob_forward_work(*sizes) == -1
+
+
 def test_what_is_on_no_gpu(lib):
     import torch
 
@@ -77,6 +105,14 @@ def test_what_is_on_no_gpu(lib):
     with pytest.raises(ValueError):
         tr.zero_moments(x, 16)
     assert tr.zero_moments(x).nbytes == 132 and tr.zero_moments(x, 32).nbytes == 512
+    m = torch.zeros(4, 64)
+    for call in (lambda: tr.moc_logprob_forward(m), lambda: tr.moc_logprob_backward(m, x[:4])):
+        with pytest.raises(ValueError):
+            call()
+    for bad in (None, 3, [1.0], "x"):
+        for call in (lambda: tr.moc_logprob_forward(bad), lambda: tr.moc_logprob_backward(bad, bad)):
+            with pytest.raises(TypeError):
+                call()
     for bad in (None, 3, [3], [x, "y"]):
         with pytest.raises((TypeError, ValueError)):
             tr.moc_adamw_step(bad, [x], [tr.zero_moments(x)], 1e-3, 1)
