@@ -212,6 +212,70 @@ int64_t moc_linear_work(int64_t rows, int64_t cin, int64_t cout);
 int moc_linear_parts(int32_t product, int64_t rows, int64_t cin, int64_t cout, int32_t aligned, int32_t units, int64_t* out);
 
 /*
+ * The residual connection between two blocks:
+ *   h = after(block), or block     the norm behind the block
+ *   r = scale * x + gate h         the stream; without x: gate h
+ *   n = before(r)                  the norm before the next block, of r as it is before its rounding
+ * A norm is layer norm as above, or by the root of the squares alone, gamma * v /
+ * sqrt(mean(v^2) + eps).
+ *   x       float32, float16 or bfloat16, or NULL
+ *   block   a tensor or a checkpoint
+ *   gate    [gates][cols] of values: row i takes row i / (rows / gates); gates
+ *           divides rows.  NULL with 0 gates
+ *   after, before  NULL or of kind MOC_NORM_NONE: none
+ *   r       NULL: not kept; may be x's or the block's own memory (same type and stride)
+ *   n       NULL without `before`; may be x's or the block's own memory, but not r's
+ *   kept    a checkpoint that n is written to before its rounding (its E is that of
+ *           n's type), or NULL
+ * cols 1 .. MOC_RESIDUAL_MAX_COLS; rows == 0 is a no-op; r or n is wanted.  Statistics
+ * and sums are held in 32 bits.  Errors: MOC_EINVAL, MOC_EHIP.
+ */
+#define MOC_NORM_NONE  0
+#define MOC_NORM_LAYER 1
+#define MOC_NORM_RMS   2
+
+#define MOC_RESIDUAL_MAX_COLS 16384
+
+typedef struct {
+  int32_t kind;             /* MOC_NORM_NONE .. MOC_NORM_RMS */
+  int32_t param_type;       /* float32, float16, bfloat16 */
+  const void *gamma, *beta; /* device, [cols]; NULL: 1 and 0; MOC_NORM_RMS has no beta */
+  float *mean, *rstd;       /* device, [rows]: written by the forward, read by the backward pass; MOC_NORM_RMS has no mean */
+  float eps;                /* >= 0 */
+  int32_t reserved;         /* 0 */
+} moc_row_norm;
+
+int moc_residual_forward(int64_t rows, int64_t cols, const moc_matrix* x, const moc_matrix* block, const moc_matrix* gate,
+                         int64_t gates, float scale, const moc_row_norm* after, const moc_row_norm* before,
+                         const moc_matrix* r, const moc_matrix* n, const moc_matrix* kept, void* hip_stream);
+
+/*
+ * Its gradients.  With norm' a norm's gradient as above (without the mean's
+ * part for MOC_NORM_RMS):
+ *   d = dr + before'(dn),  dx = scale * d,  dgate = sum over a gate's rows of d h,
+ *   dblock = after'(gate d), or gate d
+ *   dr      the stream's gradient, or NULL;  dn  n's, NULL without `before`; one of them is there
+ *   r       as the forward pass has left it, or a checkpoint of it; looked at with `before` only
+ *   block   as it was given to the forward pass; looked at with `after` or for dgate
+ *   dx, dblock  values, NULL: not wanted.  dx may be dr's or r's own memory, dblock dn's or the block's (same type and
+ *           stride), but not each other's
+ *   grads   the parameters' gradients, device, float [cols] (gate: [gates][cols]),
+ *           or NULL; each NULL: not wanted.  With rows == 0 they are set to zero.
+ *   work    moc_residual_backward_work bytes; not needed without grads
+ * Errors: MOC_EINVAL, MOC_EHIP.
+ */
+typedef struct {
+  float *before_gamma, *before_beta, *after_gamma, *after_beta, *gate;
+} moc_residual_grads;
+
+int64_t moc_residual_backward_work(int64_t rows, int64_t cols, int64_t gates);
+int moc_residual_backward(int64_t rows, int64_t cols, const moc_matrix* dr, const moc_matrix* dn, const moc_matrix* r,
+                          const moc_matrix* block, const moc_matrix* gate, int64_t gates, float scale,
+                          const moc_row_norm* after, const moc_row_norm* before, const moc_matrix* dx,
+                          const moc_matrix* dblock, const moc_residual_grads* grads, void* work, int64_t work_bytes,
+                          void* hip_stream);
+
+/*
  * Log probabilities of rows of logits, z = scale * logits:
  *   lse = log sum over the columns of exp(z),  logp = z[token] - lse,
  *   entropy = lse - sum of p z  with p = exp(z - lse),

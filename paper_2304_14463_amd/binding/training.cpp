@@ -11,6 +11,7 @@
 
 #include <stdint.h>
 #include <algorithm>
+#include <initializer_list>
 #include <string>
 #include <utility>
 #include <vector>
@@ -31,6 +32,9 @@ struct Calls {
   decltype(&moc_linear_backward_input) linear_backward_input;
   decltype(&moc_linear_backward_weight) linear_backward_weight;
   decltype(&moc_linear_work) linear_work;
+  decltype(&moc_residual_forward) residual_forward;
+  decltype(&moc_residual_backward) residual_backward;
+  decltype(&moc_residual_backward_work) residual_backward_work;
   decltype(&moc_logprob_forward_work) logprob_forward_work;
   decltype(&moc_logprob_forward) logprob_forward;
   decltype(&moc_logprob_backward) logprob_backward;
@@ -476,8 +480,6 @@ PyObject* linear_backward_weight(PyObject*, PyObject* const* a, Py_ssize_t count
   END_HANDLE_TH_ERRORS
 }
 
-// ---- log probabilities --------------------------------------------------------------------------
-
 double number(PyObject* x) {
   const double v = PyFloat_AsDouble(x);
   if (v == -1.0 && PyErr_Occurred()) throw python_error();
@@ -491,6 +493,195 @@ void apart(const Held& out, const char* name, const Vector& in, const char* what
   if (!out.there || !in.data || in.x.numel() == 0) return;
   if (shared(out.span(), Span{reinterpret_cast<uintptr_t>(in.data), 1, (int64_t)in.x.nbytes(), 1})) bad(name, std::string("shares memory with ") + what);
 }
+
+PyObject* none() {
+  Py_INCREF(Py_None);
+  return Py_None;
+}
+
+// ---- the residual connection --------------------------------------------------------------------
+
+// A norm as Python has it: None, or (kind, gamma, beta, eps).
+struct RowNorm {
+  moc_row_norm n = {};
+  Vector gamma, beta, mean, rstd;
+  THPObjectPtr stats;   // (mean or None, rstd)
+  bool on() const { return n.kind != MOC_NORM_NONE; }
+  const moc_row_norm* get() const { return on() ? &n : nullptr; }
+};
+RowNorm row_norm_of(PyObject* x, int64_t cols, const char* what, const at::Tensor& beside) {
+  RowNorm r;
+  if (x == Py_None) return r;
+  if (!PyTuple_Check(x) || PyTuple_GET_SIZE(x) != 4) refuse(PyExc_TypeError, std::string(what) + ": a Norm or None expected");
+  PyObject* const kind = PyTuple_GET_ITEM(x, 0);
+  const bool text = PyUnicode_Check(kind);
+  r.n.kind = text && PyUnicode_CompareWithASCIIString(kind, "layer") == 0 ? MOC_NORM_LAYER : text && PyUnicode_CompareWithASCIIString(kind, "rms") == 0 ? MOC_NORM_RMS : -1;
+  if (r.n.kind < 0) bad(what, "a norm's kind is \"layer\" or \"rms\"");
+  r.gamma = vector(PyTuple_GET_ITEM(x, 1), cols, what, beside);
+  r.beta = vector(PyTuple_GET_ITEM(x, 2), cols, what, beside);
+  if (r.beta.data && r.n.kind == MOC_NORM_RMS) bad(what, "a norm of kind \"rms\" has no beta");
+  if (r.gamma.data && r.beta.data && r.gamma.type != r.beta.type) bad(what, "gamma and beta must have one type");
+  const double eps = number(PyTuple_GET_ITEM(x, 3));
+  if (!(eps >= 0.0)) bad(what, "eps is a number of 0 or more");
+  r.n.gamma = r.gamma.data;
+  r.n.beta = r.beta.data;
+  r.n.param_type = r.gamma.data ? r.gamma.type : r.beta.type;
+  r.n.eps = (float)eps;
+  return r;
+}
+// Room for a norm's statistics.
+void room_for_statistics(RowNorm& r, int64_t rows, const at::Tensor& like) {
+  if (!r.on()) {
+    r.stats = THPObjectPtr(none());
+    return;
+  }
+  const bool layer = r.n.kind == MOC_NORM_LAYER;
+  at::Tensor room = room_for(like, at::kFloat, {layer ? 2 : 1, rows});
+  r.n.rstd = static_cast<float*>(room.data_ptr()) + (layer ? rows : 0);
+  r.n.mean = layer ? static_cast<float*>(room.data_ptr()) : nullptr;
+  THPObjectPtr mean = layer ? wrapped(room.select(0, 0)) : THPObjectPtr(none()), rstd = wrapped(room.select(0, layer ? 1 : 0));
+  r.stats = THPObjectPtr(PyTuple_Pack(2, mean.get(), rstd.get()));
+  if (!r.stats) throw python_error();
+}
+// A norm's statistics as the forward pass has returned them.
+void take_statistics(RowNorm& r, PyObject* x, int64_t rows, const char* what, const at::Tensor& beside) {
+  if (!r.on()) return;
+  if (!PyTuple_Check(x) || PyTuple_GET_SIZE(x) != 2) bad(what, "the statistics (mean, rstd) of the forward pass expected");
+  if (r.n.kind == MOC_NORM_LAYER) {
+    r.mean = vector(PyTuple_GET_ITEM(x, 0), rows, what, beside, true);
+    r.n.mean = static_cast<float*>(r.mean.data);
+  }
+  r.rstd = vector(PyTuple_GET_ITEM(x, 1), rows, what, beside, true);
+  r.n.rstd = static_cast<float*>(r.rstd.data);
+}
+
+// A gate for every rows / gates rows: [gates][cols], or [cols] for all of them.
+Held gate_of(PyObject* x, int64_t rows, int64_t cols, const at::Tensor& beside) {
+  Held h;
+  if (x == Py_None) return h;
+  if (THPVariable_Check(x) && THPVariable_Unpack(x).dim() == 1) {
+    THPObjectPtr row = wrapped(THPVariable_Unpack(x).unsqueeze(0));
+    h = held(row, "gate", 1, cols);
+  } else {
+    h = held(x, "gate", -1, cols);
+  }
+  if (h.kept) bad("gate", "a tensor expected");
+  if (h.rows < 1 || h.rows > std::max<int64_t>(rows, 1) || rows % h.rows != 0) bad("gate", "a number of rows that divides " + std::to_string(rows) + " expected");
+  same_device(beside, h.values);
+  return h;
+}
+
+void apart_from_norm(const Held& out, const char* name, const RowNorm& r) {
+  for (const Vector* v : {&r.gamma, &r.beta, &r.mean, &r.rstd}) apart(out, name, *v, "a norm's vector");
+}
+
+at::ScalarType first_type(std::initializer_list<const Held*> of, at::ScalarType otherwise) {
+  for (const Held* h : of)
+    if (h->there && !h->kept) return h->values.scalar_type();
+  return otherwise;
+}
+
+// residual_forward(x, block, gate, scale, after, before, keep, dtype, want_stream, out, out_norm) -> (code, r, n, after's statistics, before's, kept)
+PyObject* residual_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  arguments(count, 11, "residual_forward");
+  const Held b = held(a[1], "block"), x = held(a[0], "x", b.rows, b.cols, true);
+  if (x.kept) bad("x", "a tensor expected");
+  same_device(b.values, x.values);
+  const Held gate = gate_of(a[2], b.rows, b.cols, b.values);
+  const double scale = number(a[3]);
+  RowNorm after = row_norm_of(a[4], b.cols, "after", b.values), before = row_norm_of(a[5], b.cols, "before", b.values);
+  if (!before.on() && a[6] != Py_None) bad("keep", "there is no norm to keep");
+  if (!before.on() && a[10] != Py_None) bad("out_norm", "there is no norm before the next block");
+  const bool stream_too = truth(a[8]);
+  if (!stream_too && !before.on()) bad("want_stream", "neither the stream nor a norm of it is wanted");
+  THPObjectPtr r, n, kept;
+  r = stream_too ? result(a[9], b.values, first_type({&x, &b}, dtype_of(a[7], at::kFloat)), b.rows, b.cols) : THPObjectPtr(none());
+  n = before.on() ? result(a[10], b.values, dtype_of(a[7], first_type({&b, &x}, at::kFloat)), b.rows, b.cols) : THPObjectPtr(none());
+  kept = room_kept(a[6], b.values, b.rows, b.cols);
+  const Held hr = held(r, "out", b.rows, b.cols, true), hn = held(n, "out_norm", b.rows, b.cols, true), hk = held(kept, "keep", b.rows, b.cols, true);
+  for (const Held* h : {&hr, &hn, &hk}) same_device(b.values, h->values);
+  for (const Held* h : {&hr, &hn}) {
+    const char* const name = h == &hr ? "out" : "out_norm";
+    apart(*h, name, x, "x", true);
+    apart(*h, name, b, "block", true);
+    apart(*h, name, gate, "gate");
+    apart_from_norm(*h, name, after);
+    apart_from_norm(*h, name, before);
+  }
+  apart(hn, "out_norm", hr, "out");
+  for (const Held* h : {&x, &b, &gate, &hr, &hn}) apart(hk, "keep", *h, "another argument");
+  room_for_statistics(after, b.rows, b.values);
+  room_for_statistics(before, b.rows, b.values);
+  void* const stream = stream_for(b.values);
+  const int code = released([&] {
+    return calls.residual_forward(b.rows, b.cols, x.get(), b.get(), gate.get(), gate.there ? gate.rows : 0, (float)scale, after.get(), before.get(), hr.get(), hn.get(), hk.get(), stream);
+  });
+  return Py_BuildValue("iNNNNN", code, r.release(), n.release(), after.stats.release(), before.stats.release(), kept.release());
+  END_HANDLE_TH_ERRORS
+}
+
+// residual_backward(dr, dn, r, block, gate, scale, after, after_stats, before, before_stats, want_x, want_params, dtype, out_x, out_block, work)
+//   -> (code, dx, dblock, gate, after_gamma, after_beta, before_gamma, before_beta)
+PyObject* residual_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
+  HANDLE_TH_ERRORS
+  arguments(count, 16, "residual_backward");
+  const bool by_dr = a[0] != Py_None;
+  const Held lead = held(by_dr ? a[0] : a[1], by_dr ? "dr" : "dn");
+  const int64_t rows = lead.rows, cols = lead.cols;
+  const Held dr = held(a[0], "dr", rows, cols, true), dn = held(a[1], "dn", rows, cols, true), r = held(a[2], "r", rows, cols, true), b = held(a[3], "block", rows, cols, true);
+  if (dr.kept || dn.kept) bad(dr.kept ? "dr" : "dn", "a tensor expected");
+  for (const Held* h : {&dr, &dn, &r, &b}) same_device(lead.values, h->values);
+  const Held gate = gate_of(a[4], rows, cols, lead.values);
+  const double scale = number(a[5]);
+  RowNorm after = row_norm_of(a[6], cols, "after", lead.values), before = row_norm_of(a[8], cols, "before", lead.values);
+  take_statistics(after, a[7], rows, "after_stats", lead.values);
+  take_statistics(before, a[9], rows, "before_stats", lead.values);
+  if (before.on() != dn.there) bad("dn", before.on() ? "the gradient of the norm is missing" : "there is no norm before the next block");
+  if (before.on() && !r.there) bad("r", "the stream is missing");
+  const bool params = truth(a[11]);
+  if (!b.there && (after.on() || (gate.there && params))) bad("block", "the block's output is missing");
+  THPObjectPtr x_out, b_out;
+  x_out = a[13] != Py_None || truth(a[10]) ? result(a[13], lead.values, first_type({&dr, &r, &dn}, at::kFloat), rows, cols) : THPObjectPtr(none());
+  b_out = result(a[14], lead.values, dtype_of(a[12], first_type({&b, &dn, &dr}, at::kFloat)), rows, cols);
+  const Held dx = held(x_out, "out_x", rows, cols, true), db = held(b_out, "out_block", rows, cols);
+  for (const Held* h : {&dx, &db}) {
+    const char* const name = h == &dx ? "out_x" : "out_block";
+    same_device(lead.values, h->values);
+    apart(*h, name, dr, "dr", h == &dx);
+    apart(*h, name, r, "r", h == &dx);
+    apart(*h, name, dn, "dn", h == &db);
+    apart(*h, name, b, "block", h == &db);
+    apart(*h, name, gate, "gate");
+    apart_from_norm(*h, name, after);
+    apart_from_norm(*h, name, before);
+  }
+  apart(dx, "out_x", db, "out_block");
+  moc_residual_grads grads = {};
+  THPObjectPtr got[5];   // gate, after's gamma and beta, before's
+  float** const at[5] = {&grads.gate, &grads.after_gamma, &grads.after_beta, &grads.before_gamma, &grads.before_beta};
+  const bool wanted[5] = {gate.there, after.gamma.data != nullptr, after.beta.data != nullptr, before.gamma.data != nullptr, before.beta.data != nullptr};
+  for (int i = 0; i < 5; ++i) {
+    if (!params || !wanted[i]) {
+      got[i] = THPObjectPtr(none());
+      continue;
+    }
+    at::Tensor t = i == 0 ? room_for(lead.values, at::kFloat, {gate.rows, cols}) : room_for(lead.values, at::kFloat, {cols});
+    *at[i] = static_cast<float*>(t.data_ptr());
+    got[i] = wrapped(std::move(t));
+  }
+  const int64_t gates = gate.there ? gate.rows : 0;
+  const Work work = workspace(a[15], a[15] == Py_None && params ? calls.residual_backward_work(rows, cols, gates) : 0, lead.values);
+  void* const stream = stream_for(lead.values);
+  const int code = released([&] {
+    return calls.residual_backward(rows, cols, dr.get(), dn.get(), r.get(), b.get(), gate.get(), gates, (float)scale, after.get(), before.get(), dx.get(), db.get(), &grads, work.data,
+                                   work.bytes, stream);
+  });
+  return Py_BuildValue("iNNNNNNN", code, x_out.release(), b_out.release(), got[0].release(), got[1].release(), got[2].release(), got[3].release(), got[4].release());
+  END_HANDLE_TH_ERRORS
+}
+
+// ---- log probabilities --------------------------------------------------------------------------
 
 // n signed numbers of 4 or 8 bytes, or none.
 struct Tokens {
@@ -508,11 +699,6 @@ Tokens tokens_of(PyObject* p, int64_t n, const at::Tensor& beside) {
   t.v.data = x.data_ptr();
   t.bytes = (int32_t)x.element_size();
   return t;
-}
-
-PyObject* none() {
-  Py_INCREF(Py_None);
-  return Py_None;
 }
 
 // logprob_forward(logits, tokens, scale, top, work) -> (code, logp, lse, entropy, top_logp, top_tokens)
@@ -795,6 +981,9 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
   take(c.linear_backward_input, "moc_linear_backward_input");
   take(c.linear_backward_weight, "moc_linear_backward_weight");
   take(c.linear_work, "moc_linear_work");
+  take(c.residual_forward, "moc_residual_forward");
+  take(c.residual_backward, "moc_residual_backward");
+  take(c.residual_backward_work, "moc_residual_backward_work");
   take(c.logprob_forward_work, "moc_logprob_forward_work");
   take(c.logprob_forward, "moc_logprob_forward");
   take(c.logprob_backward, "moc_logprob_backward");
@@ -813,7 +1002,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t count) {
 
 #define MOC_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {MOC_METHOD(bind), MOC_METHOD(checkpoint_write), MOC_METHOD(checkpoint_read), MOC_METHOD(norm_forward), MOC_METHOD(norm_backward), MOC_METHOD(linear_forward),
-                         MOC_METHOD(linear_backward_input), MOC_METHOD(linear_backward_weight), MOC_METHOD(logprob_forward), MOC_METHOD(logprob_backward), MOC_METHOD(adamw_step), MOC_METHOD(moments_read), MOC_METHOD(shares), {nullptr, nullptr, 0, nullptr}};
+                         MOC_METHOD(linear_backward_input), MOC_METHOD(linear_backward_weight), MOC_METHOD(residual_forward), MOC_METHOD(residual_backward), MOC_METHOD(logprob_forward), MOC_METHOD(logprob_backward), MOC_METHOD(adamw_step), MOC_METHOD(moments_read), MOC_METHOD(shares), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_training", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

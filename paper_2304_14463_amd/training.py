@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import collections
 import ctypes
+import typing
 
 from . import moccasin as moc
 
@@ -29,7 +30,7 @@ BLOCK = 32
 
 EXPORTS = ("moc_checkpoint_write", "moc_checkpoint_read", "moc_norm_forward", "moc_norm_backward", "moc_norm_backward_work", "moc_linear_forward",
            "moc_linear_backward_input", "moc_linear_backward_weight", "moc_linear_work", "moc_linear_parts",
-           "moc_logprob_forward_work", "moc_logprob_forward", "moc_logprob_backward", "moc_adamw_step", "moc_moments_read", "moc_training_version")
+           "moc_residual_forward", "moc_residual_backward", "moc_residual_backward_work", "moc_logprob_forward_work", "moc_logprob_forward", "moc_logprob_backward", "moc_adamw_step", "moc_moments_read", "moc_training_version")
 
 
 class Matrix(ctypes.Structure):
@@ -94,9 +95,11 @@ def lib():
                            ("moc_linear_backward_input", [I64, I64, I64, M, M, I32, M, M, VP, I64, VP]),
                            ("moc_linear_backward_weight", [I64, I64, I64, M, M, M, VP, VP, I64, VP])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
-        for name, args in (("moc_norm_backward_work", [I64, I64]), ("moc_linear_work", [I64, I64, I64]), ("moc_logprob_forward_work", [I64, I64, I32])):
+        for name, args in (("moc_norm_backward_work", [I64, I64]), ("moc_linear_work", [I64, I64, I64]), ("moc_residual_backward_work", [I64, I64, I64]),
+                           ("moc_logprob_forward_work", [I64, I64, I32])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, I64
-        for name, args in (("moc_logprob_forward", [I64, I64, M, VP, I32, F32, I32, VP, VP, VP, VP, VP, VP, I64, VP]),
+        for name, args in (("moc_residual_forward", [I64, I64, M, M, M, I64, F32, VP, VP, M, M, M, VP]),
+                           ("moc_residual_backward", [I64, I64, M, M, M, M, M, I64, F32, VP, VP, M, M, VP, VP, I64, VP]), ("moc_logprob_forward", [I64, I64, M, VP, I32, F32, I32, VP, VP, VP, VP, VP, VP, I64, VP]),
                            ("moc_logprob_backward", [I64, I64, M, VP, VP, VP, I32, VP, VP, F32, M, VP]), ("moc_adamw_step", [I64, VP, VP, VP]), ("moc_moments_read", [I64, VP, VP])):
             getattr(L, name).argtypes, getattr(L, name).restype = args, ctypes.c_int
         L.moc_linear_parts.argtypes, L.moc_linear_parts.restype = [I32, I64, I64, I64, I32, I32, ctypes.POINTER(I64)], ctypes.c_int
@@ -220,6 +223,40 @@ def moc_linear_parts(product, rows, cin, cout, aligned=True, units=0):
     out = (ctypes.c_int64 * 5)()
     moc._check(lib().moc_linear_parts(PRODUCTS[product], rows, cin, cout, int(aligned), units, out), "moc_linear_parts")
     return Parts(out[0], bool(out[1]), *out[2:])
+
+
+class Norm(typing.NamedTuple):
+    """A norm of rows: `kind` "layer" (mean and deviation, gamma and beta) or "rms" (the root of the mean square, gamma);
+    None for gamma and beta stands for 1 and 0."""
+    kind: str
+    gamma: object = None
+    beta: object = None
+    eps: float = 1e-5
+
+
+Residual = collections.namedtuple("Residual", "r n after before kept")
+ResidualGrads = collections.namedtuple("ResidualGrads", "dx dblock gate after_gamma after_beta before_gamma before_beta")
+
+
+def moc_residual_forward(x, block, gate=None, scale=1.0, after=None, before=None, keep=None, dtype=None, want_stream=True, out=None, out_norm=None, stream=None):
+    """The stream between two blocks, r = scale * x + gate * after(block), and the norm before the next one, n = before(r): `after` and
+    `before` are Norms or None, `gate` [cols] or [gates, cols] for rows / gates rows each, `block` a tensor or a Checkpoint, `x` may be
+    None.  Returns (r, n, (mean, rstd) of each norm, n in 8 bits if `keep` names a format or is a Checkpoint to write to); None for
+    what is not there.  `dtype`: n's, default the block's.  `out` may be x or block, and so may `out_norm`."""
+    code, *got = _call("residual_forward", stream, x, block, gate, scale, after, before, keep, dtype, want_stream, out, out_norm)
+    moc._check(code, "moc_residual_forward")
+    return Residual(*got)
+
+
+def moc_residual_backward(dr, dn, r=None, block=None, gate=None, scale=1.0, after=None, after_stats=None, before=None, before_stats=None, want_x=True, want_params=True, dtype=None,
+                          out_x=None, out_block=None, work=None, stream=None):
+    """The gradients of moc_residual_forward from those of the stream (or None) and of the norm (None without `before`), what the
+    forward pass was given and what it has left; `r` and `block` are tensors or Checkpoints.  Returns (dx, dblock of `dtype`, default the
+    block's, and float32 gradients of the gate, [gates, cols], and of the norms' parameters); None for what is not there.
+    `out_x` may be dr or r, `out_block` dn or block."""
+    code, *got = _call("residual_backward", stream, dr, dn, r, block, gate, scale, after, after_stats, before, before_stats, want_x, want_params, dtype, out_x, out_block, work)
+    moc._check(code, "moc_residual_backward")
+    return ResidualGrads(*got)
 
 
 LogProbs = collections.namedtuple("LogProbs", "logp lse entropy top_logp top_tokens")

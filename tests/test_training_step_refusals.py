@@ -65,12 +65,65 @@ def test_moments_read(lib):
     assert call(count=0, m=None) == 0 and call(tensors=0) == 0
 
 
-def test_logprob(lib):
+class RowNorm(ctypes.Structure):
+    """moc_row_norm"""
+    _fields_ = [("kind", I32), ("param_type", I32), ("gamma", P), ("beta", P), ("mean", P), ("rstd", P), ("eps", F), ("reserved", I32)]
+
+
+class Grads(ctypes.Structure):
+    """moc_residual_grads"""
+    _fields_ = [("before_gamma", P), ("before_beta", P), ("after_gamma", P), ("after_beta", P), ("gate", P)]
+
+
+def mat(type_=BF16, cols=64, stride=None, data=A, reserved=0, scales=A):
     from paper_2304_14463_amd.training import Matrix
+    return Matrix(data, scales if type_ in (E4M3, I8) else None, cols if stride is None else stride, 2, type_, reserved)
 
-    def mat(type_=BF16, cols=64, stride=None, data=A, reserved=0):
-        return Matrix(data, A if type_ >= E4M3 else None, cols if stride is None else stride, 2, type_, reserved)
 
+def row_norm(kind=1, **changed):
+    n = RowNorm(kind, F32, A, A if kind == 1 else None, A, A, 1e-5, 0)
+    for k, v in changed.items():
+        setattr(n, k, v)
+    return ctypes.byref(n)
+
+
+BAD_NORMS = [dict(kind=3), dict(kind=-1), dict(param_type=E4M3), dict(param_type=-1), dict(gamma=A + 2), dict(beta=A + 1), dict(kind=2, beta=A), dict(mean=None), dict(rstd=None), dict(mean=A + 2), dict(rstd=A + 1),
+             dict(eps=-1.0), dict(eps=float("nan")), dict(reserved=1)]
+BAD_MATRICES = [mat(7), mat(-1), mat(stride=63), mat(data=None), mat(data=A + 1), mat(F32, data=A + 2), mat(stride=1 << 23), mat(reserved=1)]
+
+
+def test_residual(lib):
+    def forward(rows=8, cols=64, x=mat(), block=mat(), gate=mat(), gates=2, scale=1.0, after=row_norm(), before=row_norm(2), r=mat(), n=mat(), kept=None):
+        return lib.moc_residual_forward(rows, cols, x, block, gate, gates, scale, after, before, r, n, kept, None)
+
+    def backward(rows=8, cols=64, dr=mat(), dn=mat(), r=mat(), block=mat(), gate=mat(), gates=2, scale=1.0, after=row_norm(), before=row_norm(), dx=mat(), dblock=mat(),
+                 grads=Grads(A, A, A, A, A), work=A, work_bytes=0):
+        return lib.moc_residual_backward(rows, cols, dr, dn, r, block, gate, gates, scale, after, before, dx, dblock, None if grads is None else ctypes.byref(grads), work, work_bytes, None)
+
+    sizes = [dict(rows=-1), dict(rows=1 << 31), dict(cols=0), dict(cols=16385), dict(gates=-1), dict(gates=3), dict(gates=16), dict(gates=0), dict(gate=None)]
+    for bad in sizes + [dict(scale=float("nan")), dict(scale=float("inf"))] + [dict(after=row_norm(**k)) for k in BAD_NORMS] + [dict(before=row_norm(**k)) for k in BAD_NORMS] + [dict(gate=mat(E4M3))]:
+        assert forward(**bad) == -1 and backward(**bad) == -1, bad
+    for k in ("x", "block", "gate", "r", "n"):
+        for m in BAD_MATRICES:
+            assert forward(**{k: m}) == -1, k
+    for k in ("dr", "dn", "r", "block", "gate", "dx", "dblock"):
+        for m in BAD_MATRICES:
+            assert backward(**{k: m}) == -1, k
+    for bad in (dict(block=None), dict(x=mat(I8)), dict(r=mat(E4M3)), dict(n=mat(E4M3)), dict(n=None), dict(before=None), dict(before=row_norm(0)), dict(r=None, n=None, before=None), dict(kept=mat()),
+                dict(kept=mat(I8, data=None)), dict(kept=mat(I8, scales=None)), dict(kept=mat(I8), n=None, before=None)):
+        assert forward(**bad) == -1, bad
+    for bad in (dict(dn=None), dict(before=None), dict(dr=None, dn=None, before=None), dict(r=None), dict(block=None), dict(dr=mat(E4M3)), dict(dn=mat(I8)), dict(dx=mat(E4M3)), dict(dblock=mat(I8)),
+                dict(grads=Grads(A + 2)), dict(grads=Grads(None, A + 1)), dict(grads=Grads(None, None, A + 2)), dict(grads=Grads(None, None, None, None, A + 2)), dict(before=row_norm(2)), dict(after=row_norm(2)),
+                dict(after=None), dict(gate=None, gates=0), dict(block=None, after=None, grads=Grads(None, None, None, None, A))):
+        assert backward(**bad) == -1, bad
+    none = mat(data=None)
+    assert forward(rows=0, x=none, block=none, r=none, n=none, gates=1) == 0
+    assert backward(rows=0, dr=none, dn=none, r=none, block=none, dx=none, dblock=none, gates=1, grads=None) == 0
+    for bad in ((-1, 64, 0), (8, 0, 0), (8, 64, 3), (8, 16385, 0), (8, 64, -1)):
+        assert lib.moc_residual_backward_work(*bad) == -1
+
+
+def test_logprob(lib):
     def forward(rows=4, vocab=64, logits=mat(), tokens=A, bytes_=8, scale=1.0, top=5, logp=A, lse=A, entropy=A, top_logp=A, top_tokens=A):
         return lib.moc_logprob_forward(rows, vocab, logits, tokens, bytes_, scale, top, logp, lse, entropy, top_logp, top_tokens, None, 0, None)
 
@@ -106,11 +159,11 @@ def test_what_is_on_no_gpu(lib):
         tr.zero_moments(x, 16)
     assert tr.zero_moments(x).nbytes == 132 and tr.zero_moments(x, 32).nbytes == 512
     m = torch.zeros(4, 64)
-    for call in (lambda: tr.moc_logprob_forward(m), lambda: tr.moc_logprob_backward(m, x[:4])):
+    for call in (lambda: tr.moc_residual_forward(m, m.clone()), lambda: tr.moc_residual_backward(m, None), lambda: tr.moc_logprob_forward(m), lambda: tr.moc_logprob_backward(m, x[:4])):
         with pytest.raises(ValueError):
             call()
     for bad in (None, 3, [1.0], "x"):
-        for call in (lambda: tr.moc_logprob_forward(bad), lambda: tr.moc_logprob_backward(bad, bad)):
+        for call in (lambda: tr.moc_residual_forward(None, bad), lambda: tr.moc_residual_backward(bad, bad), lambda: tr.moc_logprob_forward(bad), lambda: tr.moc_logprob_backward(bad, bad)):
             with pytest.raises(TypeError):
                 call()
     for bad in (None, 3, [3], [x, "y"]):
