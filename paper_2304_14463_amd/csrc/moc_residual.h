@@ -104,15 +104,6 @@ __device__ __forceinline__ void rounded(const float (&v)[kRun], float (&w)[kRun]
   }
 }
 
-template <int K>
-__device__ __forceinline__ void store_run_of(const Mat& m, uint32_t row, int col, int n, const float (&of)[kRun]) {
-  if (n <= 0) return;
-  float v[kRun];
-  rounded(of, v);
-  if constexpr (K >= 0) store_run<K>(row_at(m, row), col, n, v);
-  else store_any(m.type, row_at(m, row), col, n, v);
-}
-
 // The same in kernels made for a type, of rows of eight columns at least: always from within the row, without a branch, so that
 // the waits for it are for nothing else.  Lanes beyond the row have its last eight values.
 template <int K>
@@ -178,6 +169,18 @@ __device__ __forceinline__ void put(const Mat& m, uint32_t row, uint32_t col, ui
     __builtin_memcpy(at, t, sizeof t);
   } else {
     put_part(at, t, cols - col);
+  }
+}
+
+template <int K>
+__device__ __forceinline__ void store_run_of(const Mat& m, uint32_t row, int col, int n, const float (&of)[kRun]) {
+  if (n <= 0) return;
+  if constexpr (K >= 0) {
+    put<K>(m, row, (uint32_t)col, (uint32_t)(col + n), of);
+  } else {
+    float v[kRun];
+    rounded(of, v);
+    store_any(m.type, row_at(m, row), col, n, v);
   }
 }
 

@@ -212,11 +212,6 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
   const float layer2 = g.before.layer ? 1.0f : 0.0f, layer1 = g.after.layer ? 1.0f : 0.0f;
   Runs<CH> gamma1, beta1, gate, gamma2;
   Runs<CH> sg1, sb1, sgate, sg2, sb2;
-  if constexpr (MODE == kNormed) {
-    hold_param<T, CH>(g.after.gamma, g.after.param_type, lane, cols, 1.0f, gamma1);
-    hold_param<T, CH>(g.after.beta, g.after.param_type, lane, cols, 0.0f, beta1);
-  }
-  hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, cols, 1.0f, gamma2);
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -243,9 +238,16 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
   };
   for (uint32_t which = from; which < last; ++which) {
     const uint32_t first = which * g.rows_per_gate + chunk * g.chunk_rows, end = min(first + g.chunk_rows, (which + 1) * g.rows_per_gate);
-    if constexpr (MODE != kPlain) hold_gate<T, CH>(g, which, lane, gate);
     uint32_t row = first + mine;
     if (kAhead && row < end) load(row);
+    if (which == from) {   // with the first row on its way
+      if constexpr (MODE == kNormed) {
+        hold_param<T, CH>(g.after.gamma, g.after.param_type, lane, cols, 1.0f, gamma1);
+        hold_param<T, CH>(g.after.beta, g.after.param_type, lane, cols, 0.0f, beta1);
+      }
+      hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, cols, 1.0f, gamma2);
+    }
+    if constexpr (MODE != kPlain) hold_gate<T, CH>(g, which, lane, gate);
     for (; row < end; row += kRows) {   // groups of lanes that end earlier share no barrier
       if (!kAhead) load(row);
       Runs<CH> h, d;

@@ -39,14 +39,6 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_forward_kernel(Res
   Sums sums{room};
   const int lane = threadIdx.x % T, mine = kRows > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / T) : 0;
   const bool whole = S != kAny || (g.cols >= kRun && !g.parts);   // which S says: see forward_shape
-  Runs<CH> gamma1, beta1, gate, gamma2, beta2;
-  if constexpr (AFTER) {
-    hold_param<T, CH>(g.after.gamma, g.after.param_type, lane, g.cols, 1.0f, gamma1);
-    hold_param<T, CH>(g.after.beta, g.after.param_type, lane, g.cols, 0.0f, beta1);
-  }
-  if (g.gates <= 1) hold_gate<T, CH>(g, 0, lane, gate);
-  hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, g.cols, 1.0f, gamma2);
-  hold_param<T, CH>(g.before.beta, g.before.param_type, lane, g.cols, 0.0f, beta2);
   const uint32_t step = gridDim.x * kRows;
   uint32_t row = blockIdx.x * kRows + mine;
   Raw wb[CH], wx[CH], wg[CH];
@@ -60,6 +52,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_forward_kernel(Res
     }
   };
   if (row < g.rows) load(row);
+  Runs<CH> gamma1, beta1, gate, gamma2, beta2;
+  if constexpr (AFTER) {
+    hold_param<T, CH>(g.after.gamma, g.after.param_type, lane, g.cols, 1.0f, gamma1);
+    hold_param<T, CH>(g.after.beta, g.after.param_type, lane, g.cols, 0.0f, beta1);
+  }
+  if (g.gates <= 1) hold_gate<T, CH>(g, 0, lane, gate);
+  hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, g.cols, 1.0f, gamma2);
+  hold_param<T, CH>(g.before.beta, g.before.param_type, lane, g.cols, 0.0f, beta2);
   for (; row < g.rows; row += step) {
     Runs<CH> v;
     Raw x[CH];
