@@ -535,11 +535,15 @@ void room_for_statistics(RowNorm& r, int64_t rows, const at::Tensor& like) {
     r.stats = THPObjectPtr(none());
     return;
   }
-  const bool layer = r.n.kind == MOC_NORM_LAYER;
-  at::Tensor room = room_for(like, at::kFloat, {layer ? 2 : 1, rows});
-  r.n.rstd = static_cast<float*>(room.data_ptr()) + (layer ? rows : 0);
-  r.n.mean = layer ? static_cast<float*>(room.data_ptr()) : nullptr;
-  THPObjectPtr mean = layer ? wrapped(room.select(0, 0)) : THPObjectPtr(none()), rstd = wrapped(room.select(0, layer ? 1 : 0));
+  THPObjectPtr mean(none()), rstd;
+  if (r.n.kind == MOC_NORM_LAYER) {
+    at::Tensor x = room_for(like, at::kFloat, {rows});
+    r.n.mean = static_cast<float*>(x.data_ptr());
+    mean = wrapped(std::move(x));
+  }
+  at::Tensor x = room_for(like, at::kFloat, {rows});
+  r.n.rstd = static_cast<float*>(x.data_ptr());
+  rstd = wrapped(std::move(x));
   r.stats = THPObjectPtr(PyTuple_Pack(2, mean.get(), rstd.get()));
   if (!r.stats) throw python_error();
 }

@@ -243,9 +243,9 @@ def moc_residual_forward(x, block, gate=None, scale=1.0, after=None, before=None
     `before` are Norms or None, `gate` [cols] or [gates, cols] for rows / gates rows each, `block` a tensor or a Checkpoint, `x` may be
     None.  Returns (r, n, (mean, rstd) of each norm, n in 8 bits if `keep` names a format or is a Checkpoint to write to); None for
     what is not there.  `dtype`: n's, default the block's.  `out` may be x or block, and so may `out_norm`."""
-    code, *got = _call("residual_forward", stream, x, block, gate, scale, after, before, keep, dtype, want_stream, out, out_norm)
+    code, r, n, after, before, kept = _call("residual_forward", stream, x, block, gate, scale, after, before, keep, dtype, want_stream, out, out_norm)
     moc._check(code, "moc_residual_forward")
-    return Residual(*got)
+    return Residual(r, n, after, before, kept)
 
 
 def moc_residual_backward(dr, dn, r=None, block=None, gate=None, scale=1.0, after=None, after_stats=None, before=None, before_stats=None, want_x=True, want_params=True, dtype=None,
