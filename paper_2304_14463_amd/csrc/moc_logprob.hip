@@ -3,18 +3,23 @@
 // Forward: one pass over a row.  A lane holds the largest logit m it has met, s = sum of e and w = sum of e t with
 // t = scale (x - m) / ln 2 and e = 2^t; a larger one scales both, s' = f s and w' = f (w + d s) with d = scale (m - m') / ln 2 and
 // f = 2^d, and so do lanes that are joined.  Then log sum exp = scale m + ln s and the entropy ln s - ln 2 w / s.
-// The alternatives: a wave keeps its 64 best, one a lane in falling order, as whole numbers that order by value and
-// then by place; a value above the last one wanted moves those below it one lane on.
+// The alternatives: the wanted number of lanes have a largest logit that is not below some value, so nothing below it is among
+// them; the few lanes whose largest is not below it have their columns read again, what is not below it goes to LDS, and its
+// places in the order are counted.  Few rows are cut into parts, whose sums and alternatives a second kernel joins.
 // Backward: a pass over the logits and their gradient.
-#include "moc_training.h"
+#include <algorithm>
+
+#include "moc_rows.h"
+#include "moc_wave.h"
 
 namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kMostTop = kWave;
+constexpr int kMostTop = kWave, kMostParts = kWave;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kFar = -200.0f;   // 2^kFar is 0: a value further below the largest adds nothing, an infinite one neither
 
+struct Sums;
 struct LogprobArgs {
   const void* logits;
   int64_t stride;
@@ -24,6 +29,9 @@ struct LogprobArgs {
   const void* tokens;
   float *logp, *lse, *entropy, *top_logp;
   int64_t* top_tokens;
+  int parts, part_cols;
+  Sums* part_sums;   // [rows][parts]
+  uint64_t* part_keys;      // [rows][parts][top]
   // backward
   const float *lse_of, *entropy_of, *dlogp, *dentropy;
   void* out;
@@ -93,8 +101,23 @@ __device__ __forceinline__ void join(Sums& a, Sums b) {
   a.w += b.w;
 }
 
-__device__ __forceinline__ Sums from_lane(const Sums& x, int offset) {
-  return Sums{__shfl_xor(x.m, offset), __shfl_xor(x.at, offset), __shfl_xor(x.s, offset), __shfl_xor(x.w, offset)};
+// Over the wave, in lane 63: shifts of the vector ALU inside rows of 16 lanes, then across them.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float shifted(float a, float otherwise) {
+  return bits_float((uint32_t)__builtin_amdgcn_update_dpp((int)float_bits(otherwise), (int)float_bits(a), CTRL, ROWS, 0xF, false));
+}
+__device__ __forceinline__ float wave_largest(float a) {
+  a = fmaxf(a, shifted<0x111, 0xF>(a, -kInf));
+  a = fmaxf(a, shifted<0x112, 0xF>(a, -kInf));
+  a = fmaxf(a, shifted<0x114, 0xF>(a, -kInf));
+  a = fmaxf(a, shifted<0x118, 0xF>(a, -kInf));
+  a = fmaxf(a, shifted<0x142, 0xA>(a, -kInf));
+  a = fmaxf(a, shifted<0x143, 0xC>(a, -kInf));
+  return bits_float((uint32_t)__builtin_amdgcn_readlane((int)float_bits(a), kWave - 1));
+}
+__device__ __forceinline__ Sums join_wave(Sums x) {
+  move_to(x, wave_largest(x.s == 0.0f ? -kInf : x.at));   // one that holds nothing has no say; where none holds any, s and w are 0 all the same
+  return Sums{wave_largest(x.m), x.at, wave_sum(x.s), wave_sum(x.w)};
 }
 
 // ---- alternatives -------------------------------------------------------------------------------
@@ -110,70 +133,143 @@ __device__ __forceinline__ float logit_of(Key k) {
 }
 __device__ __forceinline__ uint32_t place_of(Key k) { return ~(uint32_t)k; }
 
-__device__ __forceinline__ Key lane_key(Key k, int lane) {
-  return (Key)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
-}
-// The key of the lane before.
-__device__ __forceinline__ Key key_before(Key k) {
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)k, 0x138, 0xF, 0xF, false), hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(k >> 32), 0x138, 0xF, 0xF, false);
-  return (Key)hi << 32 | lo;
-}
-
-struct Best {
-  Key key = 0;            // of this lane; falling over the wave
-  Key last = 0;           // the last one wanted
-  float above = -kInf;    // its logit
-  bool full = false;      // as many as are wanted are there
-
-  __device__ __forceinline__ void insert(Key c, int lane, int top) {   // c: the same in all lanes
-    const int before = __builtin_popcountll(__builtin_amdgcn_ballot_w64(key > c));
-    const Key moved = key_before(key);
-    key = lane < before ? key : lane == before ? c : moved;
-    last = lane_key(key, top - 1);
-  }
-  // The run of each lane, from column `col` on, `n` of it in the row.  `over` lets values through: above it, or at it too
-  // where `with`.
-  __device__ __forceinline__ void offer(const float (&v)[kRun], int col, int n, float over, bool with, int lane, int top) {
+// A logit that at least `top` of the lanes reach with their largest, in all threads: the largest number of 16 bits that as many
+// of the upper halves of their orders are not below.
+constexpr int kRoom = 1024;
+struct TopRoom {
+  float largest[kThreads];
+  uint16_t lanes[kThreads];
+  uint32_t reach, found;
+  float least;
+  Key keys[kRoom], best[kMostTop];
+};
+__device__ __forceinline__ void find_least(TopRoom& r, int top) {
+  if (threadIdx.x < kWave) {
+    uint32_t half[kWaves], t = 0;
 #pragma unroll
-    for (int i = 0; i < kRun; ++i) {
-      uint64_t some = __builtin_amdgcn_ballot_w64(i < n && (v[i] > over || (with && v[i] == over)));
-      if (some == 0) continue;
-      const Key k = key_of(v[i], (uint32_t)(col + i));
-      while (some != 0) {
-        const int from = __builtin_ctzll(some);
-        some &= some - 1;
-        const Key c = lane_key(k, from);
-        if (c > last) insert(c, lane, top);
-      }
+    for (int i = 0; i < kWaves; ++i) half[i] = (uint32_t)(key_of(r.largest[i * kWave + threadIdx.x], 0) >> 48);
+#pragma unroll
+    for (int bit = 15; bit >= 0; --bit) {
+      const uint32_t next = t | 1u << bit;
+      int count = 0;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(half[i] >= next));
+      if (count >= top) t = next;
+    }
+    const float least = logit_of((Key)t << 48);
+    if (threadIdx.x == 0) r.least = least == least ? least : -kInf;
+  }
+}
+
+// What is above `least`, or not below it (`with`), of the columns of lanes that reach it, to r.keys as far as it goes.
+template <int TYPE>
+__device__ __forceinline__ void gather(const void* row, int from, int to, float least, bool with, TopRoom& r) {
+  const uint32_t lanes = r.reach, total = lanes * (uint32_t)((to - from + kThreads * kRun - 1) / (kThreads * kRun));
+  for (uint32_t i = threadIdx.x; i < total; i += kThreads) {
+    const int col = from + (int)(i / lanes * kThreads + r.lanes[i % lanes]) * kRun, n = to - col;
+    if (n <= 0) continue;
+    float v[kRun];
+    load_run<TYPE>(row, col, n, v);
+#pragma unroll
+    for (int j = 0; j < kRun; ++j) {
+      if (j >= n || !(with ? v[j] >= least : v[j] > least)) continue;
+      const uint32_t at = atomicAdd(&r.found, 1u);
+      if (at < kRoom) r.keys[at] = key_of(v[j], (uint32_t)(col + j));
     }
   }
-  __device__ __forceinline__ void settle() {
-    full = last != 0;
-    above = full ? logit_of(last) : -kInf;
-  }
-};
-
-// The value that `top` lanes reach with their x: one that many values of a first batch are not below.
-__device__ __forceinline__ float reached(float x, int lane, int top) {
-  int before = 0;
-#pragma unroll
-  for (int j = 0; j < kWave; ++j) {
-    const float other = bits_float((uint32_t)__builtin_amdgcn_readlane((int)float_bits(x), j));
-    before += other > x || (other == x && j < lane) ? 1 : 0;
-  }
-  const uint64_t me = __builtin_amdgcn_ballot_w64(before == top - 1);
-  return bits_float((uint32_t)__builtin_amdgcn_readlane((int)float_bits(x), me ? __builtin_ctzll(me) : 0));
 }
 
-// The best 64 of two falling lists, falling.
-__device__ __forceinline__ Key merge(Key a, Key reversed, int lane) {
-  Key k = a > reversed ? a : reversed;
+// More logits than there is room for: those above `least`, and of those that equal it the first ones, as many as are missing.
+// Where even those above it are too many, one after the other by a pass each.  By all threads, as all of these.
+template <int TYPE>
+__device__ __attribute__((noinline)) void gather_again(const void* row, int from, int to, float least, int top, TopRoom* room) {
+  TopRoom& r = *room;
+  if (threadIdx.x == 0) r.found = 0;
+  __syncthreads();
+  gather<TYPE>(row, from, to, least, false, r);
+  __syncthreads();
+  const uint32_t above = r.found;
+  if (above <= kRoom - kMostTop) {
+    if (threadIdx.x < kWave) {
+      uint32_t have = above;
+      for (int at = from; at < to && have < (uint32_t)top; at += kWave * kRun) {
+        const int col = at + (int)threadIdx.x * kRun, n = to - col;
+        float v[kRun];
+        load_run<TYPE>(row, col, n, v);
+        uint32_t equal = 0;
 #pragma unroll
-  for (int d = kWave / 2; d > 0; d /= 2) {
-    const Key other = __shfl_xor((unsigned long long)k, d);
-    k = ((lane & d) == 0) == (k > other) ? k : other;
+        for (int j = 0; j < kRun; ++j) equal |= j < n && v[j] == least ? 1u << j : 0;
+        const int mine = __builtin_popcount(equal), up_to = scan_sum(mine);
+        uint32_t place = have + (uint32_t)(up_to - mine);
+        for (; equal != 0 && place < (uint32_t)top; equal &= equal - 1, ++place) r.keys[place] = key_of(least, (uint32_t)(col + __builtin_ctz(equal)));
+        have += (uint32_t)__builtin_amdgcn_readlane(up_to, kWave - 1);
+      }
+      if (threadIdx.x == 0) r.found = min(max((uint32_t)top, above), have);
+    }
+    __syncthreads();
+    return;
   }
-  return k;
+  Key before = ~(Key)0;
+  int there = 0;
+  for (; there < top; ++there) {
+    Key most = 0;
+    for (int col = from + (int)threadIdx.x * kRun; col < to; col += kThreads * kRun) {
+      const int n = to - col;
+      float v[kRun];
+      load_run<TYPE>(row, col, n, v);
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) {
+        if (j >= n || v[j] != v[j]) continue;
+        const Key k = key_of(v[j], (uint32_t)(col + j));
+        most = k < before && k > most ? k : most;
+      }
+    }
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+      const Key other = __shfl_xor((unsigned long long)most, d);
+      most = other > most ? other : most;
+    }
+    __syncthreads();   // what was read of best below
+    if (threadIdx.x % kWave == 0) r.best[threadIdx.x / kWave] = most;
+    __syncthreads();
+    for (int i = 0; i < kWaves; ++i) most = r.best[i] > most ? r.best[i] : most;
+    if (most == 0) break;
+    before = most;
+    if (threadIdx.x == 0) r.keys[there] = most;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) r.found = (uint32_t)there;
+  __syncthreads();
+}
+
+// The first `top` of n keys in LDS, in falling order, to best; 0 behind the last.  Ends with a barrier.
+__device__ __forceinline__ void order(const Key* keys, uint32_t n, int top, Key* best) {
+  if (threadIdx.x < kMostTop) best[threadIdx.x] = 0;
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+    const Key k = keys[i];
+    int before = 0;
+    for (uint32_t j = 0; j < n; ++j) before += keys[j] > k ? 1 : 0;
+    if (before < top) best[before] = k;
+  }
+  __syncthreads();
+}
+
+// The best of columns from .. to, of which `mine` is the largest of this thread's, to r.best.
+template <int TYPE>
+__device__ __forceinline__ void select_top(const void* row, int from, int to, float mine, int top, TopRoom& r) {
+  r.largest[threadIdx.x] = mine;
+  if (threadIdx.x == 0) r.reach = r.found = 0;
+  __syncthreads();
+  find_least(r, top);
+  __syncthreads();
+  const float least = r.least;
+  if (mine >= least) r.lanes[atomicAdd(&r.reach, 1u)] = (uint16_t)threadIdx.x;
+  __syncthreads();
+  gather<TYPE>(row, from, to, least, true, r);
+  __syncthreads();
+  if (r.found > kRoom) gather_again<TYPE>(row, from, to, least, top, &r);
+  order(r.keys, r.found, top, r.best);
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -255,50 +351,38 @@ __device__ __forceinline__ void write_top(const LogprobArgs& g, int64_t row, con
   g.top_tokens[row * g.top + lane] = r.none ? -1 : (int64_t)place_of(k);
 }
 
+// In all threads: the row's sums, and in lane i the best but i.
+template <int TYPE, bool TOP>
+__device__ __forceinline__ void finish_row(const LogprobArgs& g, int64_t row, Sums x, Key k, float* room) {
+  using T = typename Stored<TYPE>::type;
+  // beyond float32's range, or with its largest logit there, which then counted as nothing
+  const bool again = x.m > -kInf && (!(x.s > 0.0f && x.s < kInf) || x.at != anchor(x.m, g.scale2));
+  if (again) x = row_again<TYPE>(g, static_cast<const T*>(g.logits) + row * g.stride, x.m, room);
+  if (threadIdx.x >= kWave) return;
+  const Row r(x, again);
+  if (threadIdx.x == 0) write_row<TYPE>(g, row, r);
+  if constexpr (TOP) write_top(g, row, r, k, threadIdx.x);
+}
+
 template <int TYPE, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprob_forward_kernel(LogprobArgs g) {
   using T = typename Stored<TYPE>::type;
-  constexpr int kAhead = 4;
+  constexpr int kAhead = 4, kStep = kThreads * kRun;
   __shared__ Sums sums[kWaves];
   __shared__ float room[2 * kWaves];
-  __shared__ Key keys[TOP ? kWaves : 1][kWave];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int64_t row = block_of();
+  __shared__ __attribute__((aligned(8))) char top_room[TOP ? sizeof(TopRoom) : 8];
+  const int64_t block = block_of(), row = block / g.parts;
   if (row >= g.rows) return;
+  const int part = (int)(block - row * g.parts), from = part * g.part_cols, to = min(from + g.part_cols, g.vocab);
   const void* const at = static_cast<const T*>(g.logits) + row * g.stride;
   Sums x{-kInf, 0.0f, 0.0f, 0.0f};
-  Best best;
-  bool first = true;
-  int col = threadIdx.x * kRun;
-  const auto take = [&](auto& v, int n) {   // N / 8 runs, kThreads * 8 columns apart; the last of n values
-    constexpr int N = sizeof(v) / sizeof(float);
-    float largest = -kInf;
-    if constexpr (TOP) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) largest = fmaxf(largest, v[i]);
-    }
-    add_values(x, v, g.scale2);
-    if constexpr (TOP) {
-      const float over = first ? reached(largest, lane, g.top) : best.above;
-      const bool with = first || !best.full;
-      if (__builtin_amdgcn_ballot_w64(with || largest > over) != 0) {
-#pragma unroll
-        for (int u = 0; u < N / kRun; ++u) {
-          float run[kRun];
-#pragma unroll
-          for (int i = 0; i < kRun; ++i) run[i] = v[u * kRun + i];
-          best.offer(run, col + u * kThreads * kRun, u == N / kRun - 1 ? n : kRun, over, with, lane, g.top);
-        }
-        best.settle();
-      }
-      first = false;
-    }
-  };
-  for (; col - threadIdx.x * kRun + kAhead * kThreads * kRun <= g.vocab; col += kAhead * kThreads * kRun) {
+  int first = from;
+  for (; first + kAhead * kStep <= to; first += kAhead * kStep) {
+    const int col = first + threadIdx.x * kRun;
     Raw w[kAhead];
     float v[kAhead * kRun];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) w[u] = load_raw<TYPE>(at, nullptr, col + u * kThreads * kRun, kRun);
+    for (int u = 0; u < kAhead; ++u) w[u] = load_raw<TYPE>(at, nullptr, col + u * kStep, kRun);
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       float run[kRun];
@@ -306,34 +390,79 @@ __global__ __launch_bounds__(kThreads) void logprob_forward_kernel(LogprobArgs g
 #pragma unroll
       for (int i = 0; i < kRun; ++i) v[u * kRun + i] = run[i];
     }
-    take(v, kRun);
+    add_values(x, v, g.scale2);
   }
-  for (; col - threadIdx.x * kRun < g.vocab; col += kThreads * kRun) {
-    const int n = g.vocab - col;
+  for (; first < to; first += kStep) {
+    const int col = first + threadIdx.x * kRun, n = to - col;
+    if (n <= 0) break;
     float v[kRun];
     load_run<TYPE>(at, col, n, v);
+    if (n < kRun) {
 #pragma unroll
-    for (int i = 0; i < kRun; ++i) v[i] = i < n ? v[i] : -kInf;
-    take(v, n);
+      for (int i = 0; i < kRun; ++i) v[i] = i < n ? v[i] : -kInf;
+    }
+    add_values(x, v, g.scale2);
   }
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) join(x, from_lane(x, d));
-  if (lane == 0) sums[wave] = x;
-  if constexpr (TOP) keys[wave][lane] = best.key;
+  if constexpr (TOP) select_top<TYPE>(at, from, to, x.m, g.top, *reinterpret_cast<TopRoom*>(top_room));
+  x = join_wave(x);
+  if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave] = x;
   __syncthreads();
   x = sums[0];
   for (int i = 1; i < kWaves; ++i) join(x, sums[i]);
-  // beyond float32's range, or with its largest logit there, which then counted as nothing
-  const bool again = x.m > -kInf && (!(x.s > 0.0f && x.s < kInf) || x.at != anchor(x.m, g.scale2));
-  if (again) x = row_again<TYPE>(g, at, x.m, room);
-  if (wave != 0) return;
-  const Row r(x, again);
-  if (lane == 0) write_row<TYPE>(g, row, r);
-  if constexpr (TOP) {
-    Key k = best.key;
-    for (int i = 1; i < kWaves; ++i) k = merge(k, keys[i][kWave - 1 - lane], lane);
-    write_top(g, row, r, k, lane);
+  Key k = 0;
+  if constexpr (TOP) k = reinterpret_cast<TopRoom*>(top_room)->best[threadIdx.x % kMostTop];
+  if (g.parts > 1) {
+    if (threadIdx.x == 0) g.part_sums[block] = x;
+    if (TOP && threadIdx.x < g.top) g.part_keys[block * g.top + threadIdx.x] = k;
+    return;
   }
+  finish_row<TYPE, TOP>(g, row, x, k, room);
+}
+
+// A row's parts joined.
+template <int TYPE, bool TOP>
+__global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
+  __shared__ float room[2 * kWaves];
+  __shared__ Sums sums;
+  __shared__ Key keys[TOP ? kMostParts * kMostTop : 1], best[TOP ? kMostTop : 1];
+  __shared__ Key least;
+  __shared__ uint32_t found;
+  const int64_t row = block_of();
+  if (row >= g.rows) return;
+  const int lane = threadIdx.x % kWave;
+  const Key* const from = g.part_keys + row * g.parts * g.top;
+  if (threadIdx.x < kWave) {
+    Sums x{-kInf, 0.0f, 0.0f, 0.0f};
+    if (lane < g.parts) x = g.part_sums[row * g.parts + lane];
+    x = join_wave(x);
+    if (lane == 0) sums = x;
+    if constexpr (TOP) {
+      // `each` keys of a part are not below its each-th; of those, as many as it takes are not below this one
+      const int each = (g.top + g.parts - 1) / g.parts, needed = (g.top + each - 1) / each;
+      const Key k = lane < g.parts ? from[lane * g.top + each - 1] : 0;
+      int before = 0;
+      for (int j = 0; j < g.parts; ++j) {
+        const Key other = (Key)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k, j);
+        before += other > k || (other == k && j < lane) ? 1 : 0;
+      }
+      if (lane < g.parts && before == needed - 1) least = k;
+      if (lane == 0) found = 0;
+    }
+  }
+  __syncthreads();
+  const Sums x = sums;
+  Key k = 0;
+  if constexpr (TOP) {
+    const Key bound = least;
+    for (int i = threadIdx.x; i < g.parts * g.top; i += kThreads) {
+      const Key one = from[i];
+      if (one != 0 && one >= bound) keys[atomicAdd(&found, 1u)] = one;
+    }
+    __syncthreads();
+    order(keys, found, g.top, best);
+    k = best[threadIdx.x % kMostTop];
+  }
+  finish_row<TYPE, TOP>(g, row, x, k, room);
 }
 
 // ---- backward -----------------------------------------------------------------------------------
@@ -382,6 +511,22 @@ template <bool TOP>
 Forward forward_of(int type) {
   return type == MOC_BF16 ? logprob_forward_kernel<MOC_BF16, TOP> : type == MOC_F16 ? logprob_forward_kernel<MOC_F16, TOP> : logprob_forward_kernel<MOC_F32, TOP>;
 }
+template <bool TOP>
+Forward join_of(int type) {
+  return type == MOC_BF16 ? logprob_join_kernel<MOC_BF16, TOP> : type == MOC_F16 ? logprob_join_kernel<MOC_F16, TOP> : logprob_join_kernel<MOC_F32, TOP>;
+}
+
+// Into how many parts a row is cut, and of how many columns: four workgroups for a unit, of whole turns.
+struct Parts {
+  int parts, cols;
+};
+Parts parts_of(int64_t rows, int64_t vocab, int units) {
+  constexpr int64_t kStep = kThreads * kRun;
+  const int64_t steps = (vocab + kStep - 1) / kStep, wanted = std::min<int64_t>({(4 * (int64_t)units + rows - 1) / std::max<int64_t>(rows, 1), steps, kMostParts});
+  const int64_t each = (steps + wanted - 1) / wanted;
+  return Parts{(int)((steps + each - 1) / each), (int)std::min(each * kStep, vocab)};
+}
+int64_t part_bytes(const Parts& p, int64_t rows, int top) { return p.parts > 1 ? rows * p.parts * (int64_t)(sizeof(Sums) + top * sizeof(Key)) : 0; }
 template <bool ENTROPY>
 Backward backward_of(int type) {
   return type == MOC_BF16 ? logprob_backward_kernel<MOC_BF16, ENTROPY> : type == MOC_F16 ? logprob_backward_kernel<MOC_F16, ENTROPY> : logprob_backward_kernel<MOC_F32, ENTROPY>;
@@ -396,7 +541,10 @@ extern "C" {
 
 int64_t moc_logprob_forward_work(int64_t rows, int64_t vocab, int32_t top) {
   if (!sizes_ok(rows, vocab) || vocab < 1 || top < 0 || top > kMostTop || top > vocab) return MOC_EINVAL;
-  return 0;
+  int units = 0;
+  const int rc = moc_compute_units(&units);
+  if (rc != MOC_OK) return rc;
+  return part_bytes(parts_of(rows, vocab, units), rows, top);
 }
 
 int moc_logprob_forward(int64_t rows, int64_t vocab, const moc_matrix* logits, const void* tokens, int32_t token_bytes, float scale, int32_t top, float* logp, float* lse,
@@ -406,13 +554,27 @@ int moc_logprob_forward(int64_t rows, int64_t vocab, const moc_matrix* logits, c
   if (rows == 0) return MOC_OK;
   if ((tokens == nullptr) != (logp == nullptr) || !lse || !entropy || !aligned_to(logp, 4) || !aligned_to(lse, 4) || !aligned_to(entropy, 4)) return MOC_EINVAL;
   if (top > 0 && (!top_logp || !top_tokens || !aligned_to(top_logp, 4) || !aligned_to(top_tokens, 8))) return MOC_EINVAL;
+  int units = 0;
+  const int rc = moc_compute_units(&units);
+  if (rc != MOC_OK) return rc;
+  const Parts p = parts_of(rows, vocab, units);
+  if (p.parts > 1 && (!work || !aligned_to(work, 16) || work_bytes < part_bytes(p, rows, top))) return MOC_EINVAL;
   LogprobArgs g = {};
+  g.parts = p.parts; g.part_cols = p.cols;
+  if (p.parts > 1) {
+    g.part_sums = static_cast<Sums*>(work);
+    g.part_keys = reinterpret_cast<Key*>(g.part_sums + rows * p.parts);
+  }
   g.logits = logits->data; g.stride = logits->stride;
   g.rows = rows; g.vocab = (int)vocab; g.top = top; g.token_bytes = token_bytes;
   g.scale = scale; g.scale2 = (float)((double)scale * 1.4426950408889634);
   g.tokens = tokens; g.logp = logp; g.lse = lse; g.entropy = entropy; g.top_logp = top_logp; g.top_tokens = top_tokens;
-  hipLaunchKernelGGL(top > 0 ? forward_of<true>(logits->type) : forward_of<false>(logits->type), grid_of(rows), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), g);
+  hipLaunchKernelGGL(top > 0 ? forward_of<true>(logits->type) : forward_of<false>(logits->type), grid_of(rows * p.parts), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), g);
   MOC_HIP(hipGetLastError());
+  if (p.parts > 1) {
+    hipLaunchKernelGGL(top > 0 ? join_of<true>(logits->type) : join_of<false>(logits->type), grid_of(rows), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), g);
+    MOC_HIP(hipGetLastError());
+  }
   return MOC_OK;
 }
 

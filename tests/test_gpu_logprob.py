@@ -163,6 +163,25 @@ def test_masks_and_orders(tr, vocab, dtype):
     check_gradient(d[ok], x[ok], tokens[ok], got.lse[ok.cuda()], got.entropy[ok.cuda()], dlogp[ok], dh[ok], 1.0)
 
 
+@pytest.mark.parametrize("rows,vocab", [(1100, 70001), (64, 300001)])
+def test_alternatives_that_lie_close_together(tr, rows, vocab):
+    """More logits above what many lanes reach than there is room for: whole runs of a few lanes, over all of a row or of a part; and
+    rows with more equal ones than that."""
+    g = gen(rows, vocab)
+    x = torch.randn(rows, vocab, generator=g).half()
+    run = torch.arange(vocab) // 8 % 256
+    some = [0, 7, rows // 2, rows - 1]
+    x[0] = torch.where(run < 20, 100 + torch.rand(vocab, generator=g) * 50, -1.0).half()
+    x[7] = torch.where(run % 37 == 5, 3.0, -torch.rand(vocab, generator=g)).half()
+    x[rows // 2] = torch.where(run == 255, torch.arange(vocab) / 8.0, -math.inf).half()
+    x[rows - 1] = torch.where((run < 2) | (torch.arange(vocab) > vocab - 3000), 5.0, 0.0).half()
+    for top in (1, 5, 20, 64):
+        got = tr.moc_logprob_forward(x.cuda(), top=top)
+        want = definition(x[some].double(), torch.zeros(4, dtype=torch.int64), 1.0, top)
+        assert torch.equal(got.top_tokens.cpu()[some], want["ids"])
+        check_forward(type(got)(None, *(None if t is None else t[some] for t in got[1:])), want, vocab, 1.0)
+
+
 def test_values_that_are_no_logits(tr):
     """NaN and +infinity anywhere, in every kind of row, leave a row's results NaN and no alternatives; other rows keep theirs."""
     for dtype in TYPES.values():
