@@ -481,27 +481,48 @@ __global__ __launch_bounds__(kThreads) void logprob_backward_kernel(LogprobArgs 
   const int64_t token = g.dlogp ? token_of(g, row) : -1;
   const float dl = token < 0 ? 0.0f : token < g.vocab ? g.dlogp[row] : bits_float(0x7FC00000u);
   const bool empty = lse == -kInf;
-  Raw w[kTurns];
+  const auto gradient = [&](float x, int col) {
+    const float z = larger(__builtin_fmaf(x, g.scale, -lse), kFar), p = exp2_of(z * kLog2e);
+    float d = dl * ((token == col ? 1.0f : 0.0f) - p);
+    if (ENTROPY) d -= dh * p * (z + entropy);
+    return empty ? 0.0f : g.scale * d;
+  };
+  if constexpr (TYPE == MOC_F32) {   // four values a lane: 16 bytes, next to the neighbour's
+    constexpr int kFew = 4;
+    u32x4 w[2 * kTurns];
 #pragma unroll
-  for (int t = 0; t < kTurns; ++t) {
-    const int col = from + (t * kThreads + threadIdx.x) * kRun;
-    w[t] = load_raw<TYPE>(at, nullptr, col, g.vocab - col);
-  }
-#pragma unroll
-  for (int t = 0; t < kTurns; ++t) {
-    const int col = from + (t * kThreads + threadIdx.x) * kRun, n = g.vocab - col;
-    if (n <= 0) break;
-    float v[kRun];
-    values_of<TYPE>(w[t], v);
-    const int64_t mine = token - col;
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) {
-      const float z = larger(__builtin_fmaf(v[i], g.scale, -lse), kFar), p = exp2_of(z * kLog2e);
-      float d = dl * ((mine == i ? 1.0f : 0.0f) - p);
-      if (ENTROPY) d -= dh * p * (z + entropy);
-      v[i] = empty ? 0.0f : g.scale * d;
+    for (int t = 0; t < 2 * kTurns; ++t) {
+      const int col = from + (t * kThreads + threadIdx.x) * kFew;
+      if (col + kFew <= g.vocab) __builtin_memcpy(&w[t], static_cast<const float*>(at) + col, 16);
     }
-    store_any(g.out_type, out, col, n, v);
+#pragma unroll
+    for (int t = 0; t < 2 * kTurns; ++t) {
+      const int col = from + (t * kThreads + threadIdx.x) * kFew;
+      if (col + kFew <= g.vocab) {
+#pragma unroll
+        for (int i = 0; i < kFew; ++i) w[t][i] = float_bits(gradient(bits_float(w[t][i]), col + i));
+        __builtin_memcpy(reinterpret_cast<float*>(out) + col, &w[t], 16);
+      } else {
+        for (int c = col; c < g.vocab; ++c) reinterpret_cast<float*>(out)[c] = gradient(static_cast<const float*>(at)[c], c);
+      }
+    }
+  } else {
+    Raw w[kTurns];
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+      const int col = from + (t * kThreads + threadIdx.x) * kRun;
+      w[t] = load_raw<TYPE>(at, nullptr, col, g.vocab - col);
+    }
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+      const int col = from + (t * kThreads + threadIdx.x) * kRun, n = g.vocab - col;
+      if (n <= 0) break;
+      float v[kRun];
+      values_of<TYPE>(w[t], v);
+#pragma unroll
+      for (int i = 0; i < kRun; ++i) v[i] = gradient(v[i], col + i);
+      store_any(g.out_type, out, col, n, v);
+    }
   }
 }
 
