@@ -120,6 +120,36 @@ __device__ __forceinline__ Sums join_wave(Sums x) {
   return Sums{wave_largest(x.m), x.at, wave_sum(x.s), wave_sum(x.w)};
 }
 
+// ---- columns ------------------------------------------------------------------------------------
+
+// The columns lo .. hi - 1 of a row, taken in runs of eight from `first` on, where runs begin at aligned addresses: up to seven
+// columns before lo.
+constexpr int kStep = kThreads * kRun;
+struct Columns {
+  int first, lo, hi;
+};
+// Runs begin at addresses that are multiples of 16 bytes.
+template <int TYPE>
+__device__ __forceinline__ int before_row(const void* row) {
+  return (int)(reinterpret_cast<uintptr_t>(row) % 16) / (int)sizeof(typename Stored<TYPE>::type);
+}
+__device__ __forceinline__ bool whole_run(const Columns& c, int col) { return col >= c.lo && col + kRun <= c.hi; }
+// A run that is not wholly there, `otherwise` for what is not: loads without a branch, none of which is waited for alone.
+template <int TYPE>
+__device__ __forceinline__ void load_edge(const void* row, const Columns& c, int col, float otherwise, float (&v)[kRun]) {
+  using T = typename Stored<TYPE>::type;
+  T t[kRun];
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) t[i] = static_cast<const T*>(row)[min(max(col + i, c.lo), c.hi - 1)];
+#pragma unroll
+  for (int i = 0; i < kRun; ++i) v[i] = col + i >= c.lo && col + i < c.hi ? (float)t[i] : otherwise;
+}
+template <int TYPE>
+__device__ __forceinline__ void load_columns(const void* row, const Columns& c, int col, float otherwise, float (&v)[kRun]) {
+  if (whole_run(c, col)) load_run<TYPE>(row, col, kRun, v);
+  else load_edge<TYPE>(row, c, col, otherwise, v);
+}
+
 // ---- alternatives -------------------------------------------------------------------------------
 
 using Key = uint64_t;   // a logit's order in the upper half, the complement of its place in the lower; 0: none
@@ -163,16 +193,16 @@ __device__ __forceinline__ void find_least(TopRoom& r, int top) {
 
 // What is above `least`, or not below it (`with`), of the columns of lanes that reach it, to r.keys as far as it goes.
 template <int TYPE>
-__device__ __forceinline__ void gather(const void* row, int from, int to, float least, bool with, TopRoom& r) {
-  const uint32_t lanes = r.reach, total = lanes * (uint32_t)((to - from + kThreads * kRun - 1) / (kThreads * kRun));
+__device__ __forceinline__ void gather(const void* row, const Columns& c, float least, bool with, TopRoom& r) {
+  const uint32_t lanes = r.reach, total = lanes * (uint32_t)((c.hi - c.first + kStep - 1) / kStep);
   for (uint32_t i = threadIdx.x; i < total; i += kThreads) {
-    const int col = from + (int)(i / lanes * kThreads + r.lanes[i % lanes]) * kRun, n = to - col;
-    if (n <= 0) continue;
+    const int col = c.first + (int)(i / lanes * kThreads + r.lanes[i % lanes]) * kRun;
+    if (col >= c.hi) continue;
     float v[kRun];
-    load_run<TYPE>(row, col, n, v);
+    load_columns<TYPE>(row, c, col, bits_float(0x7FC00000u), v);
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
-      if (j >= n || !(with ? v[j] >= least : v[j] > least)) continue;
+      if (!(with ? v[j] >= least : v[j] > least)) continue;
       const uint32_t at = atomicAdd(&r.found, 1u);
       if (at < kRoom) r.keys[at] = key_of(v[j], (uint32_t)(col + j));
     }
@@ -182,11 +212,12 @@ __device__ __forceinline__ void gather(const void* row, int from, int to, float 
 // More logits than there is room for: those above `least`, and of those that equal it the first ones, as many as are missing.
 // Where even those above it are too many, one after the other by a pass each.  By all threads, as all of these.
 template <int TYPE>
-__device__ __attribute__((noinline)) void gather_again(const void* row, int from, int to, float least, int top, TopRoom* room) {
+__device__ __attribute__((noinline)) void gather_again(const void* row, Columns c, float least, int top, TopRoom* room) {
   TopRoom& r = *room;
+  const int from = c.lo, to = c.hi;
   if (threadIdx.x == 0) r.found = 0;
   __syncthreads();
-  gather<TYPE>(row, from, to, least, false, r);
+  gather<TYPE>(row, c, least, false, r);
   __syncthreads();
   const uint32_t above = r.found;
   if (above <= kRoom - kMostTop) {
@@ -255,9 +286,9 @@ __device__ __forceinline__ void order(const Key* keys, uint32_t n, int top, Key*
   __syncthreads();
 }
 
-// The best of columns from .. to, of which `mine` is the largest of this thread's, to r.best.
+// The best of some columns, of which `mine` is the largest of this thread's, to r.best.
 template <int TYPE>
-__device__ __forceinline__ void select_top(const void* row, int from, int to, float mine, int top, TopRoom& r) {
+__device__ __forceinline__ void select_top(const void* row, const Columns& c, float mine, int top, TopRoom& r) {
   r.largest[threadIdx.x] = mine;
   if (threadIdx.x == 0) r.reach = r.found = 0;
   __syncthreads();
@@ -266,9 +297,9 @@ __device__ __forceinline__ void select_top(const void* row, int from, int to, fl
   const float least = r.least;
   if (mine >= least) r.lanes[atomicAdd(&r.reach, 1u)] = (uint16_t)threadIdx.x;
   __syncthreads();
-  gather<TYPE>(row, from, to, least, true, r);
+  gather<TYPE>(row, c, least, true, r);
   __syncthreads();
-  if (r.found > kRoom) gather_again<TYPE>(row, from, to, least, top, &r);
+  if (r.found > kRoom) gather_again<TYPE>(row, c, least, top, &r);
   order(r.keys, r.found, top, r.best);
 }
 
@@ -367,43 +398,48 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& g, int64_t row, Su
 template <int TYPE, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprob_forward_kernel(LogprobArgs g) {
   using T = typename Stored<TYPE>::type;
-  constexpr int kAhead = 4, kStep = kThreads * kRun;
+  constexpr int kAhead = 4;
   __shared__ Sums sums[kWaves];
   __shared__ float room[2 * kWaves];
   __shared__ __attribute__((aligned(8))) char top_room[TOP ? sizeof(TopRoom) : 8];
   const int64_t block = block_of(), row = block / g.parts;
   if (row >= g.rows) return;
-  const int part = (int)(block - row * g.parts), from = part * g.part_cols, to = min(from + g.part_cols, g.vocab);
   const void* const at = static_cast<const T*>(g.logits) + row * g.stride;
+  const int begin = (int)(block - row * g.parts) * g.part_cols - before_row<TYPE>(at);
+  const Columns c{begin, max(begin, 0), min(begin + g.part_cols, g.vocab)};
   Sums x{-kInf, 0.0f, 0.0f, 0.0f};
-  int first = from;
-  for (; first + kAhead * kStep <= to; first += kAhead * kStep) {
+  // kAhead runs of a lane on their way at a time; at both ends they may not all be there
+  for (int first = c.first; first < c.hi; first += kAhead * kStep) {
     const int col = first + threadIdx.x * kRun;
     Raw w[kAhead];
     float v[kAhead * kRun];
+    if (first >= c.lo && first + kAhead * kStep <= c.hi) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) w[u] = load_raw<TYPE>(at, nullptr, col + u * kStep, kRun);
+      for (int u = 0; u < kAhead; ++u) w[u] = load_raw<TYPE>(at, nullptr, col + u * kStep, kRun);
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      float run[kRun];
-      values_of<TYPE>(w[u], run);
+      for (int u = 0; u < kAhead; ++u) {
+        float run[kRun];
+        values_of<TYPE>(w[u], run);
 #pragma unroll
-      for (int i = 0; i < kRun; ++i) v[u * kRun + i] = run[i];
+        for (int i = 0; i < kRun; ++i) v[u * kRun + i] = run[i];
+      }
+      add_values(x, v, g.scale2);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (whole_run(c, col + u * kStep)) w[u] = load_raw<TYPE>(at, nullptr, col + u * kStep, kRun);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (first + u * kStep >= c.hi) break;
+        if (col + u * kStep >= c.hi) continue;
+        float run[kRun];
+        if (whole_run(c, col + u * kStep)) values_of<TYPE>(w[u], run);
+        else load_edge<TYPE>(at, c, col + u * kStep, -kInf, run);
+        add_values(x, run, g.scale2);
+      }
     }
-    add_values(x, v, g.scale2);
   }
-  for (; first < to; first += kStep) {
-    const int col = first + threadIdx.x * kRun, n = to - col;
-    if (n <= 0) break;
-    float v[kRun];
-    load_run<TYPE>(at, col, n, v);
-    if (n < kRun) {
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) v[i] = i < n ? v[i] : -kInf;
-    }
-    add_values(x, v, g.scale2);
-  }
-  if constexpr (TOP) select_top<TYPE>(at, from, to, x.m, g.top, *reinterpret_cast<TopRoom*>(top_room));
+  if constexpr (TOP) select_top<TYPE>(at, c, x.m, g.top, *reinterpret_cast<TopRoom*>(top_room));
   x = join_wave(x);
   if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave] = x;
   __syncthreads();
@@ -509,7 +545,7 @@ __global__ __launch_bounds__(kThreads) void logprob_backward_kernel(LogprobArgs 
   } else {
     // Runs begin where the output is 16 bytes apart from an aligned address: rows of an odd size do not (4999 x 32003 fp16
     // 166 us at 2-byte addresses).  The first run of a row may begin before it.
-    const int shift = g.out_type == TYPE ? (int)(reinterpret_cast<uintptr_t>(out) % 16) / 2 : 0;
+    const int shift = g.out_type == TYPE ? before_row<TYPE>(out) : 0;
     Raw w[kTurns];
 #pragma unroll
     for (int t = 0; t < kTurns; ++t) {
@@ -546,15 +582,15 @@ Forward join_of(int type) {
   return type == MOC_BF16 ? logprob_join_kernel<MOC_BF16, TOP> : type == MOC_F16 ? logprob_join_kernel<MOC_F16, TOP> : logprob_join_kernel<MOC_F32, TOP>;
 }
 
-// Into how many parts a row is cut, and of how many columns: four workgroups for a unit, of whole turns.
+// Into how many parts a row is cut, and of how many columns: four workgroups for a unit, of whole steps.  `before`: how many
+// columns before a row its first run may begin.
 struct Parts {
   int parts, cols;
 };
-Parts parts_of(int64_t rows, int64_t vocab, int units) {
-  constexpr int64_t kStep = kThreads * kRun;
-  const int64_t steps = (vocab + kStep - 1) / kStep, wanted = std::min<int64_t>({(4 * (int64_t)units + rows - 1) / std::max<int64_t>(rows, 1), steps, kMostParts});
+Parts parts_of(int64_t rows, int64_t vocab, int units, int before) {
+  const int64_t steps = (vocab + before + kStep - 1) / kStep, wanted = std::min<int64_t>({(4 * (int64_t)units + rows - 1) / std::max<int64_t>(rows, 1), steps, kMostParts});
   const int64_t each = (steps + wanted - 1) / wanted;
-  return Parts{(int)((steps + each - 1) / each), (int)std::min(each * kStep, vocab)};
+  return Parts{(int)((steps + each - 1) / each), (int)(each * kStep)};
 }
 int64_t part_bytes(const Parts& p, int64_t rows, int top) { return p.parts > 1 ? rows * p.parts * (int64_t)(sizeof(Sums) + top * sizeof(Key)) : 0; }
 template <bool ENTROPY>
@@ -574,7 +610,7 @@ int64_t moc_logprob_forward_work(int64_t rows, int64_t vocab, int32_t top) {
   int units = 0;
   const int rc = moc_compute_units(&units);
   if (rc != MOC_OK) return rc;
-  return part_bytes(parts_of(rows, vocab, units), rows, top);
+  return std::max(part_bytes(parts_of(rows, vocab, units, 0), rows, top), part_bytes(parts_of(rows, vocab, units, kRun - 1), rows, top));
 }
 
 int moc_logprob_forward(int64_t rows, int64_t vocab, const moc_matrix* logits, const void* tokens, int32_t token_bytes, float scale, int32_t top, float* logp, float* lse,
@@ -587,7 +623,8 @@ int moc_logprob_forward(int64_t rows, int64_t vocab, const moc_matrix* logits, c
   int units = 0;
   const int rc = moc_compute_units(&units);
   if (rc != MOC_OK) return rc;
-  const Parts p = parts_of(rows, vocab, units);
+  const bool aligned = aligned_to(logits->data, 16) && (rows == 1 || logits->stride * type_bytes(logits->type) % 16 == 0);
+  const Parts p = parts_of(rows, vocab, units, aligned ? 0 : kRun - 1);
   if (p.parts > 1 && (!work || !aligned_to(work, 16) || work_bytes < part_bytes(p, rows, top))) return MOC_EINVAL;
   LogprobArgs g = {};
   g.parts = p.parts; g.part_cols = p.cols;
