@@ -14,6 +14,7 @@ namespace {
 // turn and 891 with two, 16 blocks of 2048 in 8 bits 2630 with one, 2381 with two, 2348 with four.
 constexpr int kThreads = 256, kFew = 4, kTurn = kThreads * kFew;
 constexpr int turns(bool eight) { return eight ? 2 : 1; }
+constexpr int kReadTurns = 4;
 constexpr int chunk(bool eight) { return kTurn * turns(eight); }   // values of a workgroup
 using Four = float[kFew];
 constexpr int kTensors = 40;                              // of a launch: its arguments have to stay below 4 KB
@@ -326,7 +327,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(AdamwArgs g) {
 }
 
 __global__ __launch_bounds__(kThreads) void moments_read_kernel(AdamwArgs g) {
-  constexpr int kTurns = turns(true), kChunk = chunk(true);
+  constexpr int kTurns = kReadTurns, kChunk = kTurn * kTurns;
   const uint32_t block = (uint32_t)block_of();
   const int at = entry_of(g.first, block);
   const Entry& e = g.entry[at];
@@ -467,7 +468,7 @@ int moc_moments_read(int64_t tensors, const moc_moments_tensor* tensor, void* hi
     if (t.count > 0 && (!t.m_values || !t.v_values || !aligned_to(t.m_values, type_bytes(t.value_type)) || !aligned_to(t.v_values, type_bytes(t.value_type)))) return MOC_EINVAL;
   }
   AdamwArgs g = {};
-  return queue(moments_read_kernel, chunk(true), g, tensors, static_cast<hipStream_t>(hip_stream), [&](int64_t i, Entry& e) {
+  return queue(moments_read_kernel, kTurn * kReadTurns, g, tensors, static_cast<hipStream_t>(hip_stream), [&](int64_t i, Entry& e) {
     const moc_moments_tensor& t = tensor[i];
     if (t.count == 0) return false;
     e.m = const_cast<void*>(t.m); e.v = const_cast<void*>(t.v);

@@ -472,17 +472,20 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
     if (lane < g.parts) x = g.part_sums[row * g.parts + lane];
     x = join_wave(x);
     if (lane == 0) sums = x;
-    if constexpr (TOP) {
-      // `each` keys of a part are not below its each-th; of those, as many as it takes are not below this one
-      const int each = (g.top + g.parts - 1) / g.parts, needed = (g.top + each - 1) / each;
-      const Key k = lane < g.parts ? from[lane * g.top + each - 1] : 0;
-      int before = 0;
-      for (int j = 0; j < g.parts; ++j) {
-        const Key other = (Key)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k, j);
-        before += other > k || (other == k && j < lane) ? 1 : 0;
-      }
-      if (lane < g.parts && before == needed - 1) least = k;
-      if (lane == 0) found = 0;
+  } else if (TOP && threadIdx.x < 2 * kWave) {
+    // `each` keys of a part are not below its each-th; of those, as many as it takes are not below the largest number of 16 bits
+    // that so many of their upper ends are not below
+    const int each = (g.top + g.parts - 1) / g.parts, needed = (g.top + each - 1) / each;
+    const uint32_t upper = lane < g.parts ? (uint32_t)(from[lane * g.top + each - 1] >> 48) : 0;
+    uint32_t t = 0;
+#pragma unroll
+    for (int bit = 15; bit >= 0; --bit) {
+      const uint32_t next = t | 1u << bit;
+      if (__builtin_popcountll(__builtin_amdgcn_ballot_w64(upper >= next)) >= needed) t = next;
+    }
+    if (lane == 0) {
+      least = (Key)t << 48;
+      found = 0;
     }
   }
   __syncthreads();
