@@ -224,6 +224,20 @@ __device__ __forceinline__ float of_row(const float* p, uint32_t row) {
   return reinterpret_cast<Constant>(reinterpret_cast<uintptr_t>(p))[row];
 }
 
+// A parameter's run: as it is held, or read again from cache in kernels that have no registers for it.
+template <bool HOLD>
+__device__ __forceinline__ const float (&param_of(const float (&held)[kRun], const void* p, int type, int col, int cols, float other, float (&room)[kRun]))[kRun] {
+  if constexpr (HOLD) return held;
+  if (p) {
+    const Mat m{static_cast<char*>(const_cast<void*>(p)), nullptr, 0, 0, type};
+    values_of_run<kTensor>(m, load_run_of<kTensor>(m, 0, col, cols, cols >= kRun), col, cols, cols >= kRun, room);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) room[i] = other;
+  }
+  return room;
+}
+
 // ---- arithmetic ---------------------------------------------------------------------------------
 
 // Operations as they are written, none of them fused by the compiler: every kernel gives the same bits.

@@ -192,15 +192,15 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_any_kerne
   }
 }
 
-// Made for types: of a call with a norm before the next block, with dr, dx and dblock, and gates of many rows.  MODE: kPlain,
-// where the block's output is not looked at, kGated, or kNormed with a norm behind it (and a gate, which may be ones).
-// Lanes beyond the row take no part but in the sums.
-constexpr int kPlain = 0, kGated = 1, kNormed = 2;
+// Made for types: of a call with a norm before the next block, with dr and dblock, and gates of many rows.  MODE: kAlone, where
+// there is but a norm, without dr, kPlain, where the block's output is not looked at, kGated, or kNormed with a norm behind it
+// (and a gate, which may be ones).  Lanes beyond the row take no part but in the sums.
+constexpr int kAlone = 0, kPlain = 1, kGated = 2, kNormed = 3;
 
 template <int S, int B, int D, int T, int CH, int MODE>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(ResidualArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
-  constexpr bool kAhead = CH == 1 || T <= 512;
+  constexpr bool kAhead = CH == 1 || T <= 512, kHold = kAhead;
   using Sums = RowSums<T, 2>;
   __shared__ float room[Sums::kRoom];
   __shared__ float stage[kRows > 1 ? kRows * kRun * T : 1];
@@ -226,8 +226,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
       const uint32_t col = (c * T + lane) * kRun;
       wr[c] = fetch<S>(g.r, row, col, cols);
       wn[c] = fetch<D>(g.dn, row, col, cols);
-      wd[c] = fetch<S>(g.dr, row, col, cols);
-      if constexpr (MODE != kPlain) wb[c] = fetch<B>(g.block, row, col, cols);
+      if constexpr (MODE != kAlone) wd[c] = fetch<S>(g.dr, row, col, cols);
+      if constexpr (MODE > kPlain) wb[c] = fetch<B>(g.block, row, col, cols);
     }
     stats[0] = of_row(means2, row);
     stats[1] = of_row(g.before.rstd, row);
@@ -240,14 +240,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
     const uint32_t first = which * g.rows_per_gate + chunk * g.chunk_rows, end = min(first + g.chunk_rows, (which + 1) * g.rows_per_gate);
     uint32_t row = first + mine;
     if (kAhead && row < end) load(row);
-    if (which == from) {   // with the first row on its way
+    if (kHold && which == from) {   // with the first row on its way
       if constexpr (MODE == kNormed) {
         hold_param<T, CH>(g.after.gamma, g.after.param_type, lane, cols, 1.0f, gamma1);
         hold_param<T, CH>(g.after.beta, g.after.param_type, lane, cols, 0.0f, beta1);
       }
       hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, cols, 1.0f, gamma2);
     }
-    if constexpr (MODE != kPlain) hold_gate<T, CH>(g, which, lane, gate);
+    if constexpr (MODE > kPlain && kHold) hold_gate<T, CH>(g, which, lane, gate);
     for (; row < end; row += kRows) {   // groups of lanes that end earlier share no barrier
       if (!kAhead) load(row);
       Runs<CH> h, d;
@@ -258,8 +258,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
       for (int c = 0; c < CH; ++c) {
         cr[c] = wr[c];
         cn[c] = wn[c];
-        cd[c] = wd[c];
-        if constexpr (MODE != kPlain) cb[c] = wb[c];
+        if constexpr (MODE != kAlone) cd[c] = wd[c];
+        if constexpr (MODE > kPlain) cb[c] = wb[c];
       }
       if (kAhead) load(min(row + kRows, end - 1));   // behind the last row it once more
 #pragma unroll
@@ -268,13 +268,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
         if (col < cols && col + kRun > cols) {
           settle_run<S>(cr[c], col, cols);
           settle_run<D>(cn[c], col, cols);
-          settle_run<S>(cd[c], col, cols);
-          if constexpr (MODE != kPlain) settle_run<B>(cb[c], col, cols);
+          if constexpr (MODE != kAlone) settle_run<S>(cd[c], col, cols);
+          if constexpr (MODE > kPlain) settle_run<B>(cb[c], col, cols);
         }
         if (col < cols) {
           values_fetched<S>(g.r, cr[c], h[c]);
           values_fetched<D>(g.dn, cn[c], d[c]);
-          before_run(h[c], d[c], mean2, rstd2, gamma2[c], sg2[c], sb2[c], m);   // where the row has ended h meets zeros
+          float ga[kRun];   // where the row has ended h meets zeros
+          before_run(h[c], d[c], mean2, rstd2, param_of<kHold>(gamma2[c], g.before.gamma, g.before.param_type, (int)col, g.cols, 1.0f, ga), sg2[c], sb2[c], m);
         }
       }
       sums(m);
@@ -285,19 +286,26 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
         const uint32_t col = (c * T + lane) * kRun;
         if (col < cols) {
           float v[kRun];
-          values_fetched<S>(g.dr, cd[c], v);
           norm_gradient(d[c], h[c], rstd2, a2, b2);
-          add_run(d[c], v);
+          if constexpr (MODE != kAlone) {
+            values_fetched<S>(g.dr, cd[c], v);
+            add_run(d[c], v);
+          }
+          if (g.dx.data) {
 #pragma unroll
-          for (int i = 0; i < kRun; ++i) v[i] = g.scale * d[c][i];
-          put<S>(g.dx, row, col, cols, v);
-          if constexpr (MODE != kPlain) {
+            for (int i = 0; i < kRun; ++i) v[i] = g.scale * d[c][i];
+            put<S>(g.dx, row, col, cols, v);
+          }
+          if constexpr (MODE > kPlain) {
             if (col + kRun > cols) {
 #pragma unroll
               for (uint32_t i = 0; i < kRun; ++i) d[c][i] = col + i < cols ? d[c][i] : 0.0f;
             }
             values_fetched<B>(g.block, cb[c], h[c]);
-            gate_run<MODE == kNormed>(h[c], d[c], v, mean1, rstd1, gamma1[c], beta1[c], gate[c], sg1[c], sb1[c], m);
+            float ga[kRun], be[kRun], of[kRun];
+            gate_run<MODE == kNormed>(h[c], d[c], v, mean1, rstd1, param_of<kHold || MODE != kNormed>(gamma1[c], g.after.gamma, g.after.param_type, (int)col, g.cols, 1.0f, ga),
+                                      param_of<kHold || MODE != kNormed>(beta1[c], g.after.beta, g.after.param_type, (int)col, g.cols, 0.0f, be),
+                                      param_of<kHold>(gate[c], g.gates ? row_at(g.gate, which) : nullptr, g.gate.type, (int)col, g.cols, 1.0f, of), sg1[c], sb1[c], m);
             add_run(sgate[c], v);
           }
         }
@@ -420,7 +428,7 @@ Shape backward_shape(int64_t cols) {
 }
 template <int S, int B, int D>
 Shape backward_shape(int mode, int64_t cols) {
-  return mode == kPlain ? backward_shape<S, D, D, kPlain>(cols) : mode == kGated ? backward_shape<S, B, D, kGated>(cols) : backward_shape<S, B, D, kNormed>(cols);
+  return mode == kAlone ? backward_shape<S, D, D, kAlone>(cols) : mode == kPlain ? backward_shape<S, D, D, kPlain>(cols) : mode == kGated ? backward_shape<S, B, D, kGated>(cols) : backward_shape<S, B, D, kNormed>(cols);
 }
 Shape any_shape(bool after, int64_t cols) { return after ? backward_shape<kAny, kAny, kAny, kNormed>(cols) : backward_shape<kAny, kAny, kAny, kPlain>(cols); }
 template <int D>
@@ -513,13 +521,13 @@ int moc_residual_backward(int64_t rows, int64_t cols, const moc_matrix* dr, cons
   ResidualArgs g = {};
   g.parts = lies_over(dx, {dr, dn, r, block, gate}) || lies_over(dblock, {dr, dn, r, block, gate});
   // kernels made for some types, where all matrices are of them and a row's last run may be loaded whole
-  const bool ragged = cols < kRun || (g.parts && cols % kRun != 0), usual = last && dr && dx && dblock && !(gates > 1 && gates == rows) && !ragged;
-  const int kd = agreed({dn, dblock}, kAny), ks = agreed({dr, r, dx}, kAny), kb = needed ? kind_of(block->type) : kd, mode = first ? kNormed : needed || gate ? kGated : kPlain;
-  const Shape s = !usual || (mode != kPlain && !needed) ? any_shape(first, cols)
+  const bool ragged = cols < kRun || (g.parts && cols % kRun != 0), usual = last && dblock && !(gates > 1 && gates == rows) && !ragged;
+  const int kd = agreed({dn, dblock}, kAny), ks = agreed({dr, r, dx}, kAny), kb = needed ? kind_of(block->type) : kd, mode = first ? kNormed : needed || gate ? kGated : dr ? kPlain : kAlone;
+  const Shape s = !usual || (mode > kPlain && !(needed && dr)) ? any_shape(first, cols)
                   : kd == MOC_BF16                      ? backward_shape<MOC_BF16>(ks, kb, mode, cols)
                   : kd == MOC_F16                       ? backward_shape<MOC_F16>(ks, kb, mode, cols)
                                                         : any_shape(first, cols);
-  const Cut c = cut_of(s, rows, gates, units, mode == kPlain && cols <= 4096 ? kManyWaves : kFewWaves);
+  const Cut c = cut_of(s, rows, gates, units, mode <= kPlain && cols <= 4096 ? kManyWaves : kFewWaves);
   const bool gate_parts = d.gate && !c.own && c.chunks > 1;
   const int64_t need = sums_bytes(c, kinds, gates, d.gate != nullptr, cols);
   if (need > 0 && (!work || !aligned_to(work, 16) || work_bytes < need)) return MOC_EINVAL;

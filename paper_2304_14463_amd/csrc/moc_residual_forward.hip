@@ -52,14 +52,17 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_forward_kernel(Res
     }
   };
   if (row < g.rows) load(row);
+  constexpr bool kHold = CH == 1 || T < kMaxThreads;
   Runs<CH> gamma1, beta1, gate, gamma2, beta2;
-  if constexpr (AFTER) {
+  if constexpr (AFTER && kHold) {
     hold_param<T, CH>(g.after.gamma, g.after.param_type, lane, g.cols, 1.0f, gamma1);
     hold_param<T, CH>(g.after.beta, g.after.param_type, lane, g.cols, 0.0f, beta1);
   }
   if (g.gates <= 1) hold_gate<T, CH>(g, 0, lane, gate);
-  hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, g.cols, 1.0f, gamma2);
-  hold_param<T, CH>(g.before.beta, g.before.param_type, lane, g.cols, 0.0f, beta2);
+  if constexpr (kHold) {
+    hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, g.cols, 1.0f, gamma2);
+    hold_param<T, CH>(g.before.beta, g.before.param_type, lane, g.cols, 0.0f, beta2);
+  }
   for (; row < g.rows; row += step) {
     Runs<CH> v;
     Raw x[CH];
@@ -79,7 +82,12 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_forward_kernel(Res
         g.after.rstd[row] = rstd;
       }
 #pragma unroll
-      for (int c = 0; c < CH; ++c) normalise(v[c], mean, rstd, gamma1[c], beta1[c]);
+      for (int c = 0; c < CH; ++c) {
+        const int col = asked_again((c * T + lane) * kRun);
+        float ga[kRun], be[kRun];
+        normalise(v[c], mean, rstd, param_of<kHold>(gamma1[c], g.after.gamma, g.after.param_type, col, g.cols, 1.0f, ga),
+                  param_of<kHold>(beta1[c], g.after.beta, g.after.param_type, col, g.cols, 0.0f, be));
+      }
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -108,7 +116,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_forward_kernel(Res
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int col = asked_again((c * T + lane) * kRun), n = g.cols - col;
-      normalise(v[c], mean, rstd, gamma2[c], beta2[c]);
+      float ga[kRun], be[kRun];
+      normalise(v[c], mean, rstd, param_of<kHold>(gamma2[c], g.before.gamma, g.before.param_type, col, g.cols, 1.0f, ga),
+                param_of<kHold>(beta2[c], g.before.beta, g.before.param_type, col, g.cols, 0.0f, be));
       store_run_of<D>(g.n, row, col, n, v[c]);
       if (!g.kept.data) continue;
       if (n < kRun) {
