@@ -11,17 +11,13 @@
 
 #include "moc_rows.h"
 
-namespace {
-
-constexpr int kMaxThreads = 1024;
-
-struct Mat {
+struct ResidualMat {
   char* data;
   uint8_t* scales;
   uint32_t step, scale_step;   // bytes from one row to the next
   int type;
 };
-struct RowNorm {
+struct ResidualNorm {
   const void *gamma, *beta;
   int param_type;
   float eps;
@@ -29,9 +25,9 @@ struct RowNorm {
   float *mean, *rstd;
 };
 struct ResidualArgs {
-  Mat x, block, gate, r, n, kept;
-  Mat dr, dn, dx, dblock;
-  RowNorm after, before;
+  ResidualMat x, block, gate, r, n, kept;
+  ResidualMat dr, dn, dx, dblock;
+  ResidualNorm after, before;
   uint32_t rows, gates, rows_per_gate;
   int cols;
   float scale, most;
@@ -43,6 +39,14 @@ struct ResidualArgs {
   bool want_gate, own_gates;   // own: a gate for every row
   uint32_t chunks, chunk_rows, groups;   // workgroups of a gate's rows, and their rows; or gates of a workgroup
 };
+
+namespace {
+
+constexpr int kMaxThreads = 1024;
+
+using Mat = ResidualMat;
+using RowNorm = ResidualNorm;
+
 constexpr int kBeforeGamma = 1, kBeforeBeta = 2, kAfterGamma = 4, kAfterBeta = 8;
 
 __device__ __forceinline__ char* row_at(const Mat& m, uint32_t row) { return m.data + (uint64_t)row * m.step; }

@@ -1,39 +1,12 @@
 // The residual connection's gradients, with the reductions of the gate's and the parameters' gradients.
-#include "moc_residual.h"
+#include "moc_residual_backward.h"
 
 namespace {
 
 // ---- backward -----------------------------------------------------------------------------------
 
-// The sums of a workgroup's kRows groups of T lanes, added in their order, to a row of floats.  By all threads.
-template <int T, int kRows, int CH>
-__device__ __forceinline__ void put_sums(const Runs<CH>& s, float* out, int cols, float* stage) {
-  const int lane = threadIdx.x % T, mine = threadIdx.x / T;
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int col = (c * T + lane) * kRun;
-    float a[kRun];
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) a[i] = s[c][i];
-    if constexpr (kRows > 1) {   // stage: [kRows][8][T]
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) stage[(mine * kRun + i) * T + lane] = a[i];
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < kRun; ++i) {
-        a[i] = 0.0f;
-#pragma unroll
-        for (int r = 0; r < kRows; ++r) a[i] += stage[(r * kRun + i) * T + lane];
-      }
-    }
-    if (mine == 0 && cols > col) store_run<MOC_F32>(out, col, cols - col, a);
-  }
-}
-
-// For anything.  S, B, D: what the stream and its gradients, the block's output, and the gradients of n and of the block hold.  The next
-// row is on its way where registers are left for it.
-template <int S, int B, int D, int T, int CH, bool AFTER>
+// For anything: what a matrix holds is asked at every run.  The next row is on its way where registers are left for it.
+template <int T, int CH, bool AFTER>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_any_kernel(ResidualArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
   using Sums = RowSums<T, 2>;
@@ -41,7 +14,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_any_kerne
   __shared__ float stage[kRows > 1 ? kRows * kRun * T : 1];
   Sums sums{room};
   const int lane = threadIdx.x % T, mine = kRows > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / T) : 0;
-  const bool whole = S != kAny || (g.cols >= kRun && !g.parts);   // which S says: see backward_shape
+  const bool whole = g.cols >= kRun && !g.parts;
   const float part = 1.0f / (float)g.cols;
   Runs<CH> gamma1, beta1, gate, gamma2;
   Runs<CH> sg1, sb1, sgate, sg2, sb2;
@@ -65,11 +38,11 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_any_kerne
     for (int c = 0; c < CH; ++c) {
       const int col = (c * T + lane) * kRun;
       if (g.before.on) {
-        wr[c] = load_run_of<S>(g.r, row, col, g.cols, whole);
-        wn[c] = load_run_of<D>(g.dn, row, col, g.cols, whole);
+        wr[c] = load_run_of<kAny>(g.r, row, col, g.cols, whole);
+        wn[c] = load_run_of<kAny>(g.dn, row, col, g.cols, whole);
       }
-      if (g.dr.data) wd[c] = load_run_of<S>(g.dr, row, col, g.cols, whole);
-      if (g.block.data) wb[c] = load_run_of<B>(g.block, row, col, g.cols, whole);
+      if (g.dr.data) wd[c] = load_run_of<kAny>(g.dr, row, col, g.cols, whole);
+      if (g.block.data) wb[c] = load_run_of<kAny>(g.block, row, col, g.cols, whole);
       if (g.own_gates) wg[c] = load_run_of<kTensor>(g.gate, row, col, g.cols, whole);
     }
     if (g.before.on) {
@@ -106,8 +79,8 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_any_kerne
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
           const int col = asked_again((c * T + lane) * kRun);
-          values_of_run<S>(g.r, r[c], col, g.cols, whole, h[c]);
-          values_of_run<D>(g.dn, n_[c], col, g.cols, whole, d[c]);
+          values_of_run<kAny>(g.r, r[c], col, g.cols, whole, h[c]);
+          values_of_run<kAny>(g.dn, n_[c], col, g.cols, whole, d[c]);
           before_run(h[c], d[c], mean2, rstd2, gamma2[c], sg2[c], sb2[c], m);   // beyond the row h meets zeros
         }
         sums(m);
@@ -127,18 +100,18 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_any_kerne
         const int col = asked_again((c * T + lane) * kRun), n = g.cols - col;
         if (g.dr.data) {
           float more[kRun];
-          values_of_run<S>(g.dr, s_[c], col, g.cols, whole, more);
+          values_of_run<kAny>(g.dr, s_[c], col, g.cols, whole, more);
           add_run(d[c], more);
         }
         if (g.dx.data) {
           float o[kRun];
 #pragma unroll
           for (int i = 0; i < kRun; ++i) o[i] = g.scale * d[c][i];
-          store_run_of<S>(g.dx, row, col, n, o);
+          store_run_of<kAny>(g.dx, row, col, n, o);
         }
         if (!g.dblock.data && !g.block.data) continue;
         if (g.block.data) {
-          values_of_run<B>(g.block, b[c], col, g.cols, whole, h[c]);
+          values_of_run<kAny>(g.block, b[c], col, g.cols, whole, h[c]);
         } else {
 #pragma unroll
           for (int i = 0; i < kRun; ++i) h[c][i] = 0.0f;
@@ -162,7 +135,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_any_kerne
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
           const int col = asked_again((c * T + lane) * kRun);
-          store_run_of<D>(g.dblock, row, col, g.cols - col, d[c]);
+          store_run_of<kAny>(g.dblock, row, col, g.cols - col, d[c]);
         }
       }
     }
@@ -184,161 +157,6 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_any_kerne
     out += g.cols;
   }
   if constexpr (AFTER) {
-    if (g.kinds & kAfterGamma) {
-      put_sums<T, kRows, CH>(sg1, out, g.cols, stage);
-      out += g.cols;
-    }
-    if (g.kinds & kAfterBeta) put_sums<T, kRows, CH>(sb1, out, g.cols, stage);
-  }
-}
-
-// Made for types: of a call with a norm before the next block, with dr and dblock, and gates of many rows.  MODE: kAlone, where
-// there is but a norm, without dr, kPlain, where the block's output is not looked at, kGated, or kNormed with a norm behind it
-// (and a gate, which may be ones).  Lanes beyond the row take no part but in the sums.
-constexpr int kAlone = 0, kPlain = 1, kGated = 2, kNormed = 3;
-
-template <int S, int B, int D, int T, int CH, int MODE>
-__global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(ResidualArgs g) {
-  constexpr int kRows = T < 256 ? 256 / T : 1;
-  constexpr bool kAhead = CH == 1 || T <= 512, kHold = kAhead;
-  using Sums = RowSums<T, 2>;
-  __shared__ float room[Sums::kRoom];
-  __shared__ float stage[kRows > 1 ? kRows * kRun * T : 1];
-  Sums sums{room};
-  const uint32_t lane = threadIdx.x % T, mine = kRows > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / T) : 0, cols = g.cols;
-  // a norm without a mean has 0 for it
-  const float part = 1.0f / (float)cols, part2 = g.before.layer ? part : 0.0f, part1 = g.after.layer ? part : 0.0f;
-  const float *const means2 = g.before.layer ? g.before.mean : g.before.rstd, *const means1 = g.after.layer ? g.after.mean : g.after.rstd;
-  const float layer2 = g.before.layer ? 1.0f : 0.0f, layer1 = g.after.layer ? 1.0f : 0.0f;
-  Runs<CH> gamma1, beta1, gate, gamma2;
-  Runs<CH> sg1, sb1, sgate, sg2, sb2;
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-#pragma unroll
-    for (int i = 0; i < kRun; ++i) sg1[c][i] = sb1[c][i] = sgate[c][i] = sg2[c][i] = sb2[c][i] = 0.0f;
-  const uint32_t from = g.chunks > 1 ? blockIdx.x / g.chunks : blockIdx.x * g.groups, last = min(from + (g.chunks > 1 ? 1 : g.groups), max(g.gates, 1u));
-  const uint32_t chunk = g.chunks > 1 ? blockIdx.x - from * g.chunks : 0;
-  Raw wr[CH], wn[CH], wd[CH], wb[CH];
-  float stats[4];
-  const auto load = [&](uint32_t row) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const uint32_t col = (c * T + lane) * kRun;
-      wr[c] = fetch<S>(g.r, row, col, cols);
-      wn[c] = fetch<D>(g.dn, row, col, cols);
-      if constexpr (MODE != kAlone) wd[c] = fetch<S>(g.dr, row, col, cols);
-      if constexpr (MODE > kPlain) wb[c] = fetch<B>(g.block, row, col, cols);
-    }
-    stats[0] = of_row(means2, row);
-    stats[1] = of_row(g.before.rstd, row);
-    if constexpr (MODE == kNormed) {
-      stats[2] = of_row(means1, row);
-      stats[3] = of_row(g.after.rstd, row);
-    }
-  };
-  for (uint32_t which = from; which < last; ++which) {
-    const uint32_t first = which * g.rows_per_gate + chunk * g.chunk_rows, end = min(first + g.chunk_rows, (which + 1) * g.rows_per_gate);
-    uint32_t row = first + mine;
-    if (kAhead && row < end) load(row);
-    if (kHold && which == from) {   // with the first row on its way
-      if constexpr (MODE == kNormed) {
-        hold_param<T, CH>(g.after.gamma, g.after.param_type, lane, cols, 1.0f, gamma1);
-        hold_param<T, CH>(g.after.beta, g.after.param_type, lane, cols, 0.0f, beta1);
-      }
-      hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, cols, 1.0f, gamma2);
-    }
-    if constexpr (MODE > kPlain && kHold) hold_gate<T, CH>(g, which, lane, gate);
-    for (; row < end; row += kRows) {   // groups of lanes that end earlier share no barrier
-      if (!kAhead) load(row);
-      Runs<CH> h, d;
-      Raw cr[CH], cn[CH], cd[CH], cb[CH];
-      const float mean2 = stats[0] * layer2, rstd2 = stats[1], mean1 = MODE == kNormed ? stats[2] * layer1 : 0.0f, rstd1 = MODE == kNormed ? stats[3] : 1.0f;
-      float m[2] = {0.0f, 0.0f};
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        cr[c] = wr[c];
-        cn[c] = wn[c];
-        if constexpr (MODE != kAlone) cd[c] = wd[c];
-        if constexpr (MODE > kPlain) cb[c] = wb[c];
-      }
-      if (kAhead) load(min(row + kRows, end - 1));   // behind the last row it once more
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const uint32_t col = (c * T + lane) * kRun;
-        if (col < cols && col + kRun > cols) {
-          settle_run<S>(cr[c], col, cols);
-          settle_run<D>(cn[c], col, cols);
-          if constexpr (MODE != kAlone) settle_run<S>(cd[c], col, cols);
-          if constexpr (MODE > kPlain) settle_run<B>(cb[c], col, cols);
-        }
-        if (col < cols) {
-          values_fetched<S>(g.r, cr[c], h[c]);
-          values_fetched<D>(g.dn, cn[c], d[c]);
-          float ga[kRun];   // where the row has ended h meets zeros
-          before_run(h[c], d[c], mean2, rstd2, param_of<kHold>(gamma2[c], g.before.gamma, g.before.param_type, (int)col, g.cols, 1.0f, ga), sg2[c], sb2[c], m);
-        }
-      }
-      sums(m);
-      const float a2 = m[0] * part2, b2 = m[1] * part;
-      m[0] = m[1] = 0.0f;
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const uint32_t col = (c * T + lane) * kRun;
-        if (col < cols) {
-          float v[kRun];
-          norm_gradient(d[c], h[c], rstd2, a2, b2);
-          if constexpr (MODE != kAlone) {
-            values_fetched<S>(g.dr, cd[c], v);
-            add_run(d[c], v);
-          }
-          if (g.dx.data) {
-#pragma unroll
-            for (int i = 0; i < kRun; ++i) v[i] = g.scale * d[c][i];
-            put<S>(g.dx, row, col, cols, v);
-          }
-          if constexpr (MODE > kPlain) {
-            if (col + kRun > cols) {
-#pragma unroll
-              for (uint32_t i = 0; i < kRun; ++i) d[c][i] = col + i < cols ? d[c][i] : 0.0f;
-            }
-            values_fetched<B>(g.block, cb[c], h[c]);
-            float ga[kRun], be[kRun], of[kRun];
-            gate_run<MODE == kNormed>(h[c], d[c], v, mean1, rstd1, param_of<kHold || MODE != kNormed>(gamma1[c], g.after.gamma, g.after.param_type, (int)col, g.cols, 1.0f, ga),
-                                      param_of<kHold || MODE != kNormed>(beta1[c], g.after.beta, g.after.param_type, (int)col, g.cols, 0.0f, be),
-                                      param_of<kHold>(gate[c], g.gates ? row_at(g.gate, which) : nullptr, g.gate.type, (int)col, g.cols, 1.0f, of), sg1[c], sb1[c], m);
-            add_run(sgate[c], v);
-          }
-        }
-      }
-      if constexpr (MODE == kNormed) sums(m);
-      const float a1 = m[0] * part1, b1 = m[1] * part;
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const uint32_t col = (c * T + lane) * kRun;
-        if (col < cols) {
-          if constexpr (MODE == kNormed) norm_gradient(d[c], h[c], rstd1, a1, b1);
-          put<D>(g.dblock, row, col, cols, d[c]);
-        }
-      }
-    }
-    if (g.want_gate) {
-      put_sums<T, kRows, CH>(sgate, g.gate_sums + (uint64_t)(which * g.chunks + chunk) * g.cols, g.cols, stage);
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < kRun; ++i) sgate[c][i] = 0.0f;
-    }
-  }
-  float* out = g.sums + (int64_t)blockIdx.x * __builtin_popcount(g.kinds) * g.cols;
-  if (g.kinds & kBeforeGamma) {
-    put_sums<T, kRows, CH>(sg2, out, g.cols, stage);
-    out += g.cols;
-  }
-  if (g.kinds & kBeforeBeta) {
-    put_sums<T, kRows, CH>(sb2, out, g.cols, stage);
-    out += g.cols;
-  }
-  if constexpr (MODE == kNormed) {
     if (g.kinds & kAfterGamma) {
       put_sums<T, kRows, CH>(sg1, out, g.cols, stage);
       out += g.cols;
@@ -406,39 +224,16 @@ __global__ __launch_bounds__(256) void zero_kernel(float* out, int64_t count) {
 
 // ---- dispatch -----------------------------------------------------------------------------------
 
-using Kernel = void (*)(ResidualArgs);
-struct Shape {
-  Kernel kern;
-  int threads, rows;   // of a workgroup
-};
-// T and CH by the columns alone: moc_residual_backward_work does not know the rest.
-template <int S, int B, int D, int T, int CH, int MODE>
-Kernel backward_kernel() {
-  if constexpr (S == kAny) return residual_backward_any_kernel<S, B, D, T, CH, MODE == kNormed>;
-  else return residual_backward_kernel<S, B, D, T, CH, MODE>;
+template <bool AFTER>
+ResidualShape any_shape(int64_t cols) {
+  if (cols <= 512) return {residual_backward_any_kernel<64, 1, AFTER>, 256, 4};
+  if (cols <= 1024) return {residual_backward_any_kernel<64, 2, AFTER>, 256, 4};
+  if (cols <= 2048) return {residual_backward_any_kernel<256, 1, AFTER>, 256, 1};
+  if (cols <= 4096) return {residual_backward_any_kernel<512, 1, AFTER>, 512, 1};
+  if (cols <= 8192) return {residual_backward_any_kernel<512, 2, AFTER>, 512, 1};
+  return {residual_backward_any_kernel<1024, 2, AFTER>, 1024, 1};
 }
-template <int S, int B, int D, int MODE>
-Shape backward_shape(int64_t cols) {
-  if (cols <= 512) return {backward_kernel<S, B, D, 64, 1, MODE>(), 256, 4};
-  if (cols <= 1024) return {backward_kernel<S, B, D, 64, 2, MODE>(), 256, 4};
-  if (cols <= 2048) return {backward_kernel<S, B, D, 256, 1, MODE>(), 256, 1};
-  if (cols <= 4096) return {backward_kernel<S, B, D, 512, 1, MODE>(), 512, 1};
-  if (cols <= 8192) return {backward_kernel<S, B, D, 512, 2, MODE>(), 512, 1};
-  return {backward_kernel<S, B, D, 1024, 2, MODE>(), 1024, 1};
-}
-template <int S, int B, int D>
-Shape backward_shape(int mode, int64_t cols) {
-  return mode == kAlone ? backward_shape<S, D, D, kAlone>(cols) : mode == kPlain ? backward_shape<S, D, D, kPlain>(cols) : mode == kGated ? backward_shape<S, B, D, kGated>(cols) : backward_shape<S, B, D, kNormed>(cols);
-}
-Shape any_shape(bool after, int64_t cols) { return after ? backward_shape<kAny, kAny, kAny, kNormed>(cols) : backward_shape<kAny, kAny, kAny, kPlain>(cols); }
-template <int D>
-Shape backward_shape(int s, int b, int mode, int64_t cols) {
-  if (s == D && b == D) return backward_shape<D, D, D>(mode, cols);
-  if (s == D && b == kKept) return backward_shape<D, kKept, D>(mode, cols);
-  if (s == MOC_F32 && b == D) return backward_shape<MOC_F32, D, D>(mode, cols);
-  if (s == MOC_F32 && b == kKept) return backward_shape<MOC_F32, kKept, D>(mode, cols);
-  return any_shape(mode == kNormed, cols);
-}
+ResidualShape any_shape(bool after, int64_t cols) { return after ? any_shape<true>(cols) : any_shape<false>(cols); }
 
 constexpr int kFewWaves = 8, kManyWaves = 16;   // 256 and 128 registers a lane
 
@@ -448,7 +243,7 @@ struct Cut {
   bool own;
 };
 // `waves`: of a compute unit, by the kernels' registers.
-Cut cut_of(const Shape& s, int64_t rows, int64_t gates, int units, int waves) {
+Cut cut_of(const ResidualShape& s, int64_t rows, int64_t gates, int units, int waves) {
   Cut c = {};
   c.own = gates > 1 && gates == rows;
   const int64_t apart = c.own || gates < 1 ? 1 : gates, each = rows / apart;
@@ -521,12 +316,14 @@ int moc_residual_backward(int64_t rows, int64_t cols, const moc_matrix* dr, cons
   ResidualArgs g = {};
   g.parts = lies_over(dx, {dr, dn, r, block, gate}) || lies_over(dblock, {dr, dn, r, block, gate});
   // kernels made for some types, where all matrices are of them and a row's last run may be loaded whole
-  const bool ragged = cols < kRun || (g.parts && cols % kRun != 0), usual = last && dblock && !(gates > 1 && gates == rows) && !ragged;
+  const bool ragged = cols < kRun || (g.parts && cols % kRun != 0), usual = last && dblock && !ragged, own = gates > 1 && gates == rows;
   const int kd = agreed({dn, dblock}, kAny), ks = agreed({dr, r, dx}, kAny), kb = needed ? kind_of(block->type) : kd, mode = first ? kNormed : needed || gate ? kGated : dr ? kPlain : kAlone;
-  const Shape s = !usual || (mode > kPlain && !(needed && dr)) ? any_shape(first, cols)
-                  : kd == MOC_BF16                      ? backward_shape<MOC_BF16>(ks, kb, mode, cols)
-                  : kd == MOC_F16                       ? backward_shape<MOC_F16>(ks, kb, mode, cols)
-                                                        : any_shape(first, cols);
+  ResidualShape s = {};
+  if (usual && (mode <= kPlain || (needed && dr))) {
+    if (kd == MOC_BF16) s = moc_residual_backward_bf16(ks, kb, mode, own, cols);
+    if (kd == MOC_F16) s = moc_residual_backward_f16(ks, kb, mode, own, cols);
+  }
+  if (!s.kern) s = any_shape(first, cols);
   const Cut c = cut_of(s, rows, gates, units, mode <= kPlain && cols <= 4096 ? kManyWaves : kFewWaves);
   const bool gate_parts = d.gate && !c.own && c.chunks > 1;
   const int64_t need = sums_bytes(c, kinds, gates, d.gate != nullptr, cols);

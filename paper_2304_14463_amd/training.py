@@ -242,7 +242,7 @@ def moc_residual_forward(x, block, gate=None, scale=1.0, after=None, before=None
     """The stream between two blocks, r = scale * x + gate * after(block), and the norm before the next one, n = before(r): `after` and
     `before` are Norms or None, `gate` [cols] or [gates, cols] for rows / gates rows each, `block` a tensor or a Checkpoint, `x` may be
     None.  Returns (r, n, (mean, rstd) of each norm, n in 8 bits if `keep` names a format or is a Checkpoint to write to); None for
-    what is not there.  `dtype`: n's, default the block's.  `out` may be x or block, and so may `out_norm`."""
+    what is not there.  `dtype`: n's, default the block's, or x's if that is a Checkpoint; r is of x's, or else the block's.  `out` may be x or block, and so may `out_norm`."""
     code, r, n, after, before, kept = _call("residual_forward", stream, x, block, gate, scale, after, before, keep, dtype, want_stream, out, out_norm)
     moc._check(code, "moc_residual_forward")
     return Residual(r, n, after, before, kept)

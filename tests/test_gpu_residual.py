@@ -143,6 +143,9 @@ KINDS = [dict(block="bf16", stream="bf16", after="rms", before="layer", gates=1)
          dict(block="bf16", stream="bf16", held="e4m3", after=None, before="layer", gates=2, lead=3, pad=1),
          dict(block="fp32", stream="fp32", after="rms", before="rms", gates=6, x=False),
          dict(block="fp32", stream="bf16", after="layer", before=None, gates=1),
+         dict(block="bf16", stream="fp32", after=None, before="rms", gates=6),
+         dict(block="bf16", stream="fp32", held="int8", after="rms", before="layer", gates=6, lead=1, pad=7),
+         dict(block="bf16", stream="bf16", after=None, before="layer", gates=0),
          dict(block="bf16", stream="bf16", after=None, before=None, gates=2, scale=1.0, ptype=torch.float16, lead=1, pad=1)]
 IDS = ["-".join(str(v) for v in k.values() if not isinstance(v, torch.dtype)) for k in KINDS]
 
@@ -185,7 +188,7 @@ def test_forward(tr, cols, kind):
     if case.before:
         assert got.n is on.inner and on.intact() and fc.intact() and fs.intact()
     check_forward(case, got, want, fmt)
-    again = case.forward()
+    again = case.forward(dtype=case.block_type)   # a Checkpoint's own default is x's type
     assert torch.equal(again.r, got.r) and again.kept is None and (not case.before or torch.equal(again.n, got.n))
     if case.before:
         alone = case.forward(want_stream=False, dtype=torch.float32)
@@ -218,11 +221,11 @@ def check_backward(tr, rows, cols, kind):
     f = case.forward(dtype=case.block_type)
     g = case.g
     stats = dict(after=f.after, before=f.before)
-    for held in ("tensor", "e4m3"):
+    for held, whole in (("tensor", True), ("tensor", False), ("e4m3", False)):
         r = f.r if held == "tensor" else tr.moc_checkpoint_write(f.r, held)
         r_near = Near(f.r.cpu()) if held == "tensor" else Near(ref.values(r.codes, r.scales, held))
         stream_type = f.r.dtype
-        dr = normal(g, rows, cols, by=0.1).to(stream_type) if held == "tensor" or not case.before else None
+        dr = normal(g, rows, cols, by=0.1).to(stream_type) if whole or not case.before else None
         dn = normal(g, rows, cols, by=0.3).to(case.block_type) if case.before else None
         want = case.gradients(r_near, stats, Near(dr) if dr is not None else None, Near(dn) if dn is not None else None)
         ox, ob = Framed(rows, cols, stream_type, case.lead, case.pad), Framed(rows, cols, case.block_type, case.lead, case.pad)
@@ -236,7 +239,7 @@ def check_backward(tr, rows, cols, kind):
                 check(value, want[name])
         again = tr.moc_residual_backward(dr, dn, r, case.block, want_x=False, want_params=False, **args)
         assert torch.equal(again.dblock, got.dblock) and all(v is None for k, v in again._asdict().items() if k != "dblock")
-        if held == "tensor" and case.held == "tensor":
+        if whole and case.held == "tensor":
             # over the operands, where types allow it
             a, b = case.framed(dr), case.framed(case.block)
             over = tr.moc_residual_backward(a, dn, r, b, out_x=a, out_block=b, **args)
