@@ -1,7 +1,8 @@
 // AdamW over many tensors at once, with moments in 32 bits or in 8, and what moments stand for.
 //
 // One pass over a tensor's values, bound by memory: 28 bytes a value with moments and gradients in 32 bits, 14 to 16 with
-// moments in 8.  A launch takes up to kTensors tensors, whose descriptors travel in its arguments: nothing is copied to
+// moments in 8: 150 M parameters in 32 bits with copies 834 us (5.4 TB/s), 537 M with moments in 8 bits 1660 us (5.2), their reading
+// back 626.  A launch takes up to kTensors tensors, whose descriptors travel in its arguments: nothing is copied to
 // the device first, and a captured launch keeps them.
 #include <type_traits>
 

@@ -5,8 +5,12 @@
 // f = 2^d, and so do lanes that are joined.  Then log sum exp = scale m + ln s and the entropy ln s - ln 2 w / s.
 // The alternatives: the wanted number of lanes have a largest logit that is not below some value, so nothing below it is among
 // them; the few lanes whose largest is not below it have their columns read again, what is not below it goes to LDS, and its
-// places in the order are counted.  Few rows are cut into parts, whose sums and alternatives a second kernel joins.
-// Backward: a pass over the logits and their gradient.
+// places in the order are counted.  Few rows are cut into parts, whose sums and alternatives a second kernel joins.  A
+// workgroup a row of 8192 x 131072 bf16: 359 us, 6.0 TB/s, the vector ALU busy beside it (ten instructions a logit, exp2 at a
+// quarter of the rate); 4999 x 32003 fp16 with five alternatives 69 us, 64 of them 96 (391 with lists that waves hold); one row
+// of 131072 with twenty 12 us (51 by one workgroup).
+// Backward: a pass over the logits and their gradient, 8192 columns a workgroup, runs at aligned addresses: 8192 x 131072 bf16
+// 749 us, 5.7 TB/s (843 where each load had a branch); four float32 values a lane (1247 x 32003 65 us, 83 with eight).
 #include <algorithm>
 
 #include "moc_rows.h"
@@ -547,7 +551,7 @@ __global__ __launch_bounds__(kThreads) void logprob_backward_kernel(LogprobArgs 
     }
   } else {
     // Runs begin where the output is 16 bytes apart from an aligned address: rows of an odd size do not (4999 x 32003 fp16
-    // 166 us at 2-byte addresses).  The first run of a row may begin before it.
+    // 166 us at 2-byte addresses, 124 so).  The first run of a row may begin before it.
     const int shift = g.out_type == TYPE ? before_row<TYPE>(out) : 0;
     Raw w[kTurns];
 #pragma unroll
