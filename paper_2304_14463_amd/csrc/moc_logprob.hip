@@ -6,7 +6,7 @@
 // The alternatives: the wanted number of lanes have a largest logit that is not below some value, so nothing below it is among
 // them; the few lanes whose largest is not below it have their columns read again, what is not below it goes to LDS, and its
 // places in the order are counted.  Few rows are cut into parts, whose sums and alternatives a second kernel joins.  A
-// workgroup a row of 8192 x 131072 bf16: 359 us, 6.0 TB/s, the vector ALU busy beside it (ten instructions a logit, exp2 at a
+// workgroup a row of 8192 x 131072 bf16: 359 us, 6.0 TB/s, the vector ALU busy beside it (eight instructions a logit, exp2 at a
 // quarter of the rate); 4999 x 32003 fp16 with five alternatives 69 us, 64 of them 96 (391 with lists that waves hold); one row
 // of 131072 with twenty 12 us (51 by one workgroup).
 // Backward: a pass over the logits and their gradient, 8192 columns a workgroup, runs at aligned addresses: 8192 x 131072 bf16
@@ -173,7 +173,7 @@ constexpr int kRoom = 1024;
 struct TopRoom {
   float largest[kThreads];
   uint16_t lanes[kThreads];
-  uint32_t reach, found;
+  uint32_t reach, found, again, left;   // one for each step: a wave may read what it went by after another went on
   float least;
   Key keys[kRoom], best[kMostTop];
 };
@@ -195,7 +195,8 @@ __device__ __forceinline__ void find_least(TopRoom& r, int top) {
   }
 }
 
-// What is above `least`, or not below it (`with`), of the columns of lanes that reach it, to r.keys as far as it goes.
+// What is above `least`, or not below it (`with`), of the columns of lanes that reach it, to r.keys; no further than there is room
+// for.  4999 x 32000 fp16 with equal logits: 229 us, 578 where each logit asked for its own place and all were counted.
 template <int TYPE>
 __device__ __forceinline__ void gather(const void* row, const Columns& c, float least, bool with, TopRoom& r) {
   const uint32_t lanes = r.reach, total = lanes * (uint32_t)((c.hi - c.first + kStep - 1) / kStep);
@@ -206,75 +207,110 @@ __device__ __forceinline__ void gather(const void* row, const Columns& c, float 
     load_columns<TYPE>(row, c, col, bits_float(0x7FC00000u), v);
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
-      if (!(with ? v[j] >= least : v[j] > least)) continue;
-      const uint32_t at = atomicAdd(&r.found, 1u);
-      if (at < kRoom) r.keys[at] = key_of(v[j], (uint32_t)(col + j));
+      const uint64_t some = __builtin_amdgcn_ballot_w64(with ? v[j] >= least : v[j] > least);
+      if (some == 0) continue;
+      // one lane asks for all
+      const int first = __builtin_ctzll(some);
+      uint32_t begin = 0;
+      if ((int)(threadIdx.x % kWave) == first) begin = atomicAdd(&r.found, (uint32_t)__builtin_popcountll(some));
+      begin = (uint32_t)__builtin_amdgcn_readlane((int)begin, first);
+      const uint32_t at = begin + __builtin_amdgcn_mbcnt_hi((uint32_t)(some >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)some, 0));
+      if (at < kRoom && (some >> (threadIdx.x % kWave) & 1)) r.keys[at] = key_of(v[j], (uint32_t)(col + j));
+      if (begin > kRoom) return;   // more than there is room for, in any case
     }
   }
 }
 
-// More logits than there is room for: those above `least`, and of those that equal it the first ones, as many as are missing.
-// Where even those above it are too many, one after the other by a pass each.  By all threads, as all of these.
+// Of n keys in LDS those that can be among the first `top`, in their place; what is left of them.  By one wave: a bound by the
+// logits' bits, one after the other, and where many are equal one by their places.
+constexpr int kFewKeys = 2 * kMostTop;
+__device__ __forceinline__ uint32_t cut_keys(Key* keys, uint32_t n, int top) {
+  constexpr int kEach = kRoom / kWave;
+  const uint32_t lane = threadIdx.x % kWave;
+  uint32_t upper[kEach], lower[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const Key k = i * kWave + lane < n ? keys[i * kWave + lane] : 0;
+    upper[i] = (uint32_t)(k >> 32);
+    lower[i] = (uint32_t)k;
+  }
+  uint32_t t = 0, at = 0;
+#pragma unroll 1
+  for (uint32_t bit = 1u << 31; bit != 0; bit >>= 1) {
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(upper[i] >= (t | bit)));
+    if (count >= top) t |= bit;
+  }
+  int reach = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) reach += __builtin_popcountll(__builtin_amdgcn_ballot_w64(upper[i] >= t));
+  if (reach > kFewKeys) {
+#pragma unroll 1
+    for (uint32_t bit = 1u << 31; bit != 0; bit >>= 1) {
+      int count = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(upper[i] > t || (upper[i] == t && lower[i] >= (at | bit))));
+      if (count >= top) at |= bit;
+    }
+  }
+  uint32_t left = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const bool stays = upper[i] > t || (upper[i] == t && lower[i] >= at);
+    const uint64_t some = __builtin_amdgcn_ballot_w64(stays);
+    const uint32_t place = left + __builtin_amdgcn_mbcnt_hi((uint32_t)(some >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)some, 0));
+    if (stays) keys[place] = (Key)upper[i] << 32 | lower[i];
+    left += (uint32_t)__builtin_popcountll(some);
+  }
+  return left;
+}
+
+// More logits than there is room for: the last of the best among those that are there is a better bound.  What is above it, and of
+// those that equal it the first ones by column, as many as are missing; or all over again from there, as every key there is
+// above the bound then.  By all threads, as all of these.
 template <int TYPE>
-__device__ __attribute__((noinline)) void gather_again(const void* row, Columns c, float least, int top, TopRoom* room) {
+__device__ __attribute__((noinline)) uint32_t gather_again(const void* row, Columns c, int top, TopRoom* room) {
   TopRoom& r = *room;
-  const int from = c.lo, to = c.hi;
-  if (threadIdx.x == 0) r.found = 0;
-  __syncthreads();
-  gather<TYPE>(row, c, least, false, r);
-  __syncthreads();
-  const uint32_t above = r.found;
-  if (above <= kRoom - kMostTop) {
+  for (uint32_t above = kRoom;;) {
+    __syncthreads();
+    if (threadIdx.x < kWave) {
+      const uint32_t left = cut_keys(r.keys, above, top);
+      float least = kInf;
+      for (uint32_t i = threadIdx.x; i < left; i += kWave) least = fminf(least, logit_of(r.keys[i]));
+      least = -wave_largest(-least);
+      if (threadIdx.x == 0) {
+        r.least = least;
+        r.found = 0;
+      }
+    }
+    __syncthreads();
+    const float least = r.least;
+    gather<TYPE>(row, c, least, false, r);
+    __syncthreads();
+    above = min(r.found, (uint32_t)kRoom);
+    if (above > kRoom - kMostTop) continue;   // at least `top` of what is above the bound: it rises
     if (threadIdx.x < kWave) {
       uint32_t have = above;
-      for (int at = from; at < to && have < (uint32_t)top; at += kWave * kRun) {
-        const int col = at + (int)threadIdx.x * kRun, n = to - col;
+      for (int at = c.lo; at < c.hi && have < (uint32_t)top; at += kWave * kRun) {
+        const int col = at + (int)threadIdx.x * kRun;
         float v[kRun];
-        load_run<TYPE>(row, col, n, v);
         uint32_t equal = 0;
+        if (col < c.hi) {
+          load_columns<TYPE>(row, c, col, bits_float(0x7FC00000u), v);
 #pragma unroll
-        for (int j = 0; j < kRun; ++j) equal |= j < n && v[j] == least ? 1u << j : 0;
+          for (int j = 0; j < kRun; ++j) equal |= v[j] == least ? 1u << j : 0;
+        }
         const int mine = __builtin_popcount(equal), up_to = scan_sum(mine);
         uint32_t place = have + (uint32_t)(up_to - mine);
         for (; equal != 0 && place < (uint32_t)top; equal &= equal - 1, ++place) r.keys[place] = key_of(least, (uint32_t)(col + __builtin_ctz(equal)));
         have += (uint32_t)__builtin_amdgcn_readlane(up_to, kWave - 1);
       }
-      if (threadIdx.x == 0) r.found = min(max((uint32_t)top, above), have);
+      if (threadIdx.x == 0) r.again = min(max((uint32_t)top, above), have);
     }
     __syncthreads();
-    return;
+    return r.again;
   }
-  Key before = ~(Key)0;
-  int there = 0;
-  for (; there < top; ++there) {
-    Key most = 0;
-    for (int col = from + (int)threadIdx.x * kRun; col < to; col += kThreads * kRun) {
-      const int n = to - col;
-      float v[kRun];
-      load_run<TYPE>(row, col, n, v);
-#pragma unroll
-      for (int j = 0; j < kRun; ++j) {
-        if (j >= n || v[j] != v[j]) continue;
-        const Key k = key_of(v[j], (uint32_t)(col + j));
-        most = k < before && k > most ? k : most;
-      }
-    }
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) {
-      const Key other = __shfl_xor((unsigned long long)most, d);
-      most = other > most ? other : most;
-    }
-    __syncthreads();   // what was read of best below
-    if (threadIdx.x % kWave == 0) r.best[threadIdx.x / kWave] = most;
-    __syncthreads();
-    for (int i = 0; i < kWaves; ++i) most = r.best[i] > most ? r.best[i] : most;
-    if (most == 0) break;
-    before = most;
-    if (threadIdx.x == 0) r.keys[there] = most;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) r.found = (uint32_t)there;
-  __syncthreads();
 }
 
 // The first `top` of n keys in LDS, in falling order, to best; 0 behind the last.  Ends with a barrier.
@@ -303,8 +339,17 @@ __device__ __forceinline__ void select_top(const void* row, const Columns& c, fl
   __syncthreads();
   gather<TYPE>(row, c, least, true, r);
   __syncthreads();
-  if (r.found > kRoom) gather_again<TYPE>(row, c, least, top, &r);
-  order(r.keys, r.found, top, r.best);
+  uint32_t found = r.found;
+  if (found > kRoom) found = gather_again<TYPE>(row, c, top, &r);
+  if (found > kFewKeys) {   // ranks take time by the square of their number: few lanes with many candidates 318 us, 762 without
+    if (threadIdx.x < kWave) {
+      const uint32_t left = cut_keys(r.keys, found, top);
+      if (threadIdx.x == 0) r.left = left;
+    }
+    __syncthreads();
+    found = r.left;
+  }
+  order(r.keys, found, top, r.best);
 }
 
 // ---- forward ------------------------------------------------------------------------------------

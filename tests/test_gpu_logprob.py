@@ -344,3 +344,32 @@ def test_every_call_asks_for_the_device_of_its_tensors(tr, monkeypatch):
         for call in (lambda: tr.moc_logprob_forward(x), lambda: tr.moc_logprob_backward(x, v)):
             with pytest.raises(ValueError, match="cuda:0.*cuda:1"):
                 call()
+
+
+@pytest.mark.parametrize("rows", [1, 600])
+@pytest.mark.parametrize("vocab", [4999, 32003, 131072])
+def test_alternatives_among_many_candidates(tr, rows, vocab):
+    """Rows that rise or fall by single float32 steps, so that whatever was gathered first is not the best; and 1 .. 1025 distinct or
+    equal logits above the others, in order or not, in every place or in few lanes, with more that equal the last."""
+    g = gen(vocab)
+    steps = 1.0 + torch.arange(vocab) * 2.0 ** -23
+    cases = [steps, steps.flip(0), -steps, steps[torch.randperm(vocab, generator=g)], steps.half().float(), torch.full((vocab,), -2.5)]
+    for many in (1, 63, 64, 65, 127, 128, 129, 512, 959, 960, 961, 1023, 1024, 1025):
+        for equal in (True, False):
+            for at in (torch.arange(many) + (vocab - many) // 2, torch.randperm(vocab, generator=g)[:many]):
+                x = torch.zeros(vocab)
+                x[at] = 3.0 if equal else 3.0 + torch.randperm(many, generator=g) * 2.0 ** -20
+                cases.append(x)
+        x = torch.where(torch.arange(vocab) % 64 < 8, 1.0, -math.inf)
+        x[torch.randperm(vocab, generator=g)[:many]] = 2.0
+        cases.append(x)
+    x = torch.stack(cases)
+    tokens = torch.zeros(len(x), dtype=torch.int64)
+    for top in (1, 2, 20, 64):
+        want = definition(x.double(), tokens, 1.0, top)
+        calls = x.cuda().repeat(-(-rows // len(x)), 1) if rows > 1 else x.cuda()
+        got = [tr.moc_logprob_forward(calls, top=top)] if rows > 1 else [tr.moc_logprob_forward(calls[i:i + 1], top=top) for i in range(len(x))]
+        tops = torch.cat([f.top_tokens for f in got]).cpu()
+        assert torch.equal(tops, want["ids"].repeat(len(tops) // len(x), 1))
+        for f in got if rows > 1 else []:
+            check_forward(type(f)(None, *(None if t is None else t[:len(x)] for t in f[1:])), want, vocab, 1.0)
