@@ -491,7 +491,8 @@ Vector floats_or_none(PyObject* p, int64_t n, const char* what, const at::Tensor
 
 void apart(const Held& out, const char* name, const Vector& in, const char* what) {
   if (!out.there || !in.data || in.x.numel() == 0) return;
-  if (shared(out.span(), Span{reinterpret_cast<uintptr_t>(in.data), 1, (int64_t)in.x.nbytes(), 1})) bad(name, std::string("shares memory with ") + what);
+  const Span of{reinterpret_cast<uintptr_t>(in.data), 1, (int64_t)in.x.nbytes(), 1};
+  if (shared(out.span(), of) || shared(out.scale_span(), of)) bad(name, std::string("shares memory with ") + what);
 }
 
 PyObject* none() {
@@ -615,6 +616,8 @@ PyObject* residual_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   }
   apart(hn, "out_norm", hr, "out");
   for (const Held* h : {&x, &b, &gate, &hr, &hn}) apart(hk, "keep", *h, "another argument");
+  apart_from_norm(hk, "keep", after);
+  apart_from_norm(hk, "keep", before);
   room_for_statistics(after, b.rows, b.values);
   room_for_statistics(before, b.rows, b.values);
   void* const stream = stream_for(b.values);
@@ -774,7 +777,9 @@ struct Items {
     count = PySequence_Fast_GET_SIZE(seq.get());
     if (wanted >= 0 && count != wanted) bad(what, std::to_string(wanted) + " items expected, got " + std::to_string(count));
   }
-  PyObject* operator[](int64_t i) const { return PySequence_Fast_GET_ITEM(seq.get(), i); }
+  // as they are in hand: what the caller gave may be an iterator
+  PyObject* items() const { return const_cast<PyObject*>(seq.get()); }
+  PyObject* operator[](int64_t i) const { return PySequence_Fast_GET_ITEM(items(), i); }
 };
 
 std::string item(const char* what, int64_t i) { return std::string(what) + "[" + std::to_string(i) + "]"; }
@@ -857,7 +862,7 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const Items params(a[0], "params"), grads(a[1], "grads", params.count), moments(a[2], "moments", params.count);
   const int64_t tensors = params.count;
   const bool copied = a[3] != Py_None, same_decay = PyFloat_Check(a[4]) || PyLong_Check(a[4]);
-  const Items copies(copied ? a[3] : a[0], "copies", tensors), decay(same_decay ? a[0] : a[4], "weight_decay", tensors);
+  const Items copies(copied ? a[3] : params.items(), "copies", tensors), decay(same_decay ? params.items() : a[4], "weight_decay", tensors);
   Many many;
   std::vector<moc_adamw_tensor> list((size_t)tensors);
   for (int64_t i = 0; i < tensors; ++i) {
@@ -913,7 +918,7 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
 PyObject* moments_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
   HANDLE_TH_ERRORS
   arguments(count, 3, "moments_read");
-  const Items moments(a[0], "moments"), out(a[2] == Py_None ? a[0] : a[2], "out", moments.count);
+  const Items moments(a[0], "moments"), out(a[2] == Py_None ? moments.items() : a[2], "out", moments.count);
   Many many;
   std::vector<moc_moments_tensor> list((size_t)moments.count);
   THPObjectPtr results(PyList_New(moments.count));

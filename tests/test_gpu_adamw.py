@@ -314,3 +314,17 @@ def test_another_stream_and_device(tr, monkeypatch):
         for call in (lambda: tr.moc_adamw_step([p], [g], [mo], 0.5, 1), lambda: tr.moc_moments_read([mo])):
             with pytest.raises(ValueError, match="cuda:0.*cuda:1"):
                 call()
+
+
+def test_lists_may_be_iterators(tr):
+    """What an optimizer is given: parameters that can be gone over once."""
+    shapes = [(5, 70), (33,), (1,)]
+    params, grads = [torch.ones(s, device="cuda") for s in shapes], [torch.full(s, 0.5, device="cuda") for s in shapes]
+    moments = [tr.zero_moments(p, 32) for p in params]
+    want = [p.clone() for p in params]
+    kept = [tr.zero_moments(p, 32) for p in params]
+    tr.moc_adamw_step(want, grads, kept, 0.1, 1)
+    tr.moc_adamw_step(iter(params), iter(grads), iter(moments), 0.1, 1)
+    assert all(torch.equal(a, b) for a, b in zip(params, want)) and bool((params[0] != 1).all())
+    read = tr.moc_moments_read(iter(moments))
+    assert len(read) == 3 and all(torch.equal(m, k.m) and torch.equal(v, k.v) for (m, v), k in zip(read, kept))

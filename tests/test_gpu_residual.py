@@ -415,3 +415,14 @@ def test_every_call_asks_for_the_device_of_its_tensors(tr, monkeypatch):
         for call in (lambda: tr.moc_residual_forward(a, a.clone()), lambda: tr.moc_residual_backward(a, a.clone(), f.r, before=tr.Norm("rms"), before_stats=f.before)):
             with pytest.raises(ValueError, match="cuda:0.*cuda:1"):
                 call()
+
+
+def test_a_checkpoint_to_write_to_is_apart_from_the_norms(tr):
+    room = torch.zeros(4096, dtype=torch.uint8, device="cuda")
+    keep = tr.Checkpoint(room[:512].view(8, 64), torch.empty((8, 2), dtype=torch.uint8, device="cuda"), "int8")
+    scales = tr.Checkpoint(torch.empty((8, 64), dtype=torch.uint8, device="cuda"), room[:16].view(8, 2), "int8")
+    gamma, b = room[256:512].view(torch.float32), torch.ones(8, 64, device="cuda")
+    for after, before, kept in ((tr.Norm("rms", gamma), tr.Norm("rms"), keep), (None, tr.Norm("layer", None, gamma), keep), (None, tr.Norm("rms", room[:256].view(torch.float32)), scales)):
+        with pytest.raises(ValueError):
+            tr.moc_residual_forward(None, b, after=after, before=before, keep=kept)
+    assert not room.any()
