@@ -167,15 +167,61 @@ __device__ __forceinline__ float logit_of(Key k) {
 }
 __device__ __forceinline__ uint32_t place_of(Key k) { return ~(uint32_t)k; }
 
+// A number that `top` keys or more are not below, EACH of them a thread: the last of the best, or one with as many of its upper
+// bits as leave few keys.  Its bits one after the other, down to `lowest`.  By all threads.
+constexpr int kFewKeys = 2 * kMostTop;
+struct CutRoom {
+  uint32_t counts[2][kWaves], left;
+};
+template <int EACH>
+__device__ __forceinline__ Key bound_of(const Key (&k)[EACH], int top, int lowest, CutRoom& r) {
+  Key t = 0;
+#pragma unroll 1
+  for (int bit = 63, half = 0; bit >= lowest; --bit, half ^= 1) {
+    const Key next = t | (Key)1 << bit;
+    int count = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[i] >= next));
+    if (threadIdx.x % kWave == 0) r.counts[half][threadIdx.x / kWave] = (uint32_t)count;
+    __syncthreads();
+    count = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) count += (int)r.counts[half][i];
+    if (count < top) continue;
+    t = next;
+    if (count <= kFewKeys) break;
+  }
+  return t;
+}
+template <int EACH>
+__device__ __forceinline__ void keys_of(const Key* keys, uint32_t n, Key (&k)[EACH]) {
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) k[i] = i * kThreads + threadIdx.x < n ? keys[i * kThreads + threadIdx.x] : 0;
+}
+// Of n keys in LDS, more than a few, those that can be among the first `top`, in their place; how many those are, in all threads.
+template <int EACH>
+__device__ __forceinline__ uint32_t cut_keys(Key* keys, uint32_t n, int top, CutRoom& r) {
+  Key k[EACH];
+  keys_of(keys, n, k);
+  if (threadIdx.x == 0) r.left = 0;
+  const Key least = bound_of(k, top, 0, r);
+#pragma unroll
+  for (int i = 0; i < EACH; ++i)
+    if (k[i] >= least) keys[atomicAdd(&r.left, 1u)] = k[i];
+  __syncthreads();
+  return r.left;
+}
+
 // A logit that at least `top` of the lanes reach with their largest, in all threads: the largest number of 16 bits that as many
 // of the upper halves of their orders are not below.
 constexpr int kRoom = 1024;
 struct TopRoom {
   float largest[kThreads];
   uint16_t lanes[kThreads];
-  uint32_t reach, found, again, left;   // one for each step: a wave may read what it went by after another went on
+  uint32_t reach, found, again;   // one for each step: a wave may read what it went by after another went on
   float least;
   Key keys[kRoom], best[kMostTop];
+  CutRoom cut;
 };
 __device__ __forceinline__ void find_least(TopRoom& r, int top) {
   if (threadIdx.x < kWave) {
@@ -196,7 +242,7 @@ __device__ __forceinline__ void find_least(TopRoom& r, int top) {
 }
 
 // What is above `least`, or not below it (`with`), of the columns of lanes that reach it, to r.keys; no further than there is room
-// for.  4999 x 32000 fp16 with equal logits: 229 us, 578 where each logit asked for its own place and all were counted.
+// for.  4999 x 32000 fp16 with equal logits: 170 us, 578 where each logit asked for its own place and all were counted.
 template <int TYPE>
 __device__ __forceinline__ void gather(const void* row, const Columns& c, float least, bool with, TopRoom& r) {
   const uint32_t lanes = r.reach, total = lanes * (uint32_t)((c.hi - c.first + kStep - 1) / kStep);
@@ -221,52 +267,7 @@ __device__ __forceinline__ void gather(const void* row, const Columns& c, float 
   }
 }
 
-// Of n keys in LDS those that can be among the first `top`, in their place; what is left of them.  By one wave: a bound by the
-// logits' bits, one after the other, and where many are equal one by their places.
-constexpr int kFewKeys = 2 * kMostTop;
-__device__ __forceinline__ uint32_t cut_keys(Key* keys, uint32_t n, int top) {
-  constexpr int kEach = kRoom / kWave;
-  const uint32_t lane = threadIdx.x % kWave;
-  uint32_t upper[kEach], lower[kEach];
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const Key k = i * kWave + lane < n ? keys[i * kWave + lane] : 0;
-    upper[i] = (uint32_t)(k >> 32);
-    lower[i] = (uint32_t)k;
-  }
-  uint32_t t = 0, at = 0;
-#pragma unroll 1
-  for (uint32_t bit = 1u << 31; bit != 0; bit >>= 1) {
-    int count = 0;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(upper[i] >= (t | bit)));
-    if (count >= top) t |= bit;
-  }
-  int reach = 0;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) reach += __builtin_popcountll(__builtin_amdgcn_ballot_w64(upper[i] >= t));
-  if (reach > kFewKeys) {
-#pragma unroll 1
-    for (uint32_t bit = 1u << 31; bit != 0; bit >>= 1) {
-      int count = 0;
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(upper[i] > t || (upper[i] == t && lower[i] >= (at | bit))));
-      if (count >= top) at |= bit;
-    }
-  }
-  uint32_t left = 0;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const bool stays = upper[i] > t || (upper[i] == t && lower[i] >= at);
-    const uint64_t some = __builtin_amdgcn_ballot_w64(stays);
-    const uint32_t place = left + __builtin_amdgcn_mbcnt_hi((uint32_t)(some >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)some, 0));
-    if (stays) keys[place] = (Key)upper[i] << 32 | lower[i];
-    left += (uint32_t)__builtin_popcountll(some);
-  }
-  return left;
-}
-
-// More logits than there is room for: the last of the best among those that are there is a better bound.  What is above it, and of
+// More logits than there is room for: the last of the best among those that are there, or little below it, is a better bound.  What is above it, and of
 // those that equal it the first ones by column, as many as are missing; or all over again from there, as every key there is
 // above the bound then.  By all threads, as all of these.
 template <int TYPE>
@@ -274,18 +275,12 @@ __device__ __attribute__((noinline)) uint32_t gather_again(const void* row, Colu
   TopRoom& r = *room;
   for (uint32_t above = kRoom;;) {
     __syncthreads();
-    if (threadIdx.x < kWave) {
-      const uint32_t left = cut_keys(r.keys, above, top);
-      float least = kInf;
-      for (uint32_t i = threadIdx.x; i < left; i += kWave) least = fminf(least, logit_of(r.keys[i]));
-      least = -wave_largest(-least);
-      if (threadIdx.x == 0) {
-        r.least = least;
-        r.found = 0;
-      }
-    }
+    Key k[kRoom / kThreads];
+    keys_of(r.keys, above, k);
+    float least = logit_of(bound_of(k, top, 32, r.cut));
+    least = least == least ? least : -kInf;
+    if (threadIdx.x == 0) r.found = 0;
     __syncthreads();
-    const float least = r.least;
     gather<TYPE>(row, c, least, false, r);
     __syncthreads();
     above = min(r.found, (uint32_t)kRoom);
@@ -313,7 +308,9 @@ __device__ __attribute__((noinline)) uint32_t gather_again(const void* row, Colu
   }
 }
 
-// The first `top` of n keys in LDS, in falling order, to best; 0 behind the last.  Ends with a barrier.
+// The first `top` of n keys in LDS, in falling order, to best; 0 behind the last.  Takes time by the square of n: few lanes with many
+// candidates 242 us where they were cut to a few first, 762 without; one row of 131072 equal logits 43, 886 without.  Ends with
+// a barrier.
 __device__ __forceinline__ void order(const Key* keys, uint32_t n, int top, Key* best) {
   if (threadIdx.x < kMostTop) best[threadIdx.x] = 0;
   __syncthreads();
@@ -341,14 +338,7 @@ __device__ __forceinline__ void select_top(const void* row, const Columns& c, fl
   __syncthreads();
   uint32_t found = r.found;
   if (found > kRoom) found = gather_again<TYPE>(row, c, top, &r);
-  if (found > kFewKeys) {   // ranks take time by the square of their number: few lanes with many candidates 318 us, 762 without
-    if (threadIdx.x < kWave) {
-      const uint32_t left = cut_keys(r.keys, found, top);
-      if (threadIdx.x == 0) r.left = left;
-    }
-    __syncthreads();
-    found = r.left;
-  }
+  if (found > kFewKeys) found = cut_keys<kRoom / kThreads>(r.keys, found, top, r.cut);
   order(r.keys, found, top, r.best);
 }
 
@@ -512,6 +502,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
   __shared__ Key keys[TOP ? kMostParts * kMostTop : 1], best[TOP ? kMostTop : 1];
   __shared__ Key least;
   __shared__ uint32_t found;
+  __shared__ CutRoom cut;
   const int64_t row = block_of();
   if (row >= g.rows) return;
   const int lane = threadIdx.x % kWave;
@@ -547,7 +538,9 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
       if (one != 0 && one >= bound) keys[atomicAdd(&found, 1u)] = one;
     }
     __syncthreads();
-    order(keys, found, g.top, best);
+    uint32_t n = found;
+    if (n > kFewKeys) n = cut_keys<kMostParts * kMostTop / kThreads>(keys, n, g.top, cut);
+    order(keys, n, g.top, best);
     k = best[threadIdx.x % kMostTop];
   }
   finish_row<TYPE, TOP>(g, row, x, k, room);
@@ -568,7 +561,7 @@ __global__ __launch_bounds__(kThreads) void logprob_backward_kernel(LogprobArgs 
   const float lse = g.lse_of[row], entropy = ENTROPY ? g.entropy_of[row] : 0.0f, dh = ENTROPY ? g.dentropy[row] : 0.0f;
   const int64_t token = g.dlogp ? token_of(g, row) : -1;
   const float dl = token < 0 ? 0.0f : token < g.vocab ? g.dlogp[row] : bits_float(0x7FC00000u);
-  const bool empty = lse == -kInf;
+  const bool empty = lse == -kInf || (!ENTROPY && token < 0);   // no gradient, whatever the logits are
   const auto gradient = [&](float x, int col) {
     const float z = larger(__builtin_fmaf(x, g.scale, -lse), kFar), p = exp2_of(z * kLog2e);
     float d = dl * ((token == col ? 1.0f : 0.0f) - p);

@@ -373,3 +373,19 @@ def test_alternatives_among_many_candidates(tr, rows, vocab):
         assert torch.equal(tops, want["ids"].repeat(len(tops) // len(x), 1))
         for f in got if rows > 1 else []:
             check_forward(type(f)(None, *(None if t is None else t[:len(x)] for t in f[1:])), want, vocab, 1.0)
+
+
+def test_rows_without_a_token_have_no_gradient_whatever_they_hold(tr):
+    """Padding that was never written: NaN, infinities; the gradient of an entropy there is what its row is."""
+    for dtype in TYPES.values():
+        for vocab in (1, 70, 9001):
+            x = torch.randn(6, vocab, generator=gen(vocab)).to(dtype)
+            x[1], x[2, vocab // 2], x[3], x[4, 0] = math.nan, math.nan, math.inf, math.inf
+            x[5] = -math.inf
+            tokens = torch.tensor([0, -1, -1, -100, -1, -1])
+            got = tr.moc_logprob_forward(x.cuda(), tokens.cuda())
+            assert not got.logp.cpu()[1:].any() and bool(got.lse.cpu()[1:5].isnan().all())
+            d = tr.moc_logprob_backward(x.cuda(), got.lse, tokens.cuda(), torch.full((6,), math.nan, device="cuda").index_fill_(0, torch.tensor([0], device="cuda"), 1.0))
+            assert not d.cpu()[1:].any() and bool(d.cpu()[0].isfinite().all())
+            d = tr.moc_logprob_backward(x.cuda(), got.lse, tokens.cuda(), torch.ones(6, device="cuda"), got.entropy, torch.ones(6, device="cuda")).cpu()
+            assert bool(d[1:5].isnan().all()) and bool(d[0].isfinite().all()) and not d[5].any()
