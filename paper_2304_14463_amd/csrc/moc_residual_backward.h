@@ -8,12 +8,13 @@ struct ResidualShape {
   ResidualKernel kern;
   int threads, rows;   // of a workgroup
 };
-// What a kernel is made for.
-constexpr int kAlone = 0, kPlain = 1, kGated = 2, kNormed = 3;
+// What a kernel is made for: a norm before the next block, a gradient of the stream, the block's output looked at, a norm behind it.
+constexpr int kBefore = 1, kStream = 2, kBlock = 4, kAfter = 8;
 
 // In a source file of its own for each type of the norm's and the block's gradients; kern is null where there is none.
 ResidualShape moc_residual_backward_bf16(int stream, int block, int mode, bool own, int64_t cols);
 ResidualShape moc_residual_backward_f16(int stream, int block, int mode, bool own, int64_t cols);
+ResidualShape moc_residual_backward_f32(int stream, int block, int mode, bool own, int64_t cols);
 
 namespace {
 
@@ -43,14 +44,13 @@ __device__ __forceinline__ void put_sums(const Runs<CH>& s, float* out, int cols
   }
 }
 
-// Made for types: of a call with a norm before the next block, with dr and dblock.  MODE: kAlone, where
-// there is but a norm, without dr, kPlain, where the block's output is not looked at, kGated, or kNormed with a norm behind it
-// (and a gate, which may be ones).  OWN: a gate for every row.  Lanes beyond the row take no part but in the sums.
-
+// Made for types, of a call with dblock.  MODE: what there is; kBlock is with a gate, kAfter with one that may be ones.
+// OWN: a gate for every row.  Lanes beyond the row take no part but in the sums.
 template <int S, int B, int D, int T, int CH, int MODE, bool OWN>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(ResidualArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
   constexpr bool kAhead = CH == 1 || T <= 512, kHold = kAhead;
+  constexpr bool BEFORE = (MODE & kBefore) != 0, STREAM = (MODE & kStream) != 0, BLOCK = (MODE & kBlock) != 0, AFTER = (MODE & kAfter) != 0;
   using Sums = RowSums<T, 2>;
   __shared__ float room[Sums::kRoom];
   __shared__ float stage[kRows > 1 ? kRows * kRun * T : 1];
@@ -74,15 +74,19 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const uint32_t col = (c * T + lane) * kRun;
-      wr[c] = fetch<S>(g.r, row, col, cols);
-      wn[c] = fetch<D>(g.dn, row, col, cols);
-      if constexpr (MODE != kAlone) wd[c] = fetch<S>(g.dr, row, col, cols);
-      if constexpr (MODE > kPlain) wb[c] = fetch<B>(g.block, row, col, cols);
+      if constexpr (BEFORE) {
+        wr[c] = fetch<S>(g.r, row, col, cols);
+        wn[c] = fetch<D>(g.dn, row, col, cols);
+      }
+      if constexpr (STREAM) wd[c] = fetch<S>(g.dr, row, col, cols);
+      if constexpr (BLOCK) wb[c] = fetch<B>(g.block, row, col, cols);
       if constexpr (OWN) wg[c] = load_run_of<kTensor>(g.gate, row, (int)col, g.cols, true);
     }
-    stats[0] = of_row(means2, row);
-    stats[1] = of_row(g.before.rstd, row);
-    if constexpr (MODE == kNormed) {
+    if constexpr (BEFORE) {
+      stats[0] = of_row(means2, row);
+      stats[1] = of_row(g.before.rstd, row);
+    }
+    if constexpr (AFTER) {
       stats[2] = of_row(means1, row);
       stats[3] = of_row(g.after.rstd, row);
     }
@@ -92,25 +96,27 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
     uint32_t row = first + mine;
     if (kAhead && row < end) load(row);
     if (kHold && which == from) {   // with the first row on its way
-      if constexpr (MODE == kNormed) {
+      if constexpr (AFTER) {
         hold_param<T, CH>(g.after.gamma, g.after.param_type, lane, cols, 1.0f, gamma1);
         hold_param<T, CH>(g.after.beta, g.after.param_type, lane, cols, 0.0f, beta1);
       }
-      hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, cols, 1.0f, gamma2);
+      if constexpr (BEFORE) hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, cols, 1.0f, gamma2);
     }
-    if constexpr (MODE > kPlain && kHold && !OWN) hold_gate<T, CH>(g, which, lane, gate);
+    if constexpr (BLOCK && kHold && !OWN) hold_gate<T, CH>(g, which, lane, gate);
     for (; row < end; row += kRows) {   // groups of lanes that end earlier share no barrier
       if (!kAhead) load(row);
       Runs<CH> h, d;
       Raw cr[CH], cn[CH], cd[CH], cb[CH], cg[CH];
-      const float mean2 = stats[0] * layer2, rstd2 = stats[1], mean1 = MODE == kNormed ? stats[2] * layer1 : 0.0f, rstd1 = MODE == kNormed ? stats[3] : 1.0f;
+      const float mean2 = BEFORE ? stats[0] * layer2 : 0.0f, rstd2 = BEFORE ? stats[1] : 1.0f, mean1 = AFTER ? stats[2] * layer1 : 0.0f, rstd1 = AFTER ? stats[3] : 1.0f;
       float m[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
-        cr[c] = wr[c];
-        cn[c] = wn[c];
-        if constexpr (MODE != kAlone) cd[c] = wd[c];
-        if constexpr (MODE > kPlain) cb[c] = wb[c];
+        if constexpr (BEFORE) {
+          cr[c] = wr[c];
+          cn[c] = wn[c];
+        }
+        if constexpr (STREAM) cd[c] = wd[c];
+        if constexpr (BLOCK) cb[c] = wb[c];
         if constexpr (OWN) cg[c] = wg[c];
       }
       if (kAhead) load(min(row + kRows, end - 1));   // behind the last row it once more
@@ -118,19 +124,21 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
       for (int c = 0; c < CH; ++c) {
         const uint32_t col = (c * T + lane) * kRun;
         if (col < cols && col + kRun > cols) {
-          settle_run<S>(cr[c], col, cols);
-          settle_run<D>(cn[c], col, cols);
-          if constexpr (MODE != kAlone) settle_run<S>(cd[c], col, cols);
-          if constexpr (MODE > kPlain) settle_run<B>(cb[c], col, cols);
+          if constexpr (BEFORE) {
+            settle_run<S>(cr[c], col, cols);
+            settle_run<D>(cn[c], col, cols);
+          }
+          if constexpr (STREAM) settle_run<S>(cd[c], col, cols);
+          if constexpr (BLOCK) settle_run<B>(cb[c], col, cols);
         }
-        if (col < cols) {
+        if (BEFORE && col < cols) {
           values_fetched<S>(g.r, cr[c], h[c]);
           values_fetched<D>(g.dn, cn[c], d[c]);
           float ga[kRun];   // where the row has ended h meets zeros
           before_run(h[c], d[c], mean2, rstd2, param_of<kHold>(gamma2[c], g.before.gamma, g.before.param_type, (int)col, g.cols, 1.0f, ga), sg2[c], sb2[c], m);
         }
       }
-      sums(m);
+      if constexpr (BEFORE) sums(m);
       const float a2 = m[0] * part2, b2 = m[1] * part;
       m[0] = m[1] = 0.0f;
 #pragma unroll
@@ -138,17 +146,19 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
         const uint32_t col = (c * T + lane) * kRun;
         if (col < cols) {
           float v[kRun];
-          norm_gradient(d[c], h[c], rstd2, a2, b2);
-          if constexpr (MODE != kAlone) {
-            values_fetched<S>(g.dr, cd[c], v);
-            add_run(d[c], v);
+          if constexpr (BEFORE) norm_gradient(d[c], h[c], rstd2, a2, b2);
+          if constexpr (STREAM) values_fetched<S>(g.dr, cd[c], v);
+          if constexpr (BEFORE && STREAM) add_run(d[c], v);
+          if constexpr (!BEFORE) {
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) d[c][i] = v[i];
           }
           if (g.dx.data) {
 #pragma unroll
             for (int i = 0; i < kRun; ++i) v[i] = g.scale * d[c][i];
             put<S>(g.dx, row, col, cols, v);
           }
-          if constexpr (MODE > kPlain) {
+          if constexpr (BLOCK) {
             if (col + kRun > cols) {
 #pragma unroll
               for (uint32_t i = 0; i < kRun; ++i) d[c][i] = col + i < cols ? d[c][i] : 0.0f;
@@ -156,21 +166,21 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
             values_fetched<B>(g.block, cb[c], h[c]);
             float ga[kRun], be[kRun], of[kRun];
             if constexpr (OWN) values_of_run<kTensor>(g.gate, cg[c], (int)col, g.cols, true, of);
-            gate_run<MODE == kNormed>(h[c], d[c], v, mean1, rstd1, param_of<kHold || MODE != kNormed>(gamma1[c], g.after.gamma, g.after.param_type, (int)col, g.cols, 1.0f, ga),
-                                      param_of<kHold || MODE != kNormed>(beta1[c], g.after.beta, g.after.param_type, (int)col, g.cols, 0.0f, be),
+            gate_run<AFTER>(h[c], d[c], v, mean1, rstd1, param_of<kHold || !AFTER>(gamma1[c], g.after.gamma, g.after.param_type, (int)col, g.cols, 1.0f, ga),
+                                      param_of<kHold || !AFTER>(beta1[c], g.after.beta, g.after.param_type, (int)col, g.cols, 0.0f, be),
                                       OWN ? of : param_of<kHold>(gate[c], g.gates ? row_at(g.gate, which) : nullptr, g.gate.type, (int)col, g.cols, 1.0f, of), sg1[c], sb1[c], m);
             if constexpr (!OWN) add_run(sgate[c], v);
             else if (g.want_gate) put<MOC_F32>(Mat{reinterpret_cast<char*>(g.gate_sums), nullptr, cols * 4, 0, MOC_F32}, row, col, cols, v);
           }
         }
       }
-      if constexpr (MODE == kNormed) sums(m);
+      if constexpr (AFTER) sums(m);
       const float a1 = m[0] * part1, b1 = m[1] * part;
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         const uint32_t col = (c * T + lane) * kRun;
         if (col < cols) {
-          if constexpr (MODE == kNormed) norm_gradient(d[c], h[c], rstd1, a1, b1);
+          if constexpr (AFTER) norm_gradient(d[c], h[c], rstd1, a1, b1);
           put<D>(g.dblock, row, col, cols, d[c]);
         }
       }
@@ -192,7 +202,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
     put_sums<T, kRows, CH>(sb2, out, g.cols, stage);
     out += g.cols;
   }
-  if constexpr (MODE == kNormed) {
+  if constexpr (AFTER) {
     if (g.kinds & kAfterGamma) {
       put_sums<T, kRows, CH>(sg1, out, g.cols, stage);
       out += g.cols;
@@ -208,22 +218,37 @@ ResidualShape backward_shape(int64_t cols) {
   if (cols <= 1024) return {residual_backward_kernel<S, B, D, 64, 2, MODE, OWN>, 256, 4};
   if (cols <= 2048) return {residual_backward_kernel<S, B, D, 256, 1, MODE, OWN>, 256, 1};
   if (cols <= 4096) return {residual_backward_kernel<S, B, D, 512, 1, MODE, OWN>, 512, 1};
+  // with both norms the next row's values do not fit: 8192 x 8192 float32 576 us with a run a lane and 729 with two, bf16 261 and 249
+  if (cols <= 8192 && D == MOC_F32 && (MODE & kBefore) && (MODE & kAfter)) return {residual_backward_kernel<S, B, D, 1024, 1, MODE, OWN>, 1024, 1};
   if (cols <= 8192) return {residual_backward_kernel<S, B, D, 512, 2, MODE, OWN>, 512, 1};
   return {residual_backward_kernel<S, B, D, 1024, 2, MODE, OWN>, 1024, 1};
 }
 template <int S, int B, int D>
 ResidualShape backward_shape(int mode, bool own, int64_t cols) {
-  if (mode == kAlone) return backward_shape<S, D, D, kAlone, false>(cols);
-  if (mode == kPlain) return backward_shape<S, D, D, kPlain, false>(cols);
-  if (mode == kGated) return own ? backward_shape<S, B, D, kGated, true>(cols) : backward_shape<S, B, D, kGated, false>(cols);
-  return own ? backward_shape<S, B, D, kNormed, true>(cols) : backward_shape<S, B, D, kNormed, false>(cols);
+  switch (mode) {
+    case kBefore: return backward_shape<S, D, D, kBefore, false>(cols);
+    case kBefore | kStream: return backward_shape<S, D, D, kBefore | kStream, false>(cols);
+    case kBefore | kStream | kBlock: return own ? backward_shape<S, B, D, kBefore | kStream | kBlock, true>(cols) : backward_shape<S, B, D, kBefore | kStream | kBlock, false>(cols);
+    case kBefore | kStream | kBlock | kAfter:
+      return own ? backward_shape<S, B, D, kBefore | kStream | kBlock | kAfter, true>(cols) : backward_shape<S, B, D, kBefore | kStream | kBlock | kAfter, false>(cols);
+  }
+  if (own) return {};
+  switch (mode) {
+    case kBefore | kBlock: return backward_shape<S, B, D, kBefore | kBlock, false>(cols);
+    case kBefore | kBlock | kAfter: return backward_shape<S, B, D, kBefore | kBlock | kAfter, false>(cols);
+    case kStream | kBlock: return backward_shape<S, B, D, kStream | kBlock, false>(cols);
+    case kStream | kBlock | kAfter: return backward_shape<S, B, D, kStream | kBlock | kAfter, false>(cols);
+  }
+  return {};
 }
 template <int D>
 ResidualShape backward_shape_of(int s, int b, int mode, bool own, int64_t cols) {
   if (s == D && b == D) return backward_shape<D, D, D>(mode, own, cols);
   if (s == D && b == kKept) return backward_shape<D, kKept, D>(mode, own, cols);
-  if (s == MOC_F32 && b == D) return backward_shape<MOC_F32, D, D>(mode, own, cols);
-  if (s == MOC_F32 && b == kKept) return backward_shape<MOC_F32, kKept, D>(mode, own, cols);
+  if constexpr (D != MOC_F32) {
+    if (s == MOC_F32 && b == D) return backward_shape<MOC_F32, D, D>(mode, own, cols);
+    if (s == MOC_F32 && b == kKept) return backward_shape<MOC_F32, kKept, D>(mode, own, cols);
+  }
   return {};
 }
 

@@ -316,15 +316,17 @@ int moc_residual_backward(int64_t rows, int64_t cols, const moc_matrix* dr, cons
   ResidualArgs g = {};
   g.parts = lies_over(dx, {dr, dn, r, block, gate}) || lies_over(dblock, {dr, dn, r, block, gate});
   // kernels made for some types, where all matrices are of them and a row's last run may be loaded whole
-  const bool ragged = cols < kRun || (g.parts && cols % kRun != 0), usual = last && dblock && !ragged, own = gates > 1 && gates == rows;
-  const int kd = agreed({dn, dblock}, kAny), ks = agreed({dr, r, dx}, kAny), kb = needed ? kind_of(block->type) : kd, mode = first ? kNormed : needed || gate ? kGated : dr ? kPlain : kAlone;
+  const bool ragged = cols < kRun || (g.parts && cols % kRun != 0), usual = dblock && !ragged && (needed || !gate), own = gates > 1 && gates == rows;
+  const int kd = agreed({dn, dblock}, kAny), ks = agreed({dr, last ? r : nullptr, dx}, kAny), kb = needed ? kind_of(block->type) : kd;
+  const int mode = (last ? kBefore : 0) | (dr ? kStream : 0) | (needed ? kBlock : 0) | (first ? kAfter : 0);
   ResidualShape s = {};
-  if (usual && (mode <= kPlain || (needed && dr))) {
+  if (usual) {
+    if (kd == MOC_F32) s = moc_residual_backward_f32(ks, kb, mode, own, cols);
     if (kd == MOC_BF16) s = moc_residual_backward_bf16(ks, kb, mode, own, cols);
     if (kd == MOC_F16) s = moc_residual_backward_f16(ks, kb, mode, own, cols);
   }
   if (!s.kern) s = any_shape(first, cols);
-  const Cut c = cut_of(s, rows, gates, units, mode <= kPlain && cols <= 4096 ? kManyWaves : kFewWaves);
+  const Cut c = cut_of(s, rows, gates, units, !needed && !gate && cols <= 4096 ? kManyWaves : kFewWaves);
   const bool gate_parts = d.gate && !c.own && c.chunks > 1;
   const int64_t need = sums_bytes(c, kinds, gates, d.gate != nullptr, cols);
   if (need > 0 && (!work || !aligned_to(work, 16) || work_bytes < need)) return MOC_EINVAL;

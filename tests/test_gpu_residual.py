@@ -426,3 +426,33 @@ def test_a_checkpoint_to_write_to_is_apart_from_the_norms(tr):
         with pytest.raises(ValueError):
             tr.moc_residual_forward(None, b, after=after, before=before, keep=kept)
     assert not room.any()
+
+
+PARTS = [dict(block="bf16", stream="bf16", after="rms", before=None, gates=1),
+         dict(block="fp16", stream="fp32", held="int8", after="layer", before=None, gates=2, ptype=torch.float16),
+         dict(block="fp16", stream="fp16", after="layer", before=None, gates=0, lead=1, pad=3),
+         dict(block="bf16", stream="fp32", held="e4m3", after=None, before=None, gates=3),
+         dict(block="fp32", stream="fp32", after="layer", before="layer", gates=3, lead=1, pad=2),
+         dict(block="fp32", stream="fp32", held="e4m3", after=None, before="rms", gates=6),
+         dict(block="fp32", stream="fp32", held="int8", after="rms", before="rms", gates=6),
+         dict(block="fp32", stream="fp32", after="rms", before=None, gates=0),
+         dict(block="fp32", stream="fp32", after=None, before=None, gates=1),
+         dict(block="fp32", stream="fp32", after=None, before="layer", gates=0),
+         dict(block="fp32", stream="fp32", after=None, before=None, gates=0)]
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("kind", PARTS, ids=["-".join(str(v) for v in k.values() if not isinstance(v, torch.dtype)) for k in PARTS])
+def test_backward_of_parts_and_of_float32(tr, cols, kind):
+    """A norm behind the block or a gate alone, with no norm before the next block; without the stream's gradient."""
+    check_backward(tr, 6, cols, kind)
+
+
+@pytest.mark.parametrize("rows,cols", [(3000, 64), (2002, 1247), (600, 4096), (601, 8192)])
+@pytest.mark.parametrize("gates", [0, 1, 2, -2, -1])
+@pytest.mark.parametrize("kind", [0, 2, 4, 5, 8])
+def test_backward_of_parts_over_many_rows(tr, rows, cols, gates, kind):
+    gates = gates if gates >= 0 else rows // -gates
+    if gates < 1 or rows % gates:
+        gates = min(gates, 1)
+    check_backward(tr, rows, cols, dict(PARTS[kind], gates=gates))
