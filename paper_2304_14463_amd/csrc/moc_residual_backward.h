@@ -8,8 +8,9 @@ struct ResidualShape {
   ResidualKernel kern;
   int threads, rows;   // of a workgroup
 };
-// What a kernel is made for: a norm before the next block, a gradient of the stream, the block's output looked at, a norm behind it.
-constexpr int kBefore = 1, kStream = 2, kBlock = 4, kAfter = 8;
+// What a kernel is made for: a norm before the next block, a gradient of the stream, the block's output looked at, a norm behind it;
+// a gate, without a look at the block's output.
+constexpr int kBefore = 1, kStream = 2, kBlock = 4, kAfter = 8, kGate = 16;
 
 // In a source file of its own for each type of the norm's and the block's gradients; kern is null where there is none.
 ResidualShape moc_residual_backward_bf16(int stream, int block, int mode, bool own, int64_t cols);
@@ -44,13 +45,13 @@ __device__ __forceinline__ void put_sums(const Runs<CH>& s, float* out, int cols
   }
 }
 
-// Made for types, of a call with dblock.  MODE: what there is; kBlock is with a gate, kAfter with one that may be ones.
+// Made for types, of a call with dblock.  MODE: what there is; the gate of kBlock, kAfter and kGate may be ones.
 // OWN: a gate for every row.  Lanes beyond the row take no part but in the sums.
 template <int S, int B, int D, int T, int CH, int MODE, bool OWN>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(ResidualArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
   constexpr bool kAhead = CH == 1 || T <= 512, kHold = kAhead;
-  constexpr bool BEFORE = (MODE & kBefore) != 0, STREAM = (MODE & kStream) != 0, BLOCK = (MODE & kBlock) != 0, AFTER = (MODE & kAfter) != 0;
+  constexpr bool BEFORE = (MODE & kBefore) != 0, STREAM = (MODE & kStream) != 0, BLOCK = (MODE & kBlock) != 0, AFTER = (MODE & kAfter) != 0, GATE = BLOCK || (MODE & kGate) != 0;
   using Sums = RowSums<T, 2>;
   __shared__ float room[Sums::kRoom];
   __shared__ float stage[kRows > 1 ? kRows * kRun * T : 1];
@@ -102,7 +103,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
       }
       if constexpr (BEFORE) hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, cols, 1.0f, gamma2);
     }
-    if constexpr (BLOCK && kHold && !OWN) hold_gate<T, CH>(g, which, lane, gate);
+    if constexpr (GATE && kHold && !OWN) hold_gate<T, CH>(g, which, lane, gate);
     for (; row < end; row += kRows) {   // groups of lanes that end earlier share no barrier
       if (!kAhead) load(row);
       Runs<CH> h, d;
@@ -158,6 +159,12 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
             for (int i = 0; i < kRun; ++i) v[i] = g.scale * d[c][i];
             put<S>(g.dx, row, col, cols, v);
           }
+          if constexpr (GATE && !BLOCK) {
+            float of[kRun];
+            const float(&by)[kRun] = param_of<kHold>(gate[c], g.gates ? row_at(g.gate, which) : nullptr, g.gate.type, (int)col, g.cols, 1.0f, of);
+#pragma unroll
+            for (int i = 0; i < kRun; ++i) d[c][i] *= by[i];
+          }
           if constexpr (BLOCK) {
             if (col + kRun > cols) {
 #pragma unroll
@@ -185,7 +192,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
         }
       }
     }
-    if (!OWN && g.want_gate) {
+    if (BLOCK && !OWN && g.want_gate) {
       put_sums<T, kRows, CH>(sgate, g.gate_sums + (uint64_t)(which * g.chunks + chunk) * g.cols, g.cols, stage);
 #pragma unroll
       for (int c = 0; c < CH; ++c)
@@ -236,6 +243,8 @@ ResidualShape backward_shape(int mode, bool own, int64_t cols) {
   switch (mode) {
     case kBefore | kBlock: return backward_shape<S, B, D, kBefore | kBlock, false>(cols);
     case kBefore | kBlock | kAfter: return backward_shape<S, B, D, kBefore | kBlock | kAfter, false>(cols);
+    case kStream | kGate: return backward_shape<S, D, D, kStream | kGate, false>(cols);
+    case kBefore | kStream | kGate: return backward_shape<S, D, D, kBefore | kStream | kGate, false>(cols);
     case kStream | kBlock: return backward_shape<S, B, D, kStream | kBlock, false>(cols);
     case kStream | kBlock | kAfter: return backward_shape<S, B, D, kStream | kBlock | kAfter, false>(cols);
   }

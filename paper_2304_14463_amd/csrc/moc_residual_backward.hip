@@ -316,9 +316,9 @@ int moc_residual_backward(int64_t rows, int64_t cols, const moc_matrix* dr, cons
   ResidualArgs g = {};
   g.parts = lies_over(dx, {dr, dn, r, block, gate}) || lies_over(dblock, {dr, dn, r, block, gate});
   // kernels made for some types, where all matrices are of them and a row's last run may be loaded whole
-  const bool ragged = cols < kRun || (g.parts && cols % kRun != 0), usual = dblock && !ragged && (needed || !gate), own = gates > 1 && gates == rows;
+  const bool ragged = cols < kRun || (g.parts && cols % kRun != 0), usual = dblock && !ragged, own = gates > 1 && gates == rows;
   const int kd = agreed({dn, dblock}, kAny), ks = agreed({dr, last ? r : nullptr, dx}, kAny), kb = needed ? kind_of(block->type) : kd;
-  const int mode = (last ? kBefore : 0) | (dr ? kStream : 0) | (needed ? kBlock : 0) | (first ? kAfter : 0);
+  const int mode = (last ? kBefore : 0) | (dr ? kStream : 0) | (needed ? kBlock : 0) | (first ? kAfter : 0) | (!needed && (gate || !last) ? kGate : 0);
   ResidualShape s = {};
   if (usual) {
     if (kd == MOC_F32) s = moc_residual_backward_f32(ks, kb, mode, own, cols);
