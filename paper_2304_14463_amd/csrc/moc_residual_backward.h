@@ -45,15 +45,37 @@ __device__ __forceinline__ void put_sums(const Runs<CH>& s, float* out, int cols
   }
 }
 
+// Where a workgroup's parameters are: a run's in registers, all in LDS, of which a lane reads what it has written, or in cache.
+constexpr int kRegisters = 0, kLds = 1, kCache = 2;
+template <int WHERE>
+__device__ __forceinline__ const float (&param_at(const float (&held)[kRun], const float* lds, const void* p, int type, int col, int cols, float other, float (&room)[kRun]))[kRun] {
+  if constexpr (WHERE == kLds) {
+    __builtin_memcpy(room, lds + col, sizeof room);
+    return room;
+  } else {
+    return param_of<WHERE == kRegisters>(held, p, type, col, cols, other, room);
+  }
+}
+template <int T, int CH, int WHERE>
+__device__ __forceinline__ void place_param(const void* p, int type, int lane, int cols, float other, Runs<CH>& v, float* lds) {
+  hold_param<T, CH>(p, type, lane, cols, other, v);
+  if constexpr (WHERE == kLds) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) __builtin_memcpy(lds + (c * T + lane) * kRun, v[c], sizeof v[c]);
+  }
+}
+
 // Made for types, of a call with dblock.  MODE: what there is; the gate of kBlock, kAfter and kGate may be ones.
 // OWN: a gate for every row.  Lanes beyond the row take no part but in the sums.
 template <int S, int B, int D, int T, int CH, int MODE, bool OWN>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(ResidualArgs g) {
   constexpr int kRows = T < 256 ? 256 / T : 1;
-  constexpr bool kAhead = CH == 1 || T <= 512, kHold = kAhead;
+  constexpr bool kAhead = CH == 1 || T <= 512;
   constexpr bool BEFORE = (MODE & kBefore) != 0, STREAM = (MODE & kStream) != 0, BLOCK = (MODE & kBlock) != 0, AFTER = (MODE & kAfter) != 0, GATE = BLOCK || (MODE & kGate) != 0;
+  constexpr int kWhere = !kAhead ? kCache : T == 512 && CH == 2 && BEFORE && AFTER ? kLds : kRegisters, kPlaces = kWhere == kLds ? T * CH * kRun : 0;
   using Sums = RowSums<T, 2>;
   __shared__ float room[Sums::kRoom];
+  __shared__ __attribute__((aligned(16))) float params[kWhere == kLds ? 4 * kPlaces : 1];
   __shared__ float stage[kRows > 1 ? kRows * kRun * T : 1];
   Sums sums{room};
   const uint32_t lane = threadIdx.x % T, mine = kRows > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / T) : 0, cols = g.cols;
@@ -96,14 +118,14 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
     const uint32_t first = which * g.rows_per_gate + chunk * g.chunk_rows, end = min(first + g.chunk_rows, (which + 1) * g.rows_per_gate);
     uint32_t row = first + mine;
     if (kAhead && row < end) load(row);
-    if (kHold && which == from) {   // with the first row on its way
+    if (kWhere != kCache && which == from) {   // with the first row on its way
       if constexpr (AFTER) {
-        hold_param<T, CH>(g.after.gamma, g.after.param_type, lane, cols, 1.0f, gamma1);
-        hold_param<T, CH>(g.after.beta, g.after.param_type, lane, cols, 0.0f, beta1);
+        place_param<T, CH, kWhere>(g.after.gamma, g.after.param_type, lane, cols, 1.0f, gamma1, params);
+        place_param<T, CH, kWhere>(g.after.beta, g.after.param_type, lane, cols, 0.0f, beta1, params + kPlaces);
       }
-      if constexpr (BEFORE) hold_param<T, CH>(g.before.gamma, g.before.param_type, lane, cols, 1.0f, gamma2);
+      if constexpr (BEFORE) place_param<T, CH, kWhere>(g.before.gamma, g.before.param_type, lane, cols, 1.0f, gamma2, params + 2 * kPlaces);
     }
-    if constexpr (GATE && kHold && !OWN) hold_gate<T, CH>(g, which, lane, gate);
+    if constexpr (GATE && kWhere != kCache && !OWN) place_param<T, CH, kWhere>(g.gates ? row_at(g.gate, which) : nullptr, g.gate.type, lane, cols, 1.0f, gate, params + 3 * kPlaces);
     for (; row < end; row += kRows) {   // groups of lanes that end earlier share no barrier
       if (!kAhead) load(row);
       Runs<CH> h, d;
@@ -136,7 +158,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
           values_fetched<S>(g.r, cr[c], h[c]);
           values_fetched<D>(g.dn, cn[c], d[c]);
           float ga[kRun];   // where the row has ended h meets zeros
-          before_run(h[c], d[c], mean2, rstd2, param_of<kHold>(gamma2[c], g.before.gamma, g.before.param_type, (int)col, g.cols, 1.0f, ga), sg2[c], sb2[c], m);
+          before_run(h[c], d[c], mean2, rstd2, param_at<kWhere>(gamma2[c], params + 2 * kPlaces, g.before.gamma, g.before.param_type, (int)col, g.cols, 1.0f, ga), sg2[c], sb2[c], m);
         }
       }
       if constexpr (BEFORE) sums(m);
@@ -161,7 +183,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
           }
           if constexpr (GATE && !BLOCK) {
             float of[kRun];
-            const float(&by)[kRun] = param_of<kHold>(gate[c], g.gates ? row_at(g.gate, which) : nullptr, g.gate.type, (int)col, g.cols, 1.0f, of);
+            const float(&by)[kRun] = param_at<kWhere>(gate[c], params + 3 * kPlaces, g.gates ? row_at(g.gate, which) : nullptr, g.gate.type, (int)col, g.cols, 1.0f, of);
 #pragma unroll
             for (int i = 0; i < kRun; ++i) d[c][i] *= by[i];
           }
@@ -173,9 +195,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void residual_backward_kernel(Re
             values_fetched<B>(g.block, cb[c], h[c]);
             float ga[kRun], be[kRun], of[kRun];
             if constexpr (OWN) values_of_run<kTensor>(g.gate, cg[c], (int)col, g.cols, true, of);
-            gate_run<AFTER>(h[c], d[c], v, mean1, rstd1, param_of<kHold || !AFTER>(gamma1[c], g.after.gamma, g.after.param_type, (int)col, g.cols, 1.0f, ga),
-                                      param_of<kHold || !AFTER>(beta1[c], g.after.beta, g.after.param_type, (int)col, g.cols, 0.0f, be),
-                                      OWN ? of : param_of<kHold>(gate[c], g.gates ? row_at(g.gate, which) : nullptr, g.gate.type, (int)col, g.cols, 1.0f, of), sg1[c], sb1[c], m);
+            gate_run<AFTER>(h[c], d[c], v, mean1, rstd1, param_at<AFTER ? kWhere : kRegisters>(gamma1[c], params, g.after.gamma, g.after.param_type, (int)col, g.cols, 1.0f, ga),
+                                      param_at<AFTER ? kWhere : kRegisters>(beta1[c], params + kPlaces, g.after.beta, g.after.param_type, (int)col, g.cols, 0.0f, be),
+                                      OWN ? of : param_at<kWhere>(gate[c], params + 3 * kPlaces, g.gates ? row_at(g.gate, which) : nullptr, g.gate.type, (int)col, g.cols, 1.0f, of), sg1[c], sb1[c], m);
             if constexpr (!OWN) add_run(sgate[c], v);
             else if (g.want_gate) put<MOC_F32>(Mat{reinterpret_cast<char*>(g.gate_sums), nullptr, cols * 4, 0, MOC_F32}, row, col, cols, v);
           }
@@ -225,8 +247,6 @@ ResidualShape backward_shape(int64_t cols) {
   if (cols <= 1024) return {residual_backward_kernel<S, B, D, 64, 2, MODE, OWN>, 256, 4};
   if (cols <= 2048) return {residual_backward_kernel<S, B, D, 256, 1, MODE, OWN>, 256, 1};
   if (cols <= 4096) return {residual_backward_kernel<S, B, D, 512, 1, MODE, OWN>, 512, 1};
-  // with both norms the next row's values do not fit: 8192 x 8192 float32 576 us with a run a lane and 729 with two, bf16 261 and 249
-  if (cols <= 8192 && D == MOC_F32 && (MODE & kBefore) && (MODE & kAfter)) return {residual_backward_kernel<S, B, D, 1024, 1, MODE, OWN>, 1024, 1};
   if (cols <= 8192) return {residual_backward_kernel<S, B, D, 512, 2, MODE, OWN>, 512, 1};
   return {residual_backward_kernel<S, B, D, 1024, 2, MODE, OWN>, 1024, 1};
 }
