@@ -6,7 +6,7 @@
 // to 1024 columns, then 256, 512 and 1024 threads.  Parameters stay in registers over a workgroup's rows, and in the backward
 // pass so do their gradients' sums, which a second kernel adds over workgroups, in their order; the next row is on its
 // way meanwhile.  Kernels are made for types: with types asked at every run, code and scalar registers grew until those spilled
-// (4998 x 1247 backward from int8 94 us, 36 so).  bf16, both norms and a gate: 32768 x 4096 forward 206 us (5.2 TB/s), backward
+// (4998 x 1247 backward from int8 94 us, 36 so; 8192 x 8192 bf16 with a gate alone 274 and 115, float32 647 and 334).  bf16, both norms and a gate: 32768 x 4096 forward 206 us (5.2 TB/s), backward
 // 319 (5.1); a copy of 1 GiB reaches 5.0.  Of 8193 to 16384 columns the backward pass with both norms spills half a kilobyte a lane
 // (8192 x 16384: 866 us, 1.9 TB/s); without the norm behind the block it is 283 us, 4.8 TB/s.
 #pragma once
