@@ -10,7 +10,7 @@
 // quarter of the rate); 4999 x 32003 fp16 with five alternatives 69 us, 64 of them 96 (391 with lists that waves hold); one row
 // of 131072 with twenty 12 us (51 by one workgroup).
 // Backward: a pass over the logits and their gradient, 8192 columns a workgroup, runs at aligned addresses: 8192 x 131072 bf16
-// 749 us, 5.7 TB/s (843 where each load had a branch); four float32 values a lane (1247 x 32003 65 us, 83 with eight).
+// 742 us, 5.8 TB/s (843 where each load had a branch); four float32 values a lane (1247 x 32003 65 us, 83 with eight).
 #include <algorithm>
 
 #include "moc_rows.h"
@@ -704,7 +704,9 @@ int moc_logprob_backward(int64_t rows, int64_t vocab, const moc_matrix* logits, 
   g.scale = scale;
   g.tokens = tokens; g.lse_of = lse; g.entropy_of = entropy; g.dlogp = dlogp; g.dentropy = dentropy;
   g.out = out->data; g.out_stride = out->stride; g.out_type = out->type;
-  const int pieces = (int)((vocab + kRun - 1 + kAtOnce - 1) / kAtOnce);   // a row's first run may begin up to seven columns before it
+  // a row's first run may begin up to seven columns before it
+  const bool aligned = logits->type == MOC_F32 || out->type != logits->type || (aligned_to(out->data, 16) && (rows == 1 || out->stride * type_bytes(out->type) % 16 == 0));
+  const int pieces = (int)((vocab + (aligned ? 0 : kRun - 1) + kAtOnce - 1) / kAtOnce);
   hipLaunchKernelGGL(dentropy ? backward_of<true>(logits->type) : backward_of<false>(logits->type), grid_of(rows * pieces), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), g,
                      pieces);
   MOC_HIP(hipGetLastError());
