@@ -43,8 +43,9 @@ struct LogprobArgs {
   int out_type;
 };
 
-// To a number or NaN where one of the two is NaN.
+// NaN where one of the two is NaN.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
 __device__ __forceinline__ int64_t token_of(const LogprobArgs& g, int64_t row) {
@@ -55,13 +56,16 @@ __device__ __forceinline__ int64_t token_of(const LogprobArgs& g, int64_t row) {
 
 struct Sums {
   float m;      // the largest logit
-  float at;     // scale2 * m, or what anchor() makes of it: terms are 2^(scale2 x - at)
+  float at;     // scale2 * m, rounded, or what anchor() makes of it: terms are 2^(scale2 x - at)
   float s, w;
 };
 
-// Logits of the type's lowest value (a mask's) times scale2 pass float32's range; where nothing else has been met, `at`
-// stays above them and they count as nothing.  A row of nothing else is taken again by row_again().
-__device__ __forceinline__ float anchor(float m, float scale2) { return fmaxf(m * scale2, -0x1p127f); }
+// Up to kReach either way, scale2 * m is rounded by a quarter at most, so that the largest term is 2^(+-1/4) and all sums stay
+// in range.  Beyond it the rounding grows without bound (2^100 and more for masks of -1e9 or -1e30, and their w not a number
+// where a real logit comes after): what lies below counts as nothing beside whatever lies above, and a row of nothing else, or one with
+// logits above kReach, is taken again by row_again().
+constexpr float kReach = 0x1p23f;
+__device__ __forceinline__ float anchor(float m, float scale2) { return fmaxf(m * scale2, -kReach); }
 
 // Terms relative to `to` instead of x.at.
 __device__ __forceinline__ void move_to(Sums& x, float to) {
@@ -344,7 +348,7 @@ __device__ __forceinline__ void select_top(const void* row, const Columns& c, fl
 
 // ---- forward ------------------------------------------------------------------------------------
 
-// A row whose largest logit times scale2 leaves float32's range: differences first.  In all threads.
+// A row whose largest logit times scale2 lies beyond kReach: differences first.  In all threads.
 template <int TYPE>
 __device__ Sums row_again(const LogprobArgs& g, const void* row, float m, float* room) {
   float s = 0.0f, w = 0.0f;
@@ -377,7 +381,7 @@ __device__ Sums row_again(const LogprobArgs& g, const void* row, float m, float*
   return x;
 }
 
-// What a row's sums say; by == again: sums of differences.
+// What a row's sums say; `again`: they are sums of differences.
 struct Row {
   Sums x;
   float log;      // log2 of s
@@ -392,14 +396,14 @@ struct Row {
     if (empty) return -kInf;
     const float p = kLn2 * ((again ? (logit - x.m) * g.scale2 : __builtin_fmaf(logit, g.scale2, -x.at)) - log);
     if (p == -kInf && logit > -kInf) return __builtin_fmaf(logit, g.scale, -lse(g));   // the logit times scale2 has left the range
-    return fminf(p, 0.0f);   // a rounding of scale2 * m may leave 2^-24 above
+    return smaller(p, 0.0f);   // a rounding of scale2 * m may leave 2^-24 above
   }
   __device__ float lse(const LogprobArgs& g) const {
     if (none) return bits_float(0x7FC00000u);
     if (empty) return -kInf;
     return again ? __builtin_fmaf(kLn2, log, g.scale * x.m) : kLn2 * (x.at + log);
   }
-  __device__ float entropy() const { return none ? bits_float(0x7FC00000u) : empty ? 0.0f : fmaxf(kLn2 * (log - x.w / x.s), 0.0f); }
+  __device__ float entropy() const { return none ? bits_float(0x7FC00000u) : empty ? 0.0f : larger(kLn2 * (log - x.w / x.s), 0.0f); }
 };
 
 template <int TYPE>
@@ -425,8 +429,7 @@ __device__ __forceinline__ void write_top(const LogprobArgs& g, int64_t row, con
 template <int TYPE, bool TOP>
 __device__ __forceinline__ void finish_row(const LogprobArgs& g, int64_t row, Sums x, Key k, float* room) {
   using T = typename Stored<TYPE>::type;
-  // beyond float32's range, or with its largest logit there, which then counted as nothing
-  const bool again = x.m > -kInf && (!(x.s > 0.0f && x.s < kInf) || x.at != anchor(x.m, g.scale2));
+  const bool again = x.m > -kInf && (!(x.s > 0.0f && x.s < kInf) || !(__builtin_fabsf(x.m * g.scale2) <= kReach));
   if (again) x = row_again<TYPE>(g, static_cast<const T*>(g.logits) + row * g.stride, x.m, room);
   if (threadIdx.x >= kWave) return;
   const Row r(x, again);
