@@ -303,7 +303,9 @@ int moc_logprob_forward(int64_t rows, int64_t vocab, const moc_matrix* logits, c
 /*
  * The gradient of logp and entropy with regard to the logits:
  *   out = scale * (dlogp * ([column == token] - p) - dentropy * p * (z - lse + entropy))
- *   lse, entropy     as the forward pass has left them; entropy NULL without dentropy
+ *   lse, entropy     as the forward pass has left them; entropy NULL without dentropy.  p
+ *                    is off by what lse is, of itself; of rows with lse beyond 1024 either
+ *                    way the sum is taken again from the logits, by one workgroup
  *   tokens, dlogp    device, float [rows]: both or neither
  *   dentropy         device, float [rows], or NULL
  *   out              [rows][vocab], the logits' type or float32; may be the logits' own

@@ -10,7 +10,7 @@
 // quarter of the rate); 4999 x 32003 fp16 with five alternatives 69 us, 64 of them 96 (391 with lists that waves hold); one row
 // of 131072 with twenty 12 us (51 by one workgroup).
 // Backward: a pass over the logits and their gradient, 8192 columns a workgroup, runs at aligned addresses: 8192 x 131072 bf16
-// 742 us, 5.8 TB/s (843 where each load had a branch); four float32 values a lane (1247 x 32003 65 us, 83 with eight).
+// 690 us, 6.2 TB/s (843 where each load had a branch); four float32 values a lane (1247 x 32003 63 us, 83 with eight).
 #include <algorithm>
 
 #include "moc_rows.h"
@@ -553,9 +553,56 @@ __global__ __launch_bounds__(kThreads) void logprob_join_kernel(LogprobArgs g) {
 
 constexpr int kTurns = 4, kAtOnce = kThreads * kTurns * kRun;   // columns of a workgroup
 
+// p = exp(z - lse) is off by what lse is, of itself: of rows beyond this, where half a step of lse is 2^-14 or more, the sum is taken
+// again by differences from the largest logit.  All of a row masked by -1e9 has lse = -1e9, every p 1 by it, not one of the columns'.
+constexpr float kFarLse = 1024.0f;
+
+// Such a row, by one workgroup (the logits may be overwritten, so that no other may read them): the largest logit, the sum, the gradient.
+// A value a lane, so that there is little code: 8192 x 131072 fp32 3.9 ms, 1.6 where no row is far; one row of 131072 87 us and 5.
+template <int TYPE, class F>
+__device__ __forceinline__ void each_value(const void* row, int vocab, const F& f) {
+  constexpr int kEach = 8;   // on their way at a time
+#pragma unroll 1
+  for (int first = threadIdx.x; first < vocab; first += kEach * kThreads) {
+    typename Stored<TYPE>::type t[kEach];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) t[u] = static_cast<const typename Stored<TYPE>::type*>(row)[min(first + u * kThreads, vocab - 1)];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u)
+      if (first + u * kThreads < vocab) f(first + u * kThreads, (float)t[u]);
+  }
+}
 template <int TYPE, bool ENTROPY>
-__global__ __launch_bounds__(kThreads) void logprob_backward_kernel(LogprobArgs g, int pieces) {
+__device__ __forceinline__ void far_row(const LogprobArgs& g, const void* row, char* out, int64_t token, float dl, float dh, float entropy, float* room) {
+  float m = -kInf, s = 0.0f;
+  each_value<TYPE>(row, g.vocab, [&](int, float x) { m = fmaxf(m, x); });
+  m = wave_largest(m);
+  if (threadIdx.x % kWave == 0) room[threadIdx.x / kWave] = m;
+  __syncthreads();
+  for (int i = 0; i < kWaves; ++i) m = fmaxf(m, room[i]);
+  each_value<TYPE>(row, g.vocab, [&](int, float x) { s += exp2_of(larger((x - m) * g.scale2, kFar)); });
+  s = wave_sum(s);
+  if (threadIdx.x % kWave == 0) room[kWaves + threadIdx.x / kWave] = s;
+  __syncthreads();
+  s = 0.0f;
+  for (int i = 0; i < kWaves; ++i) s += room[kWaves + i];
+  const float log = log2f(s);
+  const bool empty = m == -kInf;
+  each_value<TYPE>(row, g.vocab, [&](int col, float x) {
+    const float t = larger((x - m) * g.scale2 - log, kFar), p = exp2_of(t);
+    float d = dl * ((token == col ? 1.0f : 0.0f) - p);
+    if (ENTROPY) d -= dh * p * __builtin_fmaf(kLn2, t, entropy);
+    d = empty ? 0.0f : g.scale * d;
+    if (g.out_type == MOC_F32) reinterpret_cast<float*>(out)[col] = d;
+    else reinterpret_cast<typename Stored<TYPE>::type*>(out)[col] = (typename Stored<TYPE>::type)d;
+  });
+}
+
+// Six waves a SIMD: with the question for far rows and eight of them 8192 x 131072 bf16 takes 740 us, 690 so, 1247 x 32003 fp32 64 and 63.
+template <int TYPE, bool ENTROPY>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(1, 6))) void logprob_backward_kernel(LogprobArgs g, int pieces) {
   using T = typename Stored<TYPE>::type;
+  __shared__ float room[2 * kWaves];
   const int64_t block = block_of(), row = block / pieces;
   if (row >= g.rows) return;
   const int from = (int)(block - row * pieces) * kAtOnce;
@@ -564,7 +611,13 @@ __global__ __launch_bounds__(kThreads) void logprob_backward_kernel(LogprobArgs 
   const float lse = g.lse_of[row], entropy = ENTROPY ? g.entropy_of[row] : 0.0f, dh = ENTROPY ? g.dentropy[row] : 0.0f;
   const int64_t token = g.dlogp ? token_of(g, row) : -1;
   const float dl = token < 0 ? 0.0f : token < g.vocab ? g.dlogp[row] : bits_float(0x7FC00000u);
-  const bool empty = lse == -kInf || (!ENTROPY && token < 0);   // no gradient, whatever the logits are
+  const bool empty = !ENTROPY && token < 0;   // no gradient, whatever the logits are
+  // In all of a row's workgroups; NaN is not.  Asked with the logits on their way, which are not looked at then.
+  const auto far = [&] {
+    if (!__builtin_amdgcn_readfirstlane(!empty && __builtin_fabsf(lse) > kFarLse)) return false;
+    if ((uint32_t)(block - row * pieces) == (uint32_t)row % (uint32_t)pieces) far_row<TYPE, ENTROPY>(g, at, out, token, dl, dh, entropy, room);   // not all of them on one XCD
+    return true;
+  };
   const auto gradient = [&](float x, int col) {
     const float z = larger(__builtin_fmaf(x, g.scale, -lse), kFar), p = exp2_of(z * kLog2e);
     float d = dl * ((token == col ? 1.0f : 0.0f) - p);
@@ -579,6 +632,7 @@ __global__ __launch_bounds__(kThreads) void logprob_backward_kernel(LogprobArgs 
       const int col = from + (t * kThreads + threadIdx.x) * kFew;
       if (col + kFew <= g.vocab) __builtin_memcpy(&w[t], static_cast<const float*>(at) + col, 16);
     }
+    if (far()) return;
 #pragma unroll
     for (int t = 0; t < 2 * kTurns; ++t) {
       const int col = from + (t * kThreads + threadIdx.x) * kFew;
@@ -600,6 +654,7 @@ __global__ __launch_bounds__(kThreads) void logprob_backward_kernel(LogprobArgs 
       const int col = from + (t * kThreads + threadIdx.x) * kRun - shift;
       if (col >= 0 && col + kRun <= g.vocab) w[t] = load_raw<TYPE>(at, nullptr, col, kRun);
     }
+    if (far()) return;
 #pragma unroll
     for (int t = 0; t < kTurns; ++t) {
       const int col = from + (t * kThreads + threadIdx.x) * kRun - shift;
@@ -646,6 +701,7 @@ Backward backward_of(int type) {
   return type == MOC_BF16 ? logprob_backward_kernel<MOC_BF16, ENTROPY> : type == MOC_F16 ? logprob_backward_kernel<MOC_F16, ENTROPY> : logprob_backward_kernel<MOC_F32, ENTROPY>;
 }
 
+float scale2_of(float scale) { return (float)((double)scale * 1.4426950408889634); }
 bool scale_ok(float scale) { return scale > 0.0f && scale <= 0x1p64f && scale >= 0x1p-64f; }
 bool tokens_ok(const void* tokens, int bytes) { return !tokens || ((bytes == 4 || bytes == 8) && aligned_to(tokens, bytes)); }
 
@@ -682,7 +738,7 @@ int moc_logprob_forward(int64_t rows, int64_t vocab, const moc_matrix* logits, c
   }
   g.logits = logits->data; g.stride = logits->stride;
   g.rows = rows; g.vocab = (int)vocab; g.top = top; g.token_bytes = token_bytes;
-  g.scale = scale; g.scale2 = (float)((double)scale * 1.4426950408889634);
+  g.scale = scale; g.scale2 = scale2_of(scale);
   g.tokens = tokens; g.logp = logp; g.lse = lse; g.entropy = entropy; g.top_logp = top_logp; g.top_tokens = top_tokens;
   hipLaunchKernelGGL(top > 0 ? forward_of<true>(logits->type) : forward_of<false>(logits->type), grid_of(rows * p.parts), dim3(kThreads), 0, static_cast<hipStream_t>(hip_stream), g);
   MOC_HIP(hipGetLastError());
@@ -704,7 +760,7 @@ int moc_logprob_backward(int64_t rows, int64_t vocab, const moc_matrix* logits, 
   LogprobArgs g = {};
   g.logits = logits->data; g.stride = logits->stride;
   g.rows = rows; g.vocab = (int)vocab; g.token_bytes = token_bytes;
-  g.scale = scale;
+  g.scale = scale; g.scale2 = scale2_of(scale);
   g.tokens = tokens; g.lse_of = lse; g.entropy_of = entropy; g.dlogp = dlogp; g.dentropy = dentropy;
   g.out = out->data; g.out_stride = out->stride; g.out_type = out->type;
   // a row's first run may begin up to seven columns before it

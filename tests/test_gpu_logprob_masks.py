@@ -12,8 +12,8 @@ import math
 import pytest
 import torch
 
-from test_gpu_logprob import U, check_forward, close, definition, gen, tr   # noqa: F401
-from training_reference import TYPES
+from test_gpu_logprob import U, check_forward, close, definition, gen, tiny, tr   # noqa: F401
+from training_reference import Framed, TYPES, half_step
 
 pytestmark = pytest.mark.gpu
 
@@ -66,3 +66,66 @@ def test_forward_of_rows_far_from_0(tr, vocab, dtype):   # noqa: F811
             for t in got:   # rows that are alike lie alike only where a row's size is a multiple of 16 bytes
                 if vocab % 8 == 0:
                     assert torch.equal(t, t[:len(x)].repeat(repeat, *[1] * (t.dim() - 1)))
+
+
+def check_far_gradient(got, x, want, tokens, dlogp, dentropy, scale, vocab):
+    """Against the gradient by 64-bit logits alone.  A probability is off by u (4 |z - lse| + 8) of itself as in
+    test_gpu_logprob.py, and by what lse is off by: as check_forward allows, or, beyond 1024 either way, where the row's own sum is
+    taken again by differences from its largest, by that sum's (V / 512 + 64) u and the rounding of its logarithm.  The entropy's part is
+    off by the same, times p, and by what the entropy is off by."""
+    scale, n = float(torch.tensor(scale)), (vocab / 512 + 64) * U
+    p, t, h = want["p"], torch.where(want["p"] > 0, want["logs"], 0.0), want["entropy"][:, None]
+    lse = want["lse"].abs().nan_to_num(posinf=math.inf)
+    e = torch.where(lse > 1024, n + 4 * U * (1 + math.log(vocab)), n + 4 * U * (want["near"] + lse))[:, None]
+    one = (torch.arange(vocab)[None] == tokens[:, None]).double()
+    dl, dh = torch.where(tokens < 0, 0.0, dlogp.double())[:, None], dentropy.double()[:, None]
+    rel, gone = U * (4 * t.abs() + 8) + e, torch.full_like(p, 2.0 ** -126)
+    value = dl * (one - p) - dh * p * (t + h)
+    bound = dl.abs() * (p * rel + gone + 2 * U * (one - p).abs() + U * one)
+    bound = bound + dh.abs() * ((p * (rel + 8 * U) + gone) * (t.abs() + h) + p * (e + entropy_bound(want, vocab)[:, None])) + 4 * U * value.abs()
+    nothing = (want["lse"] == -math.inf)[:, None]   # by the definition: all of the row's logits are -infinity
+    value, bound = torch.where(nothing, 0.0, scale * value), scale * bound + 4 * U * (scale * value).abs()
+    close(got, value, bound + half_step(got.dtype) * (value.abs() + bound) + tiny(got.dtype) + 2.0 ** -125)
+
+
+@pytest.mark.parametrize("vocab", [1, 1000, 9000, 32003])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gradient_of_rows_far_from_0(tr, vocab, dtype):   # noqa: F811
+    dtype = TYPES[dtype]
+    x = far_rows(vocab, dtype) if vocab > 1 else torch.tensor([[3.0], [-6e4], [1e4], [-math.inf], [torch.finfo(dtype).min]]).to(dtype)
+    tokens = (torch.arange(len(x)) * 331) % vocab
+    tokens[1::7] = -1
+    g = gen("far gradient", vocab)
+    dlogp, dh = torch.randn(len(x), generator=g), torch.randn(len(x), generator=g)
+    for scale in (0.5, 1.0, 1.25, 5.0):
+        want = definition(x.double(), tokens, scale, 0)
+        f = tr.moc_logprob_forward(x.cuda(), tokens.cuda(), scale=scale)
+        for out_type in {dtype, torch.float32}:
+            d = tr.moc_logprob_backward(x.cuda(), f.lse, tokens.cuda(), dlogp.cuda(), f.entropy, dh.cuda(), scale, dtype=out_type)
+            check_far_gradient(d.cpu(), x, want, tokens, dlogp, dh, scale, vocab)
+        only = tr.moc_logprob_backward(x.cuda(), f.lse, tokens.cuda(), dlogp.cuda(), scale=scale)
+        check_far_gradient(only.cpu(), x, want, tokens, dlogp, torch.zeros(len(x)), scale, vocab)
+        assert not only[1::7].any()
+        logits = x.cuda()
+        assert torch.equal(tr.moc_logprob_backward(logits, f.lse, tokens.cuda(), dlogp.cuda(), f.entropy, dh.cuda(), scale, out=logits),
+                           tr.moc_logprob_backward(x.cuda(), f.lse, tokens.cuda(), dlogp.cuda(), f.entropy, dh.cuda(), scale))
+
+
+def test_gradient_of_an_odd_matrix_far_from_0(tr):   # noqa: F811
+    """Rows at odd addresses in a larger matrix, more columns than a workgroup takes, written over the logits: far rows beside others,
+    nothing outside them."""
+    for dtype in TYPES.values():
+        rows, vocab = 6, 20001
+        x = (torch.randn(rows, vocab, generator=gen("odd", str(dtype))) * 2).to(dtype)
+        x[1] = torch.finfo(dtype).min
+        x[2] = 2000.0
+        x[4, 5:] = -3e4
+        x[4, :5] = -2e4
+        framed = Framed(rows, vocab, dtype, 3, 5)
+        framed.of(x)
+        tokens, ones = torch.arange(rows) * 4, torch.ones(rows)
+        want = definition(x.double(), tokens, 1.0, 0)
+        f = tr.moc_logprob_forward(framed.inner, tokens.cuda())
+        tr.moc_logprob_backward(framed.inner, f.lse, tokens.cuda(), ones.cuda(), f.entropy, ones.cuda(), out=framed.inner)
+        check_far_gradient(framed.inner.cpu(), x, want, tokens, ones, ones, 1.0, vocab)
+        assert framed.intact()
