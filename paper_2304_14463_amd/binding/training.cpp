@@ -719,20 +719,22 @@ PyObject* logprob_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const long top = PyLong_AsLong(a[3]);
   if (top == -1 && PyErr_Occurred()) throw python_error();
   if (top < 0 || top > 64 || top > x.cols) bad("top", "a number from 0 to 64, at most that of the columns, expected");
-  at::Tensor sums = room_for(x.values, at::kFloat, {3, x.rows}), top_logp, top_tokens;
+  // tensors of their own: views of one would share its version, and autograd refuses changes of a function's views
+  at::Tensor logp, lse = room_for(x.values, at::kFloat, {x.rows}), entropy = room_for(x.values, at::kFloat, {x.rows}), top_logp, top_tokens;
+  if (tokens.bytes) logp = room_for(x.values, at::kFloat, {x.rows});
   if (top > 0) {
     top_logp = room_for(x.values, at::kFloat, {x.rows, top});
     top_tokens = room_for(x.values, at::kLong, {x.rows, top});
   }
   const Work work = workspace(a[4], a[4] == Py_None ? calls.logprob_forward_work(x.rows, x.cols, (int32_t)top) : 0, x.values);
-  float* const room = static_cast<float*>(sums.data_ptr());
+  const auto floats = [](const at::Tensor& t) { return t.defined() ? static_cast<float*>(t.data_ptr()) : nullptr; };
   void* const stream = stream_for(x.values);
   const int code = released([&] {
-    return calls.logprob_forward(x.rows, x.cols, x.get(), tokens.v.data, tokens.bytes, (float)scale, (int32_t)top, tokens.bytes ? room : nullptr, room + x.rows, room + 2 * x.rows,
-                                 top > 0 ? static_cast<float*>(top_logp.data_ptr()) : nullptr, top > 0 ? static_cast<int64_t*>(top_tokens.data_ptr()) : nullptr, work.data, work.bytes,
+    return calls.logprob_forward(x.rows, x.cols, x.get(), tokens.v.data, tokens.bytes, (float)scale, (int32_t)top, floats(logp), floats(lse), floats(entropy), floats(top_logp),
+                                 top > 0 ? static_cast<int64_t*>(top_tokens.data_ptr()) : nullptr, work.data, work.bytes,
                                  stream);
   });
-  return Py_BuildValue("iNNNNN", code, tokens.bytes ? wrapped(sums.select(0, 0)).release() : none(), wrapped(sums.select(0, 1)).release(), wrapped(sums.select(0, 2)).release(),
+  return Py_BuildValue("iNNNNN", code, tokens.bytes ? wrapped(std::move(logp)).release() : none(), wrapped(std::move(lse)).release(), wrapped(std::move(entropy)).release(),
                        top > 0 ? wrapped(std::move(top_logp)).release() : none(), top > 0 ? wrapped(std::move(top_tokens)).release() : none());
   END_HANDLE_TH_ERRORS
 }
