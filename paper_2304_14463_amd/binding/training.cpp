@@ -128,6 +128,7 @@ struct Held {
   moc_matrix m = {};
   int64_t rows = 0, cols = 0;
   at::Tensor values;   // or the codes
+  at::Tensor scales;
   bool there = false, kept = false;
   const moc_matrix* get() const { return there ? &m : nullptr; }
   Span span() const {
@@ -162,7 +163,8 @@ Held held(PyObject* x, const char* what, int64_t rows = -1, int64_t cols = -1, b
   if (is_checkpoint(x)) {
     h.kept = true;
     h.values = attribute(x, name_codes, what);
-    const at::Tensor scales = attribute(x, name_scales, what);
+    h.scales = attribute(x, name_scales, what);
+    const at::Tensor& scales = h.scales;
     if (!h.values.is_cuda() || !scales.is_cuda() || h.values.device() != scales.device() || h.values.dim() != 2 || scales.dim() != 2)
       bad(what, "a checkpoint's codes and scales must be two-dimensional CUDA tensors on one device");
     h.rows = h.values.size(0);
@@ -287,6 +289,20 @@ void* stream_for(const at::Tensor& x) {
   return reinterpret_cast<void*>(address(handle));
 }
 
+// A tensor that a call has written to: autograd refuses graphs that have saved it, as after any change in place.
+void changed(const at::Tensor& t) {
+  if (t.defined() && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+// What of these the caller gave (`given`) has been written to, where the call was not refused.
+void changed(int code, std::initializer_list<std::pair<const Held*, PyObject*>> outputs) {
+  if (code != MOC_OK) return;
+  for (const auto& [h, given] : outputs) {
+    if (!THPVariable_Check(given) && !is_checkpoint(given)) continue;
+    changed(h->values);
+    changed(h->scales);
+  }
+}
+
 template <class F>
 int released(const F& f) {
   int code;
@@ -309,6 +325,7 @@ PyObject* checkpoint_write(PyObject*, PyObject* const* a, Py_ssize_t count) {
   apart(k, "out", x, "x");
   void* const stream = stream_for(x.values);
   const int code = released([&] { return calls.checkpoint_write(x.rows, x.cols, x.get(), k.get(), stream); });
+  changed(code, {{&k, a[2]}});
   return Py_BuildValue("iN", code, out.release());
   END_HANDLE_TH_ERRORS
 }
@@ -326,6 +343,7 @@ PyObject* checkpoint_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
   apart(y, "out", k, "kept");
   void* const stream = stream_for(k.values);
   const int code = released([&] { return calls.checkpoint_read(k.rows, k.cols, k.get(), act, y.get(), stream); });
+  changed(code, {{&y, a[3]}});
   return Py_BuildValue("iN", code, out.release());
   END_HANDLE_TH_ERRORS
 }
@@ -352,6 +370,7 @@ PyObject* norm_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return calls.norm_forward(x.rows, x.cols, x.get(), gamma.data, beta.data, gamma.data ? gamma.type : beta.type, (float)eps, y.get(), k.get(),
                               static_cast<float*>(mean.data_ptr()), static_cast<float*>(rstd.data_ptr()), stream);
   });
+  changed(code, {{&y, a[6]}, {&k, a[4]}});
   return Py_BuildValue("iNNNN", code, out.release(), wrapped(std::move(mean)).release(), wrapped(std::move(rstd)).release(), kept.release());
   END_HANDLE_TH_ERRORS
 }
@@ -392,6 +411,7 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return calls.norm_backward(d.rows, d.cols, d.get(), x.get(), gamma.data, gamma.type, static_cast<const float*>(mean.data), static_cast<const float*>(rstd.data), r.get(), dx.get(),
                                pg, pb, work.data, work.bytes, stream);
   });
+  changed(code, {{&dx, a[7]}});
   return Py_BuildValue("iNNN", code, out.release(), dgamma.release(), dbeta.release());
   END_HANDLE_TH_ERRORS
 }
@@ -423,6 +443,7 @@ PyObject* linear_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   void* const stream = stream_for(x.values);
   const int code =
       released([&] { return calls.linear_forward(rows, cin, cout, x.get(), w.get(), bias.data, bias.type, act, r.get(), y.get(), k.get(), work.data, work.bytes, stream); });
+  changed(code, {{&y, a[7]}, {&k, a[5]}});
   return Py_BuildValue("iNN", code, out.release(), kept.release());
   END_HANDLE_TH_ERRORS
 }
@@ -447,6 +468,7 @@ PyObject* linear_backward_input(PyObject*, PyObject* const* a, Py_ssize_t count)
   const Work work = workspace(a[6], a[6] == Py_None ? calls.linear_work(rows, cin, cout) : 0, d.values);
   void* const stream = stream_for(d.values);
   const int code = released([&] { return calls.linear_backward_input(rows, cin, cout, d.get(), w.get(), act, pre.get(), dx.get(), work.data, work.bytes, stream); });
+  changed(code, {{&dx, a[5]}});
   return Py_BuildValue("iN", code, out.release());
   END_HANDLE_TH_ERRORS
 }
@@ -476,6 +498,7 @@ PyObject* linear_backward_weight(PyObject*, PyObject* const* a, Py_ssize_t count
   const Work work = workspace(a[5], a[5] == Py_None ? calls.linear_work(rows, cin, cout) : 0, d.values);
   void* const stream = stream_for(d.values);
   const int code = released([&] { return calls.linear_backward_weight(rows, cin, cout, d.get(), x.get(), dw.get(), bias, work.data, work.bytes, stream); });
+  changed(code, {{&dw, a[4]}});
   return Py_BuildValue("iNN", code, out.release(), db.release());
   END_HANDLE_TH_ERRORS
 }
@@ -624,6 +647,7 @@ PyObject* residual_forward(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const int code = released([&] {
     return calls.residual_forward(b.rows, b.cols, x.get(), b.get(), gate.get(), gate.there ? gate.rows : 0, (float)scale, after.get(), before.get(), hr.get(), hn.get(), hk.get(), stream);
   });
+  changed(code, {{&hr, a[9]}, {&hn, a[10]}, {&hk, a[6]}});
   return Py_BuildValue("iNNNNN", code, r.release(), n.release(), after.stats.release(), before.stats.release(), kept.release());
   END_HANDLE_TH_ERRORS
 }
@@ -684,6 +708,7 @@ PyObject* residual_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return calls.residual_backward(rows, cols, dr.get(), dn.get(), r.get(), b.get(), gate.get(), gates, (float)scale, after.get(), before.get(), dx.get(), db.get(), &grads, work.data,
                                    work.bytes, stream);
   });
+  changed(code, {{&dx, a[13]}, {&db, a[14]}});
   return Py_BuildValue("iNNNNNNN", code, x_out.release(), b_out.release(), got[0].release(), got[1].release(), got[2].release(), got[3].release(), got[4].release());
   END_HANDLE_TH_ERRORS
 }
@@ -761,6 +786,7 @@ PyObject* logprob_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
     return calls.logprob_backward(x.rows, x.cols, x.get(), static_cast<const float*>(lse.data), static_cast<const float*>(entropy.data), dlogp.data ? tokens.v.data : nullptr, tokens.bytes,
                                   static_cast<const float*>(dlogp.data), static_cast<const float*>(dentropy.data), (float)scale, d.get(), stream);
   });
+  changed(code, {{&d, a[8]}});
   return Py_BuildValue("iN", code, out.release());
   END_HANDLE_TH_ERRORS
 }
@@ -793,6 +819,7 @@ struct Many {
     bool written;
   };
   std::vector<Piece> pieces;
+  std::vector<at::Tensor> outputs;
   at::Tensor like;
   // A contiguous CUDA tensor of n values (n < 0: any number).
   at::Tensor take(PyObject* x, const char* what, int64_t i, int64_t n, bool written) {
@@ -803,7 +830,12 @@ struct Many {
     same_device(like, t);
     const uintptr_t at = reinterpret_cast<uintptr_t>(t.data_ptr());
     if (t.numel() > 0) pieces.push_back({at, at + t.nbytes(), written});
+    if (written) outputs.push_back(t);
     return t;
+  }
+  void written(int code) const {
+    if (code != MOC_OK) return;
+    for (const at::Tensor& t : outputs) changed(t);
   }
   // What is written is apart from everything else.
   void check(const char* what) {
@@ -912,7 +944,9 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
   if (tensors == 0) return PyLong_FromLong(MOC_OK);
   many.check("adamw_step");
   void* const stream = stream_for(many.like);
-  return PyLong_FromLong(released([&] { return calls.adamw_step(tensors, list.data(), &rule, stream); }));
+  const int code = released([&] { return calls.adamw_step(tensors, list.data(), &rule, stream); });
+  many.written(code);
+  return PyLong_FromLong(code);
   END_HANDLE_TH_ERRORS
 }
 
@@ -958,6 +992,7 @@ PyObject* moments_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
   many.check("moments_read");
   void* const stream = stream_for(many.like);
   const int code = released([&] { return calls.moments_read(moments.count, list.data(), stream); });
+  if (a[2] != Py_None) many.written(code);
   return Py_BuildValue("iN", code, results.release());
   END_HANDLE_TH_ERRORS
 }

@@ -9,7 +9,9 @@ moc_norm_forward, dy, x or residual of moc_norm_backward, residual of moc_linear
 moc_linear_backward_input themselves (same type and strides).  There is no CPU fallback: a missing library or GPU raises.
 
 No call records a graph: results never require gradients, those of tensors that do included.  The gradients are calls of their
-own (moc_*_backward*); inside torch's autograd they belong into the backward of a torch.autograd.Function.
+own (moc_*_backward*); inside torch's autograd they belong into the backward of a torch.autograd.Function.  What a call is given to
+write to (parameters, moments, an `out`, a `keep`) counts as changed in place: autograd refuses a graph that has saved it before.  A captured
+graph's replay changes memory that torch does not hear of.
 
 A `Checkpoint` is an activation kept in 8 bits: a byte a value and a scale for 32 columns of a row.
 """
