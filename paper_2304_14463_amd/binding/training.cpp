@@ -821,6 +821,10 @@ struct Many {
   std::vector<Piece> pieces;
   std::vector<at::Tensor> outputs;
   at::Tensor like;
+  void expect(int64_t read, int64_t written) {
+    pieces.reserve((size_t)(read + written));
+    outputs.reserve((size_t)written);
+  }
   // A contiguous CUDA tensor of n values (n < 0: any number).
   at::Tensor take(PyObject* x, const char* what, int64_t i, int64_t n, bool written) {
     if (!THPVariable_Check(x)) refuse(PyExc_TypeError, item(what, i) + ": a CUDA tensor expected");
@@ -898,6 +902,7 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
   const bool copied = a[3] != Py_None, same_decay = PyFloat_Check(a[4]) || PyLong_Check(a[4]);
   const Items copies(copied ? a[3] : params.items(), "copies", tensors), decay(same_decay ? params.items() : a[4], "weight_decay", tensors);
   Many many;
+  many.expect(tensors + 3, 6 * tensors);
   std::vector<moc_adamw_tensor> list((size_t)tensors);
   for (int64_t i = 0; i < tensors; ++i) {
     moc_adamw_tensor& t = list[(size_t)i];
@@ -956,6 +961,7 @@ PyObject* moments_read(PyObject*, PyObject* const* a, Py_ssize_t count) {
   arguments(count, 3, "moments_read");
   const Items moments(a[0], "moments"), out(a[2] == Py_None ? moments.items() : a[2], "out", moments.count);
   Many many;
+  many.expect(4 * moments.count, 2 * moments.count);
   std::vector<moc_moments_tensor> list((size_t)moments.count);
   THPObjectPtr results(PyList_New(moments.count));
   if (!results) throw python_error();
