@@ -339,6 +339,8 @@ int moc_logprob_backward(int64_t rows, int64_t vocab, const moc_matrix* logits, 
  *   mix(low(i) ^ mix(high(i) ^ mix(t ^ mix(low(step) ^ mix(high(seed) ^ mix(low(seed)))))))
  * with low and high halves of 32 bits, the lower 16 for m, the upper for v, and
  *   mix(h):  h ^= h >> 16, h *= 0xF704BB15, h ^= h >> 15, h *= 0x371E2E67, h ^= h >> 16.
+ * t counts within a call: calls of one step (groups of parameters with rates of their
+ * own) need seeds of their own, or their tensors are rounded by the same bits.
  *
  * v below 2^-126 may count as 0.  All memory that is written is apart from all
  * other memory of the call.  A tensor of no values is left out.  No tensors:

@@ -296,7 +296,8 @@ def moc_adamw_step(params, grads, moments, lr, step, betas=(0.9, 0.999), eps=1e-
     bfloat16 tensors for the parameters' new values, or None.  Tensors are contiguous.  `step` counts from 1; `weight_decay`
     is a number, or one for each tensor; gradients are taken times `grad_scale`.  `lr`, `step` and `grad_scale` may be CUDA tensors of one
     value (float32, int64, float32), which are read when the step runs: a captured call then finds each replay's own.
-    `seed`: of the random bits that moments in 8 bits are rounded with (the step is mixed in)."""
+    `seed`: of the random bits that moments in 8 bits are rounded with (the step is mixed in, and each tensor's place in the call's list:
+    calls for groups of parameters within a step need different seeds, or the groups' tensors are rounded by the same bits)."""
     code = _call("adamw_step", stream, params, grads, moments, copies, weight_decay, lr, step, *betas, eps, grad_scale, seed)
     moc._check(code, "moc_adamw_step")
 
