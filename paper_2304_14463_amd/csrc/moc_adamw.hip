@@ -1,7 +1,7 @@
 // AdamW over many tensors at once, with moments in 32 bits or in 8, and what moments stand for.
 //
 // One pass over a tensor's values, bound by memory: 28 bytes a value with moments and gradients in 32 bits, 14 to 16 with
-// moments in 8: 150 M parameters in 32 bits with copies 834 us (5.4 TB/s), 537 M with moments in 8 bits 1660 us (5.2), their reading
+// moments in 8: the kernel over 150 M parameters in 32 bits with copies 834 us (5.4 TB/s), 537 M with moments in 8 bits 1660 us (5.2), their reading
 // back 626.  A launch takes up to kTensors tensors, whose descriptors travel in its arguments: nothing is copied to
 // the device first, and a captured launch keeps them.
 #include <type_traits>
@@ -27,7 +27,7 @@ struct Entry {
   int64_t count;
   uint32_t number;            // place in the caller's list
   float decay;
-  uint8_t param_type, grad_type, copy_type, whole;   // whole: of 8 bits
+  uint8_t param_type, grad_type, copy_type;
 };
 struct Factors {
   float lr, away, root, grad_scale;   // away = lr / (1 - beta1^step), root = 1 / sqrt(1 - beta2^step)
@@ -44,6 +44,8 @@ struct AdamwArgs {
 };
 static_assert(sizeof(AdamwArgs) <= 4096);
 
+// Two odd factors out of 150 pairs drawn at random: the pair by which a bit of the argument, flipped, most evenly flips each bit of
+// the result (0.9 points off one in two at the worst of all pairs of bits, over 200000 arguments).
 constexpr uint32_t mix(uint32_t h) {
   h ^= h >> 16;
   h *= 0xF704BB15u;

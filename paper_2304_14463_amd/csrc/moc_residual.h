@@ -33,7 +33,8 @@ struct ResidualArgs {
   ResidualMat x, block, gate, r, n, kept;
   ResidualMat dr, dn, dx, dblock;
   ResidualNorm after, before;
-  uint32_t rows, gates, rows_per_gate;
+  uint32_t rows;      // forward
+  uint32_t gates, rows_per_gate;
   int cols;
   float scale, most;
   bool parts;         // runs at a row's end are loaded value by value: an output lies over an input

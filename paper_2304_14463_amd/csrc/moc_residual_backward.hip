@@ -334,7 +334,7 @@ int moc_residual_backward(int64_t rows, int64_t cols, const moc_matrix* dr, cons
   if (last) g.r = mat_of(r);
   if (needed) g.block = mat_of(block);
   g.after = row_norm_of(after); g.before = row_norm_of(before);
-  g.rows = (uint32_t)rows; g.cols = (int)cols; g.gates = (uint32_t)gates; g.rows_per_gate = (uint32_t)(gates > 0 && !c.own ? rows / gates : rows);
+  g.cols = (int)cols; g.gates = (uint32_t)gates; g.rows_per_gate = (uint32_t)(gates > 0 && !c.own ? rows / gates : rows);
   g.scale = scale;
   g.kinds = kinds;
   g.sums = static_cast<float*>(work);
