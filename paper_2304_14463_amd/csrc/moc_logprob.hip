@@ -11,6 +11,7 @@
 // of 131072 with twenty 12 us (51 by one workgroup).
 // Backward: a pass over the logits and their gradient, 8192 columns a workgroup, runs at aligned addresses: 8192 x 131072 bf16
 // 690 us, 6.2 TB/s (843 where each load had a branch); four float32 values a lane (1247 x 32003 63 us, 83 with eight).
+// Times of one input again and again; where inputs change from pass to pass, 4999 x 32003 takes 72 us, the gradient of 1247 x 32003 69.
 #include <algorithm>
 
 #include "moc_rows.h"
@@ -63,7 +64,8 @@ struct Sums {
 // Up to kReach either way, scale2 * m is rounded by a quarter at most, so that the largest term is 2^(+-1/4) and all sums stay
 // in range.  Beyond it the rounding grows without bound (2^100 and more for masks of -1e9 or -1e30, and their w not a number
 // where a real logit comes after): what lies below counts as nothing beside whatever lies above, and a row of nothing else, or one with
-// logits above kReach, is taken again by row_again().
+// logits above kReach, is taken again by row_again().  4999 x 32000 fp32 masked by -1e9 or -1e30 106 us as by -infinity, 180
+// where the mask leaves nothing.
 constexpr float kReach = 0x1p23f;
 __device__ __forceinline__ float anchor(float m, float scale2) { return fmaxf(m * scale2, -kReach); }
 
